@@ -375,6 +375,135 @@ const char *relaysum_strerror(int code);
  * relaysum_step_static on the calling thread. */
 const char *relaysum_last_error(const relaysum_t *h);
 
+/* ---- layers on 8-bit rows -------------------------------------------------
+ *
+ * What n workers compute between two rounds when their models are
+ * transformers: the operators of a sub-layer for all workers in one launch,
+ * each worker with its own weights.  Weights are read where they lie, in the
+ * models' rows x[i], and weight gradients are written where the next round
+ * reads them, in the rows g[i].
+ *
+ *   norm         s = h + residual;  y = s * rstd * w,  rstd = 1 / sqrt(mean(s^2) + eps)
+ *                y leaves in 8 bits; for the gradient s is kept in 8 bits too
+ *   product      Y[t][c] = sum_k X[t][k] * W[c][k] of packed X and W, in integers
+ *   gradients    of the product from the packed X and W, of the norm from the packed s;
+ *                the rounding to 8 bits counts as the identity
+ *
+ * Packed rows.  A row of `width` entries is held as one int8 code per entry
+ * and one int8 exponent per group of entries; a group is the whole row
+ * (group 0) or 128 neighbouring entries (group 128):
+ *   value = code * 2^exponent, |code| <= 127, the exponent the smallest of
+ *   at least -126 that fits the group's largest entry, codes rounded to
+ *   nearest, halves to even;
+ *   exponent -128 marks a group with a NaN or an infinity: it stands for
+ *   NaN throughout.
+ * Scales are powers of two so that values are exact in bfloat16, which the
+ * gradients' products multiply in.  codes is [n][rows][stride] with stride =
+ * relaysum_packed_stride(width) and zeros behind the width; exponents are
+ * [n][rows][1], or [n][rows][stride / 128] for group 128.  Codes must be
+ * 16-byte aligned and codes behind the width zero.
+ *
+ * Every array is DEVICE memory of the current GPU, checked with the HIP
+ * runtime's pointer queries before anything is queued, and outputs share no
+ * memory with other arrays, except where a call says so.  Sums over a row and
+ * over tokens, and every product, are held in 32 bits or more.  Calls queue
+ * kernels on `hip_stream` (NULL = null stream), allocate nothing, copy
+ * nothing to the host, use no atomics (equal inputs give equal bits) and can
+ * be recorded by HIP stream capture.  They return RELAYSUM_OK or
+ * RELAYSUM_ERR_INVALID_ARG (nothing queued) or RELAYSUM_ERR_DEVICE;
+ * relaysum_layer_error() has the text.
+ *
+ * Limits: 1 <= n <= RELAYSUM_MAX_WORKERS, 0 <= rows or tokens (0: nothing to
+ * do, but weight gradients are set to 0), 1 <= width <= 32768 (up to there
+ * an integer sum of products fits 32 bits), 1 <= channels <= 2^24. */
+
+typedef enum relaysum_type {
+    RELAYSUM_FLOAT = 0,    /* binary32 */
+    RELAYSUM_BFLOAT = 1,   /* bfloat16 */
+    RELAYSUM_HALF = 2      /* binary16 */
+} relaysum_type;
+
+/* Rows of n workers: entry k of row t of worker i is entry
+ * i*worker_stride + t*row_stride + k of data.  Strides count entries and are
+ * not negative; rows that are written must not overlap.  Rows may start
+ * anywhere the type can. */
+typedef struct relaysum_rows {
+    void *data;
+    int32_t type;            /* relaysum_type */
+    int64_t worker_stride;   /* ignored for n == 1 */
+    int64_t row_stride;      /* ignored for one row */
+} relaysum_rows;
+
+/* Packed rows, dense. */
+typedef struct relaysum_packed {
+    int8_t *codes;
+    int8_t *exps;
+    int32_t group;           /* 0 or 128: the same for rows of up to 128 entries */
+} relaysum_packed;
+
+/* Codes from the start of a packed row to the next; -1 for a bad width. */
+int64_t relaysum_packed_stride(int64_t width);
+
+/* Pack rows (weights once a round, activations for a backward pass), and
+ * their values back into a type. */
+int relaysum_pack(int32_t n, int64_t rows, int64_t width, const relaysum_rows *v,
+                  const relaysum_packed *out, void *hip_stream);
+int relaysum_unpack(int32_t n, int64_t rows, int64_t width, const relaysum_packed *p,
+                    const relaysum_rows *out, void *hip_stream);
+
+/* Norm of every token's row.
+ *   h, residual, sum  rows of one type; sum = h + residual rounded to it, and
+ *            the norm is that of the rounded sum; residual and sum may both
+ *            be NULL (s = h).  sum may be h's or residual's own rows.
+ *   weight   float[width] of worker i at weight + i*weight_stride
+ *   y        out, group 0: what the product reads, and its gradient keeps
+ *   rstd     out, float[n][tokens]
+ *   saved    out, group 128, or NULL: s, for relaysum_rmsnorm_backward */
+int relaysum_rmsnorm(int32_t n, int64_t tokens, int64_t width, const relaysum_rows *h,
+                     const relaysum_rows *residual, const float *weight, int64_t weight_stride,
+                     float eps, const relaysum_rows *sum, const relaysum_packed *y, float *rstd,
+                     const relaysum_packed *saved, void *hip_stream);
+
+/* Gradients of the norm, with xh = rstd * s (s from saved) and u = dy * w:
+ *   ds = dsum + rstd * (u - xh * mean(u * xh)),   weight_grad = sum over tokens of dy * xh
+ *   dy, dsum, ds  rows of one type: the gradients of y, of the sum from
+ *            elsewhere (NULL: none) and of h and residual alike; ds may be
+ *            dy's or dsum's own rows
+ *   weight_grad   float rows, one of each worker (row_stride is not used),
+ *            overwritten
+ *   workspace     relaysum_rmsnorm_workspace bytes, 4-byte aligned (NULL if 0) */
+int64_t relaysum_rmsnorm_workspace(int32_t n, int64_t tokens, int64_t width);
+int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const relaysum_rows *dy,
+                              const relaysum_rows *dsum, const relaysum_packed *saved,
+                              const float *rstd, const float *weight, int64_t weight_stride,
+                              const relaysum_rows *ds, const relaysum_rows *weight_grad,
+                              void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* y[t][c] = sum_k x[t][k] * w[c][k] for every worker: x packed rows of tokens,
+ * w packed rows of channels (the output features), both group 0.  The sum is
+ * exact in integers; it is rounded to 24 bits and then to y's type. */
+int relaysum_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels,
+                    const relaysum_packed *x, const relaysum_packed *w, const relaysum_rows *y,
+                    void *hip_stream);
+
+/* dx[t][k] = sum_c dy[t][c] * w[c][k]; dx has dy's type. */
+int relaysum_linear_backward_input(int32_t n, int64_t tokens, int64_t width, int64_t channels,
+                                   const relaysum_rows *dy, const relaysum_packed *w,
+                                   const relaysum_rows *dx, void *hip_stream);
+
+/* weight_grad[c][k] = sum_t dy[t][c] * x[t][k], float rows, overwritten; x of
+ * either group (what relaysum_rmsnorm gave, or activations packed for this).
+ *   workspace   relaysum_linear_workspace bytes, 16-byte aligned (NULL if 0) */
+int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels);
+int relaysum_linear_backward_weight(int32_t n, int64_t tokens, int64_t width, int64_t channels,
+                                    const relaysum_rows *dy, const relaysum_packed *x,
+                                    const relaysum_rows *weight_grad, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
+
+/* Text of the calling thread's last failure in the calls on 8-bit rows (""
+ * after a call that succeeded). */
+const char *relaysum_layer_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -44,6 +44,11 @@ EXPORTED = (
     "relaysum_get_message", "relaysum_state_size", "relaysum_save_state",
     "relaysum_load_state", "relaysum_poison_next", "relaysum_strerror", "relaysum_last_error",
     "relaysum_step_static", "relaysum_kernel_path", "relaysum_consensus_distance",
+    # Layers on 8-bit rows, bound in layer.py.
+    "relaysum_packed_stride", "relaysum_pack", "relaysum_unpack", "relaysum_rmsnorm",
+    "relaysum_rmsnorm_workspace", "relaysum_rmsnorm_backward", "relaysum_linear",
+    "relaysum_linear_workspace", "relaysum_linear_backward_input",
+    "relaysum_linear_backward_weight", "relaysum_layer_error",
 )
 
 PATHS = ("tile", "dtree", "wide_dtree", "cluster", "wide", "two_pass", "dtree_seq",

@@ -1,0 +1,590 @@
+"""GPU: the layer operators on 8-bit rows against their plain 64-bit
+implementations (oracle/layer.py).
+
+Tolerances.  Packing and the product in integers are exact: equal bits.
+Floating sums: every product of the gradients' operands is exact, so a result
+is off by at most its additions' roundings, (terms + 8) * 2^-24 of the sum of
+its terms' sizes for any order of adding (doubled for adders that cut instead
+of rounding), and by the rounding to its own type.  The norm takes a few
+roundings per entry on top of its row sums' (of non-negative terms, at most
+width * 2^-24 relative; sums over a row are made of at most 32 + 10 steps)."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2110_04175_amd as rs
+from oracle import layer as plain
+from paper_2110_04175_amd import layer
+
+pytestmark = pytest.mark.gpu
+
+ULP = 2.0 ** -24
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+EPS = 1e-6
+
+
+def announce(msg):
+    sys.__stderr__.write(f"[gpu] {msg}\n")
+    sys.__stderr__.flush()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def normal(seed, *shape, std=1.0, dtype=torch.float32):
+    g = np.random.default_rng(seed).standard_normal(shape) * std
+    return torch.from_numpy(g.astype(np.float32)).cuda().to(dtype)
+
+
+def in_model(t, before=3, after=5, fill=7.0):
+    """(t copied into a view of rows of odd length, all of those rows)."""
+    n = t.shape[0]
+    flat = t.reshape(n, -1)
+    d = before + flat.shape[1] + after
+    d += 1 - d % 2
+    rows = torch.full((n, d), fill, device="cuda")
+    rows[:, before:before + flat.shape[1]] = flat
+    view = rows[:, before:before + flat.shape[1]]
+    return (view.unflatten(1, tuple(t.shape[1:])) if t.dim() > 2 else view), rows
+
+
+def untouched(view, rows, before=3, fill=7.0):
+    """Whether everything around the view still has its fill."""
+    size = view[0].numel()
+    return bool((rows[:, :before] == fill).all()) and bool((rows[:, before + size:] == fill).all())
+
+
+def same_packed(p, want):
+    codes, exps = want
+    return np.array_equal(p.codes.cpu().numpy(), codes) and np.array_equal(p.exps.cpu().numpy(), exps)
+
+
+WIDTHS = [1, 7, 16, 127, 128, 129, 511, 512, 520, 1001, 1024, 1030, 2048, 2056, 4100, 8192, 8200, 16390, 32768]
+
+
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_pack_and_unpack(width, group):
+    n, rows = (3, 5) if width < 8000 else (2, 2)
+    for dtype in TYPES:
+        announce(f"pack width={width} group={group} {dtype}")
+        v = normal(width, n, rows, width, std=0.3, dtype=dtype)
+        v[0, 0] = 0
+        v[-1, -1] *= 1e-3
+        p = layer.pack(v, group)
+        codes, exps = plain.pack(host(v), group)
+        assert same_packed(p, (codes, exps))
+        want = plain.values(codes, exps, width)
+        for out in TYPES:
+            got = layer.unpack(p, out)
+            assert torch.equal(got.cpu(), torch.from_numpy(want).to(out)), out
+
+
+def test_pack_extremes():
+    """Groups of zeros, the smallest and largest numbers, values that sit on a
+    scale's edge, NaN and infinities."""
+    rowsv = np.zeros((1, 9, 300), np.float32)
+    rowsv[0, 1, 0] = 2.0 ** -149
+    rowsv[0, 2, 5] = 3.4028234663852886e38
+    rowsv[0, 3, :3] = [127.0, 0.5, -1.5]
+    rowsv[0, 4, :3] = [np.nextafter(np.float32(127), np.float32(200)), 1.0, -3.0]
+    rowsv[0, 5, 7] = np.nan
+    rowsv[0, 6, 299] = np.inf
+    rowsv[0, 7, :] = 127 * 2.0 ** -126
+    rowsv[0, 8, 128:] = -np.inf
+    for group in (0, 128):
+        announce(f"pack extremes group={group}")
+        p = layer.pack(torch.from_numpy(rowsv).cuda(), group)
+        codes, exps = plain.pack(rowsv, group)
+        assert same_packed(p, (codes, exps))
+        back = host(layer.unpack(p, torch.float32))
+        # The largest number is held as 64 * 2^122, which rounds to an infinity.
+        with np.errstate(over="ignore"):
+            want = plain.values(codes, exps, 300).astype(np.float32)
+        np.testing.assert_array_equal(back, want)
+
+
+def test_pack_strides():
+    """Rows of models of odd length, workers inside tokens, broadcast rows."""
+    announce("pack strides")
+    v = normal(5, 4, 6, 200)
+    view, _ = in_model(v)
+    want = plain.pack(host(v), 0)
+    assert same_packed(layer.pack(view), want)
+    across = v.transpose(0, 1).contiguous().transpose(0, 1)
+    assert not across.is_contiguous() and same_packed(layer.pack(across), want)
+    one = normal(6, 1, 1, 200).expand(3, 4, 200)
+    assert same_packed(layer.pack(one), plain.pack(host(one), 0))
+    wide = torch.zeros(2, 3, 401, device="cuda", dtype=torch.bfloat16)
+    wide[:, :, 1:201] = normal(7, 2, 3, 200)
+    part = wide[:, :, 1:201]          # 2-byte aligned rows
+    assert same_packed(layer.pack(part, 128), plain.pack(host(part), 128))
+
+
+def check_norm(h, r, w, got, eps=EPS, keep=True):
+    s, y, rstd, saved = got
+    n, tokens, width = h.shape
+    if r is None:
+        assert s is h
+    else:
+        assert torch.equal(s, (h.float() + r.float()).to(h.dtype))
+    sh, wh = host(s), host(w)
+    want, want_rstd = plain.rmsnorm(sh, wh, eps)
+    # sum of squares: at most width / 16 + 10 steps, halved by the root; divide, root, reciprocal.
+    rel = (min(width, 42) + 8) * ULP
+    np.testing.assert_allclose(host(rstd), want_rstd, rtol=rel)
+    if keep:
+        assert same_packed(saved, plain.pack(sh, 128))
+    e = y.exps[:, :, :1].cpu().numpy().astype(np.int64)
+    top = np.max(np.abs(want), axis=2, keepdims=True)
+    slack = 1 + 2 * rel + 4 * ULP
+    assert (top <= 127 * 2.0 ** e * slack).all()
+    assert ((top * slack > 127 * 2.0 ** (e - 1)) | (e == -126)).all()
+    values = plain.values(y.codes.cpu().numpy(), y.exps.cpu().numpy(), width)
+    off = np.abs(values - want)
+    assert (off <= 0.5 * 2.0 ** e + (rel + 4 * ULP) * np.abs(want)).all()
+    assert (y.codes[:, :, width:] == 0).all()
+
+
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm(width, dtype):
+    announce(f"norm width={width} {dtype}")
+    n, tokens = (3, 5) if width < 8000 else (2, 2)
+    h, r = normal(1, n, tokens, width, dtype=dtype), normal(2, n, tokens, width, std=3, dtype=dtype)
+    w, _ = in_model(1 + 0.1 * normal(3, n, width))
+    check_norm(h, r, w, layer.rmsnorm(h, r, w, EPS))
+    check_norm(h, None, w, layer.rmsnorm(h, None, w, EPS))
+    s, y, rstd, saved = layer.rmsnorm(h, r, w, EPS, keep=False)
+    assert saved is None
+    check_norm(h, r, w, (s, y, rstd, None), keep=False)
+
+
+@pytest.mark.parametrize("n,tokens", [(1, 1), (16, 1), (1, 1000), (7, 33), (300, 2), (2, 0)])
+def test_norm_shapes(n, tokens):
+    announce(f"norm n={n} tokens={tokens}")
+    h, r = normal(1, n, tokens, 96, dtype=torch.bfloat16), normal(2, n, tokens, 96, dtype=torch.bfloat16)
+    w = normal(3, n, 96)
+    got = layer.rmsnorm(h, r, w, EPS)
+    if tokens:
+        check_norm(h, r, w, got)
+    else:
+        assert got[0].shape == (n, 0, 96) and got[1].codes.shape == (n, 0, 128)
+
+
+def test_norm_rows_that_are_special():
+    """A row of zeros gives zeros; one with a NaN or an infinity gives NaN,
+    and leaves the others alone; eps = 0 on a row of zeros gives NaN."""
+    announce("norm special rows")
+    h = normal(1, 1, 5, 256)
+    h[0, 1] = 0
+    h[0, 2, 9] = float("nan")
+    h[0, 3, 250] = float("inf")
+    r, w = torch.zeros_like(h), torch.ones(1, 256, device="cuda")
+    s, y, rstd, saved = layer.rmsnorm(h, r, w, EPS)
+    v = layer.unpack(y, torch.float32)
+    assert (v[0, 1] == 0).all() and torch.isnan(v[0, 2]).all() and torch.isnan(v[0, 3]).all()
+    assert saved.exps[0, 2].tolist() == [-128, saved.exps[0, 2, 1].item()]
+    assert saved.exps[0, 3, 1] == -128 and saved.exps[0, 3, 0] != -128
+    ok = [0, 4]
+    check_norm(h[:, ok], r[:, ok], w, layer.rmsnorm(h[:, ok].contiguous(), r[:, ok].contiguous(), w, EPS))
+    assert torch.isfinite(v[0, ok]).all()
+    v0 = layer.unpack(layer.rmsnorm(h, r, w, 0.0)[1], torch.float32)
+    assert torch.isnan(v0[0, 1]).all()
+
+
+def test_norm_strides():
+    """Rows across workers, parts of wider rows, a broadcast residual and weight."""
+    announce("norm strides")
+    base = normal(1, 6, 4, 331, dtype=torch.bfloat16)
+    h = base.transpose(0, 1)[:, :, 1:301]
+    r = normal(2, 1, 1, 300, dtype=torch.bfloat16).expand(4, 6, 300)
+    w = normal(3, 1, 300).expand(4, 300)
+    check_norm(h, r, w, layer.rmsnorm(h, r, w, EPS))
+
+
+def test_norm_in_place():
+    """The C call may write the sum over h's or the residual's own rows."""
+    announce("norm in place")
+    n, t, k = 2, 9, 200
+    h, r, w = normal(1, n, t, k), normal(2, n, t, k), normal(3, n, k)
+    want = layer.rmsnorm(h, r, w, EPS)
+    for over in (0, 1):
+        a, b = h.clone(), r.clone()
+        y = layer._new_packed(n, t, k, 0, h.device)
+        rstd = torch.empty(n, t, device="cuda")
+        ra, rb = layer._rows(a, "h", a.shape), layer._rows(b, "r", b.shape)
+        rc = layer._lib().relaysum_rmsnorm(n, t, k, ra, rb, w.data_ptr(), k, EPS, (ra, rb)[over],
+                                           y._c(), rstd.data_ptr(), None, rs._current_stream())
+        assert rc == 0
+        assert torch.equal((a, b)[over], want[0]) and torch.equal(y.codes, want[1].codes)
+
+
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_gradient(width, dtype):
+    n, tokens = (3, 37) if width < 3000 else (2, 3)
+    for given in (True, False):
+        announce(f"norm gradient width={width} {dtype} dsum={given}")
+        s = normal(1, n, tokens, width, std=2.0)
+        group = 128 if given else 0
+        saved = layer.pack(s, group)
+        rstd = (1 / torch.sqrt((s * s).mean(-1) + EPS)).contiguous()
+        dy = normal(2, n, tokens, width, dtype=dtype)
+        dsum = normal(3, n, tokens, width, dtype=dtype) if given else None
+        w, _ = in_model(1 + 0.1 * normal(4, n, width))
+        dw, around = in_model(torch.zeros(n, width, device="cuda"))
+        ds = layer.rmsnorm_backward(dy, dsum, saved, rstd, w, dw)
+        held = plain.values(saved.codes.cpu().numpy(), saved.exps.cpu().numpy(), width)
+        want, want_dw = plain.rmsnorm_backward(host(dy), None if dsum is None else host(dsum), held,
+                                               host(rstd), host(w))
+        xh = np.abs(held) * host(rstd)[:, :, None]
+        u = np.abs(host(dy) * host(w)[:, None, :])
+        size = host(rstd)[:, :, None] * (u + xh * np.mean(u * xh, axis=2, keepdims=True))
+        size = size + (0 if dsum is None else np.abs(host(dsum)))
+        # At most 42 + 10 additions in a row's mean, and 10 roundings per entry.
+        bound = 70 * ULP * size + 1.01 * ROUND[dtype] * np.abs(want) + TINY[dtype]
+        assert (np.abs(host(ds) - want) <= bound).all()
+        size = np.sum(np.abs(host(dy)) * xh, axis=1)
+        assert (np.abs(host(dw) - want_dw) <= (tokens + 8) * ULP * size).all()
+        assert untouched(dw, around)
+
+
+@pytest.mark.parametrize("n,tokens", [(1, 1), (16, 1), (1, 5000), (2, 0), (300, 2), (2000, 1)])
+def test_norm_gradient_shapes(n, tokens):
+    announce(f"norm gradient n={n} tokens={tokens}")
+    s = normal(1, n, tokens, 72)
+    saved = layer.pack(s, 128)
+    rstd = torch.ones(n, tokens, device="cuda")
+    dy = normal(2, n, tokens, 72)
+    w, dw = normal(3, n, 72), torch.full((n, 72), 9.0, device="cuda")
+    ds = layer.rmsnorm_backward(dy, None, saved, rstd, w, dw)
+    held = plain.values(saved.codes.cpu().numpy(), saved.exps.cpu().numpy(), 72)
+    want, want_dw = plain.rmsnorm_backward(host(dy), None, held, host(rstd), host(w))
+    u, xh = np.abs(host(dy) * host(w)[:, None, :]), np.abs(held)
+    size = u + xh * (np.mean(u * xh, axis=2, keepdims=True) if tokens else 0)
+    assert (np.abs(host(ds) - want) <= 70 * ULP * size).all()
+    assert (np.abs(host(dw) - want_dw) <= (tokens + 8) * ULP * np.sum(np.abs(host(dy)) * xh, axis=1)).all()
+
+
+def codes_of(seed, n, rows, width, group=0, spread=6):
+    """Packed rows with codes over the whole range and mixed exponents."""
+    g = np.random.default_rng(seed)
+    v = g.standard_normal((n, rows, width)) * 2.0 ** g.integers(-spread, spread + 1, (n, rows, 1))
+    codes, exps = plain.pack(v, group)
+    return layer.Packed(torch.from_numpy(codes).cuda(), torch.from_numpy(exps).cuda(), width)
+
+
+def held(p):
+    return plain.values(p.codes.cpu().numpy(), p.exps.cpu().numpy(), p.width)
+
+
+SHAPES = [  # n, tokens, width, channels
+    (1, 1, 1, 1), (2, 3, 17, 5), (16, 1, 200, 130), (3, 130, 128, 129), (1, 127, 1000, 128),
+    (2, 257, 300, 261), (5, 16, 129, 640), (1, 2, 4099, 33), (2, 33, 64, 1030), (40, 4, 96, 72),
+    (1, 700, 513, 520), (2, 64, 256, 256), (1, 8, 32768, 9), (2, 1, 2048, 700)]
+
+
+@pytest.mark.parametrize("n,tokens,width,channels", SHAPES)
+def test_linear(n, tokens, width, channels):
+    x, w = codes_of(1, n, tokens, width), codes_of(2, n, channels, width, spread=3)
+    exact = plain.linear(held(x), held(w)) if width < 5000 else None
+    if exact is None:
+        exact = np.matmul(held(x), held(w).transpose(0, 2, 1))
+    for dtype in TYPES:
+        announce(f"linear {n} {tokens} {width} {channels} {dtype}")
+        y = layer.linear(x, w, dtype)
+        # The integer sum times a power of two is exact in 64 bits.
+        want = torch.from_numpy(exact.astype(np.float32)).to(dtype)
+        assert torch.equal(y.cpu(), want)
+
+
+def test_linear_extremes():
+    """The largest sums of 32,768 products, and scales at both ends."""
+    announce("linear extremes")
+    k = 32768
+    codes = torch.full((1, 2, k), 127, dtype=torch.int8, device="cuda")
+    codes[0, 1] = -127
+    x = layer.Packed(codes, torch.tensor([[[0], [0]]], dtype=torch.int8, device="cuda"), k)
+    y = layer.linear(x, x, torch.float32)
+    top = float(127 * 127 * k)
+    assert y.tolist() == [[[top, -top], [-top, top]]]
+    e = torch.tensor([[[122], [-126]]], dtype=torch.int8, device="cuda")
+    x = layer.Packed(codes, e, k)
+    y = layer.linear(x, x, torch.float32)
+    assert y[0, 0, 0] == float("inf") and y[0, 1, 1] == 0 and y[0, 0, 1] == -top * 2.0 ** -4
+    e = torch.tensor([[[0], [-128]]], dtype=torch.int8, device="cuda")
+    y = layer.linear(layer.Packed(codes, e, k), layer.Packed(codes, torch.zeros_like(e), k), torch.float32)
+    assert torch.isfinite(y[0, 0]).all() and torch.isnan(y[0, 1]).all()
+    y = layer.linear(layer.Packed(codes, torch.zeros_like(e), k), layer.Packed(codes, e, k), torch.float32)
+    assert torch.isfinite(y[0, :, 0]).all() and torch.isnan(y[0, :, 1]).all()
+
+
+@pytest.mark.parametrize("n,tokens,width,channels", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_gradients(n, tokens, width, channels, dtype):
+    announce(f"linear gradients {n} {tokens} {width} {channels} {dtype}")
+    w = codes_of(2, n, channels, width, spread=3)
+    dy = normal(3, n, tokens, channels, std=1e-2, dtype=dtype)
+    dx = layer.linear_backward_input(dy, w)
+    assert dx.dtype == dtype
+    a, b = host(dy), held(w)
+    want, size = np.matmul(a, b), np.matmul(np.abs(a), np.abs(b))
+    bound = 2 * (channels + 8) * ULP * size + 1.01 * ROUND[dtype] * np.abs(want) + TINY[dtype]
+    assert (np.abs(host(dx) - want) <= bound).all()
+    for group in (0, 128):
+        x = codes_of(4, n, tokens, width, group)
+        dw, around = in_model(torch.zeros(n, channels, width, device="cuda"))
+        layer.linear_backward_weight(dy, x, dw)
+        b = held(x)
+        want = np.matmul(a.transpose(0, 2, 1), b)
+        size = np.matmul(np.abs(a).transpose(0, 2, 1), np.abs(b))
+        assert (np.abs(host(dw) - want) <= 2 * (tokens + 8) * ULP * size).all()
+        assert untouched(dw, around)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,tokens,width,channels", [(1, 4000, 96, 40), (2, 1601, 260, 70), (1, 20011, 64, 64)])
+def test_weight_gradient_over_many_tokens(n, tokens, width, channels, dtype):
+    """A long sum for few results, in parts that are joined."""
+    announce(f"weight gradient {n} {tokens} {width} {channels} {dtype}")
+    assert layer._lib().relaysum_linear_workspace(n, tokens, width, channels) > 0
+    x, dy = codes_of(4, n, tokens, width), normal(3, n, tokens, channels, std=1e-2, dtype=dtype)
+    dw, around = in_model(torch.zeros(n, channels, width, device="cuda"))
+    layer.linear_backward_weight(dy, x, dw)
+    a, b = host(dy), held(x)
+    want = np.matmul(a.transpose(0, 2, 1), b)
+    size = np.matmul(np.abs(a).transpose(0, 2, 1), np.abs(b))
+    assert (np.abs(host(dw) - want) <= 2 * (tokens + 8) * ULP * size).all()
+    assert untouched(dw, around)
+    again = torch.empty_like(want_ := dw.contiguous())
+    layer.linear_backward_weight(dy, x, again)
+    assert torch.equal(again, want_)
+
+
+def test_gradients_without_tokens():
+    """No tokens: the weight gradients are zeros, and nothing else is touched."""
+    announce("gradients without tokens")
+    x = layer.pack(torch.zeros(2, 0, 40, device="cuda"))
+    dy = torch.zeros(2, 0, 30, device="cuda")
+    dw, around = in_model(torch.full((2, 30, 40), 5.0, device="cuda"))
+    layer.linear_backward_weight(dy, x, dw)
+    assert (dw == 0).all() and untouched(dw, around)
+    w = layer.pack(torch.ones(2, 30, 40, device="cuda"))
+    assert layer.linear_backward_input(dy, w).shape == (2, 0, 40)
+    assert layer.linear(x, w).shape == (2, 0, 30)
+    assert layer.unpack(x).shape == (2, 0, 40)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_pass_on_what_is_no_number(dtype):
+    """A NaN in dY reaches its token's dX and its channel's dW, an infinity
+    stays one; a token held as NaN reaches every dW, a channel every dX."""
+    announce(f"gradients of NaN {dtype}")
+    n, t, k, c = 1, 70, 40, 50
+    ones = torch.ones(n, t, k, device="cuda")
+    x, w = layer.pack(ones), layer.pack(torch.ones(n, c, k, device="cuda"))
+    dy = torch.ones(n, t, c, device="cuda", dtype=dtype)
+    dy[0, 3, 4] = float("nan")
+    dy[0, 66, 7] = float("-inf")
+    dx = layer.linear_backward_input(dy, w)
+    assert torch.isnan(dx[0, 3]).all() and (dx[0, 66] == float("-inf")).all()
+    fine = [i for i in range(t) if i not in (3, 66)]
+    assert (dx[0, fine] == c).all()
+    dw = torch.zeros(n, c, k, device="cuda")
+    layer.linear_backward_weight(dy, x, dw)
+    assert torch.isnan(dw[0, 4]).all() and (dw[0, 7] == float("-inf")).all()
+    fine = [i for i in range(c) if i not in (4, 7)]
+    assert (dw[0, fine] == t).all()
+    ones[0, 69, 39] = float("nan")
+    layer.linear_backward_weight(torch.ones_like(dy), layer.pack(ones), dw)
+    assert torch.isnan(dw).all()
+    layer.linear_backward_weight(torch.ones_like(dy), layer.pack(ones.repeat(1, 1, 5), 128), big := torch.zeros(n, c, 5 * k, device="cuda"))
+    assert torch.isfinite(big[0, :, 128:]).sum() == 0 or torch.isnan(big[0, :, :128]).all()
+
+
+def test_gradient_strides():
+    """dY as part of wider rows, workers inside tokens, and broadcast."""
+    announce("gradient strides")
+    n, t, k, c = 3, 20, 70, 90
+    w, x = codes_of(2, n, c, k), codes_of(4, n, t, k)
+    base = normal(5, t, n, 2 * c + 1, dtype=torch.bfloat16)
+    for dy in (base.transpose(0, 1)[:, :, 1:c + 1], normal(6, n, 1, c).expand(n, t, c),
+               normal(7, 1, t, c, dtype=torch.float16).expand(n, t, c)):
+        a = host(dy)
+        dx = layer.linear_backward_input(dy, w)
+        want, size = np.matmul(a, held(w)), np.matmul(np.abs(a), np.abs(held(w)))
+        bound = 2 * (c + 8) * ULP * size + 1.01 * ROUND[dy.dtype] * np.abs(want) + TINY[dy.dtype]
+        assert (np.abs(host(dx) - want) <= bound).all()
+        dw = torch.zeros(n, c, k, device="cuda")
+        layer.linear_backward_weight(dy, x, dw)
+        want = np.matmul(a.transpose(0, 2, 1), held(x))
+        size = np.matmul(np.abs(a).transpose(0, 2, 1), np.abs(held(x)))
+        assert (np.abs(host(dw) - want) <= 2 * (t + 8) * ULP * size).all()
+
+
+def test_offsets_past_32_bits():
+    """Weights and their gradient behind more than 2^31 entries of model rows,
+    tokens behind more than 2^32 bytes of activations."""
+    announce("offsets past 32 bits")
+    d = (1 << 31) + 12_345
+    x = torch.empty(2, d, device="cuda")
+    at = d - 300 * 64 - 11
+    view = x[:, at:at + 300 * 64].unflatten(1, (300, 64))
+    small = normal(1, 2, 300, 64)
+    view.copy_(small)
+    p = layer.pack(view)
+    assert same_packed(p, plain.pack(host(small), 0))
+    tok, dy = codes_of(2, 2, 50, 64), normal(3, 2, 50, 300)
+    layer.linear_backward_weight(dy, tok, view)
+    dw = torch.zeros(2, 300, 64, device="cuda")
+    layer.linear_backward_weight(dy, tok, dw)
+    assert torch.equal(view, dw)
+    del x, view
+    big = torch.zeros(3, 1 << 22, 256, dtype=torch.bfloat16, device="cuda")
+    big[2, -5:] = normal(4, 5, 256)
+    s, y, rstd, saved = layer.rmsnorm(big, None, torch.ones(3, 256, device="cuda"), EPS)
+    part = layer.rmsnorm(big[2:, -5:].contiguous(), None, torch.ones(1, 256, device="cuda"), EPS)
+    assert torch.equal(y.codes[2, -5:], part[1].codes[0])
+    assert torch.equal(saved.codes[2, -5:], part[3].codes[0]) and torch.equal(rstd[2, -5:], part[2][0])
+    w = codes_of(5, 3, 8, 256)
+    out = layer.linear(y, w)
+    assert torch.equal(out[2, -5:], layer.linear(part[1], layer.Packed(w.codes[2:].contiguous(), w.exps[2:].contiguous(), 256))[0])
+    assert torch.equal(layer.unpack(y)[2, -5:], layer.unpack(part[1])[0])
+
+
+def test_on_a_stream_of_its_own_and_in_a_graph():
+    """A recorded sub-layer, replayed with new inputs, gives what eager calls give."""
+    announce("stream and graph")
+    n, t, k, c = 4, 96, 160, 200
+    h, r = normal(1, n, t, k, dtype=torch.bfloat16), normal(2, n, t, k, dtype=torch.bfloat16)
+    nw, wv = 1 + 0.1 * normal(3, n, k), normal(4, n, c, k, std=0.1)
+    dy = normal(5, n, t, c, std=1e-2, dtype=torch.bfloat16)
+    dnw, dw = torch.zeros_like(nw), torch.zeros_like(wv)
+
+    def step():
+        w = layer.pack(wv)
+        s, y, rstd, saved = layer.rmsnorm(h, r, nw, EPS)
+        out = layer.linear(y, w)
+        layer.linear_backward_weight(dy, y, dw)
+        dn = layer.linear_backward_input(dy, w)
+        ds = layer.rmsnorm_backward(dn, None, saved, rstd, nw, dnw)
+        return s, out, ds, dnw, dw
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = [v.clone() for v in step()]
+    torch.cuda.current_stream().wait_stream(side)
+    eager = [v.clone() for v in step()]
+    assert all(torch.equal(a, b) for a, b in zip(first, eager))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for k2 in range(4):
+        h.copy_(normal(10 + k2, n, t, k))
+        wv.copy_(normal(20 + k2, n, c, k, std=0.1))
+        dw.zero_()
+        graph.replay()
+        got = [v.clone() for v in outs]
+        torch.cuda.synchronize()
+        eager = [v.clone() for v in step()]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, eager)), k2
+
+
+def test_gradients_against_differences():
+    """The sub-layer's gradient of sum dy * y + dsum * s, with y the product of
+    the held rows, against differences of the plain norm and product (no
+    rounding to 8 bits in them).  The product is linear in each operand and so
+    are the differences; the norm's curvature over a step of 2^-7 of a row of
+    size 1 is below 2^-12 of the gradient's size."""
+    announce("gradients against differences")
+    n, t, k, c = 2, 5, 24, 12
+    h, nw = normal(1, n, t, k), 1 + 0.1 * normal(2, n, k)
+    wv, dy, dsum = normal(3, n, c, k, std=0.3), normal(4, n, t, c), normal(5, n, t, k)
+    s, y, rstd, saved = layer.rmsnorm(h, None, nw, EPS)
+    w = layer.pack(wv)
+    dw, dnw = torch.zeros_like(wv), torch.zeros_like(nw)
+    layer.linear_backward_weight(dy, y, dw)
+    dn = layer.linear_backward_input(dy, w)
+    ds = layer.rmsnorm_backward(dn, dsum, saved, rstd, nw, dnw)
+
+    hs, ns, ws = held(saved), host(nw), held(w)
+
+    def f_norm(s, g):
+        # rstd belongs to the unrounded rows: the plain norm is taken at the held ones.
+        return np.sum(host(dn) * plain.rmsnorm(s, g, EPS)[0]) + np.sum(host(dsum) * s)
+
+    step = 2.0 ** -7
+    # The held rows are off by 2^-7 of a group's largest entry, about 3 here:
+    # at most 2^-5 of the gradient's size through rstd and xh.
+    size = np.abs(host(ds)).max()
+    for at in [(0, 0, 0), (1, 4, 23), (0, 3, 7), (1, 1, 11)]:
+        p = np.zeros_like(hs)
+        p[at] = step
+        d = (f_norm(hs + p, ns) - f_norm(hs - p, ns)) / (2 * step)
+        assert abs(d - host(ds)[at]) <= 2.0 ** -5 * size
+    for at in [(0, 0), (1, 23), (0, 9)]:
+        p = np.zeros_like(ns)
+        p[at] = step
+        d = (f_norm(hs, ns + p) - f_norm(hs, ns - p)) / (2 * step)
+        assert abs(d - host(dnw)[at]) <= 2.0 ** -5 * np.abs(host(dnw)).max()
+    xs = held(y)
+    for at in [(0, 0, 0), (1, 11, 23), (0, 5, 6)]:
+        p = np.zeros_like(ws)
+        p[at] = step
+        d = np.sum(host(dy) * (plain.linear(xs, ws + p) - plain.linear(xs, ws - p))) / (2 * step)
+        assert abs(d - host(dw)[at]) <= 2 * (t + 8) * ULP * np.abs(host(dw)).max() + 1e-9
+
+
+def test_calls_refuse_what_they_cannot_take():
+    announce("refusals")
+    x, w = codes_of(1, 2, 3, 64), codes_of(2, 2, 4, 64)
+    dy = torch.zeros(2, 3, 4, device="cuda")
+    with pytest.raises(ValueError):
+        layer.pack(torch.zeros(2, 64, device="cuda"))                      # two axes
+    with pytest.raises(ValueError):
+        layer.pack(torch.zeros(2, 3, 64, device="cuda", dtype=torch.float64))
+    with pytest.raises(ValueError):
+        layer.pack(torch.zeros(2, 64, 3, device="cuda").transpose(1, 2))   # last axis not dense
+    with pytest.raises(ValueError):
+        layer.pack(torch.zeros(2, 3, 64, device="cuda"), 64)
+    with pytest.raises(ValueError):
+        layer.pack(torch.zeros(1, 1, 32769, device="cuda"))
+    with pytest.raises(ValueError):
+        layer.unpack(x, torch.int8)
+    with pytest.raises(ValueError):
+        layer.linear(x, codes_of(1, 2, 4, 65))
+    with pytest.raises(rs.RelaySumError):
+        layer.linear(codes_of(1, 2, 3, 256, 128), codes_of(2, 2, 4, 256))   # grouped
+    with pytest.raises(ValueError):
+        layer.linear_backward_input(dy[:, :, :3], w)
+    with pytest.raises(ValueError):
+        layer.linear_backward_weight(dy, x, torch.zeros(2, 4, 64, device="cuda", dtype=torch.bfloat16))
+    with pytest.raises(rs.RelaySumError):                                   # rows overlap
+        layer.linear_backward_weight(dy, x, torch.zeros(4, 64, device="cuda").expand(2, 4, 64))
+    with pytest.raises(ValueError):
+        layer.rmsnorm(torch.zeros(2, 3, 64, device="cuda"), torch.zeros(2, 3, 63, device="cuda"),
+                      torch.zeros(2, 64, device="cuda"))
+    with pytest.raises(ValueError):
+        layer.rmsnorm(torch.zeros(2, 3, 64, device="cuda"), None, torch.zeros(2, 64, device="cuda").half())
+    with pytest.raises(TypeError):
+        layer.rmsnorm(torch.zeros(2, 3, 64, device="cuda"), None, torch.zeros(2, 64))
+    # The C calls: host memory, and an array that reaches past its allocation.
+    lib, ok = layer._lib(), torch.zeros(1 << 20, dtype=torch.int8, device="cuda")
+    hostv = np.zeros(64, np.float32)
+    p = layer._CPacked(ok.data_ptr(), ok.data_ptr() + 4096, 0)
+    assert lib.relaysum_pack(1, 1, 64, layer.Rows(hostv.ctypes.data, 0, 64, 64), p, None) == -1
+    assert b"device memory" in lib.relaysum_layer_error()
+    # Past the end of an allocation of its own, and of everything near it.
+    src = torch.zeros(1 << 16, device="cuda")
+    far = layer.Rows(src.data_ptr(), 0, 0, 1 << 40)
+    p = layer._CPacked(ok.data_ptr(), ok.data_ptr() + 4096, 0)
+    assert lib.relaysum_pack(1, 2, 64, far, p, None) == -1
+    assert b"device memory" in lib.relaysum_layer_error()

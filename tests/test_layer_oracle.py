@@ -1,0 +1,179 @@
+"""CPU: the 64-bit plain layer operators are pinned to their definitions, and
+the library's layer calls refuse bad arguments before they reach a device."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2110_04175_amd as rs
+from oracle import layer as plain
+from paper_2110_04175_amd import layer
+
+
+@pytest.mark.parametrize("a,e", [
+    (0.0, -126), (127.0, 0), (np.nextafter(127.0, 200), 1), (1.0, -6), (63.5, -1), (63.6, 0),
+    (2.0 ** -140, -126), (127 * 2.0 ** -126, -126), (127 * 2.0 ** -125, -125),
+    (3.4028234663852886e38, 122), (np.inf, -128), (np.nan, -128)])
+def test_exponents(a, e):
+    assert plain.exponent(a) == e
+
+
+def test_packing_by_hand():
+    v = np.zeros((1, 1, 130))
+    v[0, 0, :4] = [127.0, -1.5, 0.5, 2.5]      # halves go to even
+    v[0, 0, 128] = -254.0
+    codes, exps = plain.pack(v, 128)
+    assert exps.tolist() == [[[0, 1]]] and codes.shape == (1, 1, 256)
+    assert codes[0, 0, :4].tolist() == [127, -2, 0, 2] and codes[0, 0, 128] == -127
+    codes, exps = plain.pack(v, 0)
+    assert exps.tolist() == [[[1]]]
+    assert codes[0, 0, :4].tolist() == [64, -1, 0, 1]       # 63.5 and 0.25 apart from halves
+    assert plain.values(codes, exps, 130)[0, 0, 128] == -254.0
+
+
+def test_a_group_that_is_no_number():
+    v = np.ones((1, 2, 256))
+    v[0, 0, 3] = np.nan
+    v[0, 1, 200] = -np.inf
+    codes, exps = plain.pack(v, 128)
+    assert exps[0].tolist() == [[-128, -6], [-6, -128]]
+    back = plain.values(codes, exps, 256)
+    assert np.isnan(back[0, 0, :128]).all() and (back[0, 0, 128:] == 1).all()
+
+
+def test_norm_gradient_against_differences():
+    """Of f = sum dy * y + sum dsum * s at rows whose rstd is that of s."""
+    rng = np.random.default_rng(1)
+    n, t, k = 2, 3, 7
+    s, dy, dsum = (rng.standard_normal((n, t, k)) for _ in range(3))
+    w = 1 + 0.1 * rng.standard_normal((n, k))
+
+    def f(s, w):
+        return np.sum(dy * plain.rmsnorm(s, w, 1e-6)[0]) + np.sum(dsum * s)
+
+    ds, dw = plain.rmsnorm_backward(dy, dsum, s, plain.rmsnorm(s, w, 1e-6)[1], w)
+    h = 1e-6
+    for at in np.ndindex(s.shape):
+        p = np.zeros_like(s)
+        p[at] = h
+        assert abs((f(s + p, w) - f(s - p, w)) / (2 * h) - ds[at]) < 1e-7
+    for at in np.ndindex(w.shape):
+        p = np.zeros_like(w)
+        p[at] = h
+        assert abs((f(s, w + p) - f(s, w - p)) / (2 * h) - dw[at]) < 1e-7
+
+
+def test_product_gradients_against_differences():
+    rng = np.random.default_rng(2)
+    x, w, dy = rng.standard_normal((2, 3, 4)), rng.standard_normal((2, 5, 4)), rng.standard_normal((2, 3, 5))
+    dx, dw = plain.linear_backward(dy, x, w)
+    h = 1e-4     # the function is linear in each: differences are exact up to rounding
+    for a, d, f in ((x, dx, lambda a: np.sum(dy * plain.linear(a, w))),
+                    (w, dw, lambda a: np.sum(dy * plain.linear(x, a)))):
+        for at in np.ndindex(a.shape):
+            p = np.zeros_like(a)
+            p[at] = h
+            assert abs((f(a + p) - f(a - p)) / (2 * h) - d[at]) < 1e-9
+
+
+# ---- refusals that need no device ---------------------------------------------------
+
+
+def _rows(data=1 << 20, type=0, ws=64, rs_=64):
+    return layer.Rows(data, type, ws, rs_)
+
+
+def _packed(codes=1 << 30, exps=1 << 31, group=0):
+    return layer._CPacked(codes, exps, group)
+
+
+def _text():
+    return rs.load_library().relaysum_layer_error().decode()
+
+
+@pytest.mark.parametrize("n,rows,width,v,out,says", [
+    (0, 1, 64, _rows(), _packed(), "n must be"),
+    (1, -1, 64, _rows(), _packed(), "rows must be"),
+    (1, 1, 0, _rows(), _packed(), "width"),
+    (1, 1, 32769, _rows(), _packed(), "width"),
+    (1 << 24, 1 << 30, 64, _rows(), _packed(), "2^50"),
+    (1, 1, 64, None, _packed(), "v must not be NULL"),
+    (1, 1, 64, _rows(data=None), _packed(), "v must not be NULL"),
+    (1, 1, 64, _rows(data=(1 << 20) + 2), _packed(), "4-byte aligned"),
+    (1, 1, 64, _rows(type=3), _packed(), "unknown type"),
+    (2, 1, 64, _rows(ws=-64), _packed(), "stride"),
+    (2, 1, 64, _rows(ws=1 << 44), _packed(), "stride"),
+    (1, 1, 64, _rows(), None, "out must not be NULL"),
+    (1, 1, 64, _rows(), _packed(group=64), "group"),
+    (1, 1, 64, _rows(), _packed(codes=(1 << 30) + 8), "16-byte aligned"),
+    (1, 1, 64, _rows(), _packed(codes=1 << 20), "share memory"),
+])
+def test_pack_refuses(n, rows, width, v, out, says):
+    lib = layer._lib()
+    rc = lib.relaysum_pack(n, rows, width, v, out, None)
+    assert rc == rs.RELAYSUM_ERR_INVALID_ARG
+    assert says in _text()
+
+
+def test_unpack_refuses_rows_that_overlap():
+    lib = layer._lib()
+    for out in (_rows(ws=0), _rows(ws=64, rs_=32), _rows(ws=32, rs_=64)):
+        assert lib.relaysum_unpack(2, 2, 64, _packed(), out, None) == rs.RELAYSUM_ERR_INVALID_ARG
+        assert "overlap" in _text()
+
+
+def test_norm_refuses():
+    lib = layer._lib()
+    h, w, r, y, s = _rows(), 2 << 20, 3 << 20, _packed(), _packed(5 << 30, 6 << 30, 128)
+
+    def call(res=None, out=None, y=y, saved=s, eps=1e-6, weight=w):
+        return lib.relaysum_rmsnorm(1, 1, 256, h, res, weight, 256, eps, out, y, r, saved, None)
+
+    bad = rs.RELAYSUM_ERR_INVALID_ARG
+    assert call(res=_rows(4 << 20)) == bad and "together" in _text()
+    assert call(res=_rows(4 << 20, 1), out=_rows(5 << 20)) == bad and "one type" in _text()
+    assert call(y=_packed(group=128)) == bad and "whole rows" in _text()
+    assert call(saved=_packed(5 << 30, 6 << 30, 0)) == bad and "128" in _text()
+    assert call(eps=-1.0) == bad and "eps" in _text()
+    assert call(eps=float("nan")) == bad and "eps" in _text()
+    assert call(weight=None) == bad and "weight" in _text()
+
+
+def test_gradients_refuse():
+    lib = layer._lib()
+    bad = rs.RELAYSUM_ERR_INVALID_ARG
+    need = lib.relaysum_rmsnorm_workspace(4, 4096, 512)
+    assert need > 0
+    args = (4, 4096, 512, _rows(0x100000000, 1, 4096 * 512, 512), None,
+            _packed(0x200000000, 0x300000000, 128), 0x400000000, 0x500000000, 512,
+            _rows(0x600000000, 1, 4096 * 512, 512), _rows(0x700000000, 0, 512, 0))
+    assert lib.relaysum_rmsnorm_backward(*args, 0x800000000, need - 1, None) == bad
+    assert "workspace" in _text()
+    assert lib.relaysum_rmsnorm_backward(*args, None, need, None) == bad and "workspace" in _text()
+    args = args[:10] + (_rows(0x700000000, 1, 512, 0), 0x800000000, need, None)
+    assert lib.relaysum_rmsnorm_backward(*args) == bad and "float" in _text()
+    assert lib.relaysum_linear(1, 1, 64, 0, _packed(), _packed(), _rows(), None) == bad
+    assert "channels" in _text()
+    assert lib.relaysum_linear(1, 1, 256, 64, _packed(group=128), _packed(3 << 30, 7 << 30), _rows(),
+                               None) == bad and "whole" in _text()
+    assert lib.relaysum_linear_backward_input(1, 1, 64, 64, _rows(type=1), _packed(),
+                                              _rows(2 << 20), None) == bad and "type" in _text()
+    assert lib.relaysum_linear_workspace(0, 1, 64, 64) == -1
+    assert lib.relaysum_rmsnorm_workspace(1, -1, 64) == -1
+
+
+def test_strides_of_codes():
+    lib = layer._lib()
+    for width, stride in ((1, 128), (128, 128), (129, 256), (32768, 32768), (0, -1), (32769, -1)):
+        assert lib.relaysum_packed_stride(width) == stride
+        if stride > 0:
+            assert layer.packed_stride(width) == stride == plain.stride_of(width)
+
+
+def test_binding_refuses_host_tensors():
+    v = torch.zeros(1, 2, 64)
+    with pytest.raises(TypeError):
+        layer.pack(v)
+    with pytest.raises(TypeError):
+        layer.Packed(torch.zeros(1, 2, 128, dtype=torch.int8), torch.zeros(1, 2, 1, dtype=torch.int8), 64)
