@@ -479,22 +479,26 @@ int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const re
                               const relaysum_rows *ds, const relaysum_rows *weight_grad,
                               void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Bytes that the three calls below may need as workspace, 16-byte aligned,
+ * for rows of this type (y's, or dy's); 0: none, and NULL will do.  Few
+ * results with a long sum are made in parts, which are kept there. */
+int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels, int32_t type);
+
 /* y[t][c] = sum_k x[t][k] * w[c][k] for every worker: x packed rows of tokens,
  * w packed rows of channels (the output features), both group 0.  The sum is
  * exact in integers; it is rounded to 24 bits and then to y's type. */
 int relaysum_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                     const relaysum_packed *x, const relaysum_packed *w, const relaysum_rows *y,
-                    void *hip_stream);
+                    void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* dx[t][k] = sum_c dy[t][c] * w[c][k]; dx has dy's type. */
+/* dx[t][k] = sum_c dy[t][c] * w[c][k]; dx has dy's type, w is group 0. */
 int relaysum_linear_backward_input(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                                    const relaysum_rows *dy, const relaysum_packed *w,
-                                   const relaysum_rows *dx, void *hip_stream);
+                                   const relaysum_rows *dx, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream);
 
 /* weight_grad[c][k] = sum_t dy[t][c] * x[t][k], float rows, overwritten; x of
- * either group (what relaysum_rmsnorm gave, or activations packed for this).
- *   workspace   relaysum_linear_workspace bytes, 16-byte aligned (NULL if 0) */
-int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels);
+ * either group (what relaysum_rmsnorm gave, or activations packed for this). */
 int relaysum_linear_backward_weight(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                                     const relaysum_rows *dy, const relaysum_packed *x,
                                     const relaysum_rows *weight_grad, void *workspace,

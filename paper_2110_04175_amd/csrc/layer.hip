@@ -416,98 +416,232 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(const float *partial, fl
 //
 // LDS tiles of both products: rows of 128 bytes (128 codes, or 64 bfloat16 of
 // the contracted axis) as 8 chunks of 16 bytes; chunk c of row r lies at
-// position c ^ swizzle(r).  16 lanes that read the same chunk of 16 neighbouring
-// rows then touch 16 different 16-byte bank groups, and so do the lanes that
-// write one chunk of rows 4 apart.
-__device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 7) ^ ((row >> 4) & 1); }
+// position c ^ swizzle(r).  The swizzle takes row bits 1..5 to 3 bits so that
+// bits {1,2,3}, {1,4,5}, {1,3,4} and {2,3,4} each reach all 8 positions (bit 0
+// moves a row by half of the 64 banks): lanes that read one chunk of 16
+// neighbouring rows, or of 4 times 4 rows 16 or 8 apart, touch different banks,
+// and so do lanes that write one chunk of rows 4 apart.
+__device__ __forceinline__ int swizzle(int row) {
+    return ((row >> 1) & 7) ^ (((row >> 4) & 1) * 3) ^ (((row >> 5) & 1) << 2);
+}
 __device__ __forceinline__ int tile_at(int row, int chunk) {
     return row * 128 + ((chunk ^ swizzle(row)) << 4);
 }
 
+// Which result a matrix instruction's row r of tile j is: tiles go by fours
+// (Q), and a lane's 4 rows of each of them are neighbours, so that a lane ends
+// up with 4 * Q entries in a row of the result.
+template <int Q>
+__device__ __forceinline__ int tile_row(int j, int r) {
+    return j / Q * 16 * Q + r / 4 * 4 * Q + j % Q * 4 + r % 4;
+}
+
+// A lane's place in a tile for reading 16 of its rows (tile_row<Q> of tile 0,
+// chunk lane / 16), and from there the place for tile j and chunk 4 * ks +
+// lane / 16: the swizzle is linear in the row's bits, so the two differ by a
+// constant number of rows and a constant change of the chunk's bits.  `fresh`
+// keeps the compiler from holding all of these sums in registers for the
+// whole loop, which it has not got.
+template <int Q>
+__device__ __forceinline__ int read_at(int row0, int lane) {
+    return tile_at(row0 + tile_row<Q>(0, lane % 16), lane / 16);
+}
+template <int Q>
+__device__ __forceinline__ int moved(int at, int j, int ks) {
+    const int row = tile_row<Q>(j, 0);
+    return (at ^ ((ks * 4 ^ swizzle(row)) << 4)) + row * 128;
+}
+__device__ __forceinline__ int fresh(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// 16 bytes for each lane from memory into LDS at `to` + 16 * lane, without
+// registers in between; `to` is the same for the whole wave.
+__device__ __forceinline__ void copy_to_lds(const void *from, char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+__device__ __forceinline__ void wait_for_copies() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+
 // Blocks go round the 8 XCDs; each takes a run of neighbouring tiles, which
 // share rows in its L2.
-__device__ __forceinline__ int64_t xcd_tile(int64_t block, int64_t blocks) {
-    const int64_t run = blocks / 8, rest = blocks % 8, x = block % 8;
+__device__ __forceinline__ unsigned xcd_tile(unsigned block, unsigned blocks) {
+    const unsigned run = blocks / 8, rest = blocks % 8, x = block % 8;
     return x * run + (x < rest ? x : rest) + block / 8;
 }
+
+// 4 * Q entries of a row of `cols`, from column c0 on.
+template <int Q, typename O, typename V>
+__device__ __forceinline__ void write_entries(O *row, int c0, int cols, const V *v) {
+    O out[4 * Q];
+#pragma unroll
+    for (int k = 0; k < 4 * Q; ++k) out[k] = (O)v[k / 4][k % 4];
+    if (c0 + 4 * Q <= cols) {
+        __builtin_memcpy(row + c0, out, sizeof out);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4 * Q; ++k)
+            if (c0 + k < cols) row[c0 + k] = out[k];
+    }
+}
+
+// Kinds of instructions for the scheduler's groups.
+constexpr int kMfma = 0x8, kDsRead = 0x100;
 
 struct LinearArgs {
     Packed x, w;
     Rows y;
+    int32_t *partial;   // split > 1: [split][n][tokens][channels]
     int64_t tokens;
-    int32_t width, stride, channels;
-    int64_t tiles_m;
-    int32_t tiles_n;
+    int32_t stride, channels, split;
+    int32_t tiles_m, tiles_n;
+    int32_t workers;
 };
 
 // Y[t][c] = 2^(ex[t] + ew[c]) * sum_k qx[t][k] qw[c][k]: whole numbers until
 // the one conversion (rounded to 24 bits from 2^24 on, then to the type).
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearArgs a) {
-    constexpr int kThreads = 64 * WM * WN;
-    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    __shared__ __align__(16) char lds[(BM + BN) * 128];
-    const int64_t tile = xcd_tile(blockIdx.x, gridDim.x);
-    const int64_t per = a.tiles_m * a.tiles_n;
-    const int64_t worker = tile / per, in = tile - worker * per;
-    const int64_t m0 = (in / a.tiles_n) * BM;
-    const int n0 = (int)(in % a.tiles_n) * BN;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-    const int8_t *xq = a.x.codes + worker * a.tokens * a.stride;
-    const int8_t *wq = a.w.codes + worker * (int64_t)a.channels * a.stride;
-    i4_t acc[TM][TN] = {};
-    for (int k0 = 0; k0 < a.stride; k0 += 128) {
-        u4_t st[(BM + BN) * 8 / kThreads];
+template <int BM, int BN, int WM, int WN>
+struct LinearTile {
+    static constexpr int kThreads = 64 * WM * WN, kBytes = (BM + BN) * 128;
+    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, Q = TN < 4 ? TN : 4;
+    static constexpr int kCopies = ((BM + BN) * 8 + kThreads - 1) / kThreads;
+    static_assert(BM % 8 == 0 && BN % 8 == 0, "a wave's copy, 8 rows, is of one operand");
+
+    // Starts the copies of 128 codes of every row of the tile.
+    static __device__ __forceinline__ void fetch(const int8_t *x, const int8_t *w,
+                                                 const unsigned (&at)[kCopies], char *lds) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
-        for (int i = 0; i < (BM + BN) * 8 / kThreads; ++i) {
-            const int u = i * kThreads + threadIdx.x, r = u / 8, ch = u % 8;
-            // Rows past the end repeat the last one; what they give is not stored.
-            const int8_t *p = r < BM ? xq + min(m0 + r, a.tokens - 1) * a.stride
-                                     : wq + (int64_t)min(n0 + r - BM, a.channels - 1) * a.stride;
-            st[i] = *reinterpret_cast<const u4_t *>(p + k0 + ch * 16);
+        for (int i = 0; i < kCopies; ++i) {
+            const int u = i * kThreads + wave * kWave;
+            if ((BM + BN) * 8 % kThreads && u >= (BM + BN) * 8) break;
+            copy_to_lds((u / 8 < BM ? x : w) + at[i], lds + u * 16);
         }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < (BM + BN) * 8 / kThreads; ++i) {
-            const int u = i * kThreads + threadIdx.x;
-            *reinterpret_cast<u4_t *>(lds + tile_at(u / 8, u % 8)) = st[i];
-        }
-        __syncthreads();
+    }
+
+    // xat, wat: read_at of the wave's first token and channel.
+    static __device__ __forceinline__ void multiply(const char *lds, int xat, int wat, i4_t (&acc)[TM][TN]) {
+        xat = fresh(xat);
+        wat = fresh(wat);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             i4_t xf[TM], wf[TN];
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-                xf[i] = *reinterpret_cast<const i4_t *>(
-                    lds + tile_at(wm + i * 16 + lane % 16, ks * 4 + lane / 16));
+            for (int j = 0; j < TN; ++j) wf[j] = *reinterpret_cast<const i4_t *>(lds + moved<Q>(wat, j, ks));
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-                wf[j] = *reinterpret_cast<const i4_t *>(
-                    lds + tile_at(BM + wn + j * 16 + lane % 16, ks * 4 + lane / 16));
+            for (int i = 0; i < TM; ++i) xf[i] = *reinterpret_cast<const i4_t *>(lds + moved<1>(xat, i, ks));
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[j], xf[i], acc[i][j], 0, 0, 0);
         }
+        // All of the first half's reads, then one more for every two products.
+        __builtin_amdgcn_sched_group_barrier(kDsRead, TN + TM, 0);
+#pragma unroll
+        for (int q = 0; q < TM * TN / 2; ++q) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        }
     }
-    // A lane has four neighbouring channels of one token in each accumulator.
+};
+
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void linear_kernel(LinearArgs a) {
+    using L = LinearTile<BM, BN, WM, WN>;
+    constexpr int TM = L::TM, TN = L::TN, Q = L::Q;
+    __shared__ __align__(16) char lds[2 * L::kBytes];
+    const unsigned tile = xcd_tile(blockIdx.x, gridDim.x);
+    const unsigned per = (unsigned)a.tiles_m * a.tiles_n;
+    const unsigned job = tile / per, in = tile % per;
+    const int64_t worker = job / a.split;
+    const int part = (int)(job % a.split);
+    const int64_t m0 = (int64_t)(in / a.tiles_n) * BM;
+    const int n0 = (int)(in % a.tiles_n) * BN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+    // Rows past the end repeat the last one; what they give is not stored.
+    const int8_t *x = a.x.codes + (worker * a.tokens + m0) * a.stride;
+    const int8_t *w = a.w.codes + (worker * a.channels + n0) * (int64_t)a.stride;
+    const int last_m = (int)min(a.tokens - m0, (int64_t)BM) - 1, last_n = min(a.channels - n0, BN) - 1;
+    unsigned at[L::kCopies];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t t = m0 + wm + i * 16 + lane % 16;
-        if (t >= a.tokens) continue;
-        const int ex = a.x.exps[worker * a.tokens + t];
-        T *y = row_at<T>(a.y, worker, t);
+    for (int i = 0; i < L::kCopies; ++i) {
+        const int u = i * L::kThreads + threadIdx.x, r = u / 8 < BM ? u / 8 : u / 8 - BM;
+        at[i] = (unsigned)min(r, u / 8 < BM ? last_m : last_n) * a.stride + (((u % 8) ^ swizzle(r)) << 4);
+    }
+    const int xat = read_at<1>(wm, lane), wat = BM * 128 + read_at<Q>(wn, lane);
+    // This part's share of the width, in whole steps of 128 codes.
+    const int steps = a.stride / 128;
+    const int k1 = (int)((int64_t)steps * (part + 1) / a.split) * 128;
+    int k0 = (int)((int64_t)steps * part / a.split) * 128, cur = 0;
+    i4_t acc[TM][TN] = {};
+    L::fetch(x + k0, w + k0, at, lds);
+    for (k0 += 128; k0 <= k1; k0 += 128) {
+        wait_for_copies();
+        __syncthreads();
+        if (k0 < k1) L::fetch(x + k0, w + k0, at, lds + (cur ^ L::kBytes));
+        L::multiply(lds + cur, xat, wat, acc);
+        cur ^= L::kBytes;
+    }
+    if (a.split > 1) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int c0 = n0 + wn + j * 16 + lane / 16 * 4;
+        for (int i = 0; i < TM; ++i) {
+            const int64_t t = m0 + wm + i * 16 + lane % 16;
+            if (t >= a.tokens) continue;
+            int32_t *row = a.partial + (((int64_t)part * a.workers + worker) * a.tokens + t) * a.channels;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (c0 + k >= a.channels) continue;
-                const int ew = a.w.exps[worker * a.channels + c0 + k];
-                const float v = ldexpf((float)acc[i][j][k], ex + ew);
-                y[c0 + k] = (T)(ex == kNotANumber || ew == kNotANumber ? float_of(0x7fc00000u) : v);
+            for (int j0 = 0; j0 < TN; j0 += Q)
+                write_entries<Q>(row, n0 + wn + tile_row<Q>(j0, lane / 16 * 4), a.channels, &acc[i][j0]);
+        }
+        return;
+    }
+    // A lane has 4 * Q neighbouring channels of one token in Q accumulators.
+    const int64_t t0 = m0 + wm + lane % 16;
+    int ex[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ex[i] = a.x.exps[worker * a.tokens + min(t0 + i * 16, a.tokens - 1)];
+#pragma unroll
+    for (int j0 = 0; j0 < TN; j0 += Q) {
+        const int c0 = n0 + wn + tile_row<Q>(j0, lane / 16 * 4);
+        int ew[4 * Q];
+#pragma unroll
+        for (int k = 0; k < 4 * Q; ++k) ew[k] = a.w.exps[worker * a.channels + min(c0 + k, a.channels - 1)];
+        // A whole number of at most 2^29 times 2^ex is a normal number, or 0,
+        // up to ex = 98; the second factor then makes the one rounding that
+        // can be left.
+        int most = ex[0];
+#pragma unroll
+        for (int i = 1; i < TM; ++i) most = max(most, ex[i]);
+        const bool wide = __any(most > 98);
+        float sw[4 * Q];
+#pragma unroll
+        for (int k = 0; k < 4 * Q; ++k) sw[k] = scale_of(ew[k]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            T v[4 * Q];
+            if (wide) {
+#pragma unroll
+                for (int k = 0; k < 4 * Q; ++k) {
+                    const float f = ldexpf((float)acc[i][j0 + k / 4][k % 4], ex[i] + ew[k]);
+                    v[k] = (T)(ex[i] == kNotANumber || ew[k] == kNotANumber ? float_of(0x7fc00000u) : f);
+                }
+            } else {
+                const float sx = scale_of(ex[i]);
+#pragma unroll
+                for (int k = 0; k < 4 * Q; ++k) v[k] = (T)((float)acc[i][j0 + k / 4][k % 4] * sx * sw[k]);
+            }
+            const int64_t t = t0 + i * 16;
+            if (t >= a.tokens) continue;
+            T *y = row_at<T>(a.y, worker, t);
+            if (c0 + 4 * Q <= a.channels) {
+                __builtin_memcpy(y + c0, v, sizeof v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4 * Q; ++k)
+                    if (c0 + k < a.channels) y[c0 + k] = v[k];
             }
         }
     }
@@ -520,8 +654,7 @@ struct GradArgs {
     float *partial;    // split > 1: [split][n][m][cols]
     int64_t m, r;      // rows of the result, the contracted axis
     int32_t cols, stride, split;
-    int64_t tiles_m;
-    int32_t tiles_n;
+    int32_t tiles_m, tiles_n;
     int32_t workers;
 };
 
@@ -543,144 +676,275 @@ template <> struct Parts<float> { static constexpr int n = 3; };
 
 // out[m][k] = sum_r A(m, r) * q[r][k] 2^e[r][k / group], with A(m, r) = dY[m][r]
 // (dX: m tokens, r channels) or dY[r][m] (ALONG_R, dW: m channels, r tokens).
-// Both operands are brought into LDS as bfloat16 rows along r: 8 x 4 blocks of
-// codes, and of dY for dW, are turned in registers on the way.
-template <typename T, typename O, bool ALONG_R, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void grad_kernel(GradArgs a) {
-    constexpr int kThreads = 64 * WM * WN, P = Parts<T>::n, BR = 64;
-    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    __shared__ __align__(16) char lds[(P * BM + BN) * 128];
-    char *ldb = lds + P * BM * 128;
-    const int64_t per = a.tiles_m * a.tiles_n;
-    const int64_t tile = xcd_tile(blockIdx.x, gridDim.x);
-    const int64_t job = tile / per, in = tile - job * per;
-    const int64_t worker = job / a.split;
-    const int part = (int)(job - worker * a.split);
-    const int64_t m0 = (in / a.tiles_n) * BM;
-    const int n0 = (int)(in % a.tiles_n) * BN;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-    // This part's share of the contracted axis, in whole tiles.
-    const int64_t steps = (a.r + BR - 1) / BR;
-    const int64_t s0 = steps * part / a.split, s1 = steps * (part + 1) / a.split;
-    f4_t acc[TM][TN] = {};
-    for (int64_t s = s0; s < s1; ++s) {
-        const int64_t r0 = s * BR;
-        __syncthreads();
-        if (ALONG_R) {
+// Both operands are brought into LDS as bfloat16 rows along r, 64 of r a step:
+// 8 x 4 blocks of codes, and of dY for dW, are turned in registers on the way.
+template <typename T, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
+struct GradTile {
+    static constexpr int kThreads = 64 * WM * WN, P = Parts<T>::n, BR = 64;
+    static constexpr int kA = P * BM * 128, kBytes = kA + BN * 128;
+    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, Q = TN < 4 ? TN : 4;
+    // Units of one thread: 8 r of one m (dX), or 8 r of 4 m (dW); 8 r of 4 columns.
+    static constexpr int kUnitsA = BM * BR / (ALONG_R ? 32 : 8), kUnitsB = BN * BR / 32;
+    static constexpr int UA = (kUnitsA + kThreads - 1) / kThreads, UB = (kUnitsB + kThreads - 1) / kThreads;
+    typedef T t4_t __attribute__((ext_vector_type(4)));
+
+    // What a thread holds of a step on its way to LDS: dY and codes as they
+    // are, and the exponents of its 8 rows of codes.
+    struct Held {
+        v8_t<T> a[ALONG_R ? 1 : UA];
+        t4_t at[ALONG_R ? UA : 1][8];
+        unsigned q[UB][8];
+        u2_t e[GROUPED ? 1 : UB];
+        int8_t eg[GROUPED ? UB : 1][8];
+    };
+
+    // Thread's unit i of a tile `span` wide in units of 4: its place along r.
+    // The same for a whole wave where 64 units fit the width, which leaves
+    // addresses to the scalar unit.
+    static __device__ __forceinline__ int unit_r(int i, int span) {
+        const int r = (i * kThreads + threadIdx.x) / (span / 4) * 8;
+        return span / 4 % kWave == 0 ? __builtin_amdgcn_readfirstlane(r) : r;
+    }
+
+    // Loads the step at r0.  FULL: all of it is inside; else entries past the
+    // contracted axis' end count as zeros, and only entries inside are touched.
+    // Rows (dX) or columns (both) past the result's end repeat others: what
+    // they give is not stored.
+    template <bool FULL>
+    static __device__ __forceinline__ void load(const GradArgs &g, int64_t worker, int64_t m0, int n0,
+                                                int64_t r0, Held &h) {
 #pragma unroll
-            for (int i = 0; i < BM * BR / 32 / kThreads; ++i) {
-                const int u = i * kThreads + threadIdx.x;
-                const int mm = u % (BM / 4) * 4, rr = u / (BM / 4) * 8;
-                __bf16 p[4][8][P];
+        for (int i = 0; i < UA; ++i) {
+            const int u = i * kThreads + threadIdx.x;
+            if (kUnitsA % kThreads && u >= kUnitsA) break;
+            if (ALONG_R) {
+                const int rr = unit_r(i, BM);
+                const T *p = row_at<const T>(g.a, worker, r0 + rr);
+                int64_t m = m0 + u % (BM / 4) * 4;
+                if (FULL) m = min(m, g.m - 4);
 #pragma unroll
                 for (int y = 0; y < 8; ++y) {
-                    const int64_t r = r0 + rr + y;
-                    const T *src = row_at<const T>(a.a, worker, r) + m0 + mm;
+                    if (FULL) {
+                        __builtin_memcpy(&h.at[i][y], p + y * g.a.rs + m, sizeof h.at[i][y]);
+                    } else {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        split<P>(r < a.r && m0 + mm + x < a.m ? (float)src[x] : 0.0f, p[x][y]);
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int k = 0; k < P; ++k) {
-                        b8_t v;
-#pragma unroll
-                        for (int y = 0; y < 8; ++y) v[y] = p[x][y][k];
-                        *reinterpret_cast<b8_t *>(lds + tile_at(k * BM + mm + x, rr / 8)) = v;
+                        for (int x = 0; x < 4; ++x)
+                            h.at[i][y][x] = r0 + rr + y < g.r && m + x < g.m ? p[y * g.a.rs + m + x] : (T)0.0f;
                     }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < BM * 8 / kThreads; ++i) {
-                const int u = i * kThreads + threadIdx.x, mm = u / 8, ch = u % 8;
-                const int64_t m = min(m0 + mm, a.m - 1), r = r0 + ch * 8;
-                float v[8];
-                load8(row_at<const T>(a.a, worker, m) + r, a.r - r, v);
-                b8_t q[P];
-#pragma unroll
-                for (int y = 0; y < 8; ++y) {
-                    __bf16 p[P];
-                    split<P>(v[y], p);
-#pragma unroll
-                    for (int k = 0; k < P; ++k) q[k][y] = p[k];
                 }
+            } else {
+                const T *p = row_at<const T>(g.a, worker, min(m0 + u / 8, g.m - 1)) + r0 + u % 8 * 8;
+                if (FULL) {
+                    __builtin_memcpy(&h.a[i], p, sizeof h.a[i]);
+                } else {
 #pragma unroll
-                for (int k = 0; k < P; ++k)
-                    *reinterpret_cast<b8_t *>(lds + tile_at(k * BM + mm, ch)) = q[k];
+                    for (int y = 0; y < 8; ++y) h.a[i][y] = r0 + u % 8 * 8 + y < g.r ? p[y] : (T)0.0f;
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < BN * BR / 32 / kThreads; ++i) {
+        for (int i = 0; i < UB; ++i) {
             const int u = i * kThreads + threadIdx.x;
-            const int nn = u % (BN / 4) * 4, rr = u / (BN / 4) * 8;
-            const int col = min(n0 + nn, a.stride - 4);
-            unsigned q[8];
-            float sc[8];
+            if (kUnitsB % kThreads && u >= kUnitsB) break;
+            const int rr = unit_r(i, BN), col = min(n0 + u % (BN / 4) * 4, g.stride - 4);
+            const int64_t row = worker * g.r + r0 + rr;
+            const int8_t *q = g.b.codes + row * g.stride;
+            const int8_t *e = g.b.exps + row * g.b.groups + (GROUPED ? col / kGroup : 0);
+            const int left = (int)min(g.r - r0 - rr, (int64_t)8);
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                const int64_t r = r0 + rr + y, rc = worker * a.r + min(r, a.r - 1);
-                q[y] = *reinterpret_cast<const unsigned *>(a.b.codes + rc * a.stride + col);
-                const float e = scale_of(a.b.exps[rc * a.b.groups + (a.b.groups > 1 ? col / kGroup : 0)]);
-                sc[y] = r < a.r ? e : 0.0f;
+            for (int y = 0; y < 8; ++y)
+                h.q[i][y] = FULL || y < left ? *reinterpret_cast<const unsigned *>(q + y * (int64_t)g.stride + col) : 0u;
+            if (GROUPED) {
+#pragma unroll
+                for (int y = 0; y < 8; ++y) h.eg[i][y] = FULL || y < left ? e[y * (int64_t)g.b.groups] : (int8_t)0;
+            } else if (FULL) {
+                __builtin_memcpy(&h.e[i], e, sizeof h.e[i]);
+            } else {
+                h.e[i] = u2_t{0, 0};
+#pragma unroll
+                for (int y = 0; y < 8; ++y)
+                    if (y < left) h.e[i][y / 4] |= (unsigned)(uint8_t)e[y] << (8 * (y % 4));
             }
+        }
+    }
+
+    static __device__ __forceinline__ void store(const Held &h, char *lds) {
+#pragma unroll
+        for (int i = 0; i < UB; ++i) {
+            const int u = i * kThreads + threadIdx.x;
+            if (kUnitsB % kThreads && u >= kUnitsB) break;
+            const int nn = u % (BN / 4) * 4, rr = u / (BN / 4) * 8;
+            float scale[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+                scale[y] = scale_of(GROUPED ? h.eg[i][y] : (int)(int8_t)(h.e[i][y / 4] >> (8 * (y % 4))));
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 b8_t v;
 #pragma unroll
-                for (int y = 0; y < 8; ++y) v[y] = (__bf16)(code_at(q[y], x) * sc[y]);
-                *reinterpret_cast<b8_t *>(ldb + tile_at(nn + x, rr / 8)) = v;
+                for (int y = 0; y < 8; ++y) v[y] = (__bf16)(code_at(h.q[i][y], x) * scale[y]);
+                *reinterpret_cast<b8_t *>(lds + kA + tile_at(nn + x, rr / 8)) = v;
             }
         }
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < UA; ++i) {
+            const int u = i * kThreads + threadIdx.x;
+            if (kUnitsA % kThreads && u >= kUnitsA) break;
+            const int mm = ALONG_R ? u % (BM / 4) * 4 : u / 8, ch = ALONG_R ? u / (BM / 4) : u % 8;
+#pragma unroll
+            for (int x = 0; x < (ALONG_R ? 4 : 1); ++x) {
+                b8_t v[P];
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                    __bf16 p[P];
+                    split<P>((float)(ALONG_R ? h.at[i][y][x] : h.a[i][y]), p);
+#pragma unroll
+                    for (int k = 0; k < P; ++k) v[k][y] = p[k];
+                }
+#pragma unroll
+                for (int k = 0; k < P; ++k)
+                    *reinterpret_cast<b8_t *>(lds + tile_at(k * BM + mm + x, ch)) = v[k];
+            }
+        }
+    }
+
+    static __device__ __forceinline__ void multiply(const char *lds, int aat, int bat, f4_t (&acc)[TM][TN]) {
+        aat = fresh(aat);
+        bat = fresh(bat);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             b8_t bf[TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-                bf[j] = *reinterpret_cast<const b8_t *>(
-                    ldb + tile_at(wn + j * 16 + lane % 16, ks * 4 + lane / 16));
+            for (int j = 0; j < TN; ++j) bf[j] = *reinterpret_cast<const b8_t *>(lds + moved<Q>(bat, j, ks));
 #pragma unroll
-            for (int k = P - 1; k >= 0; --k)   // the smallest part first
+            for (int k = P - 1; k >= 0; --k) {   // the smallest part first
+                b8_t af[TM];
 #pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    const b8_t af = *reinterpret_cast<const b8_t *>(
-                        lds + tile_at(k * BM + wm + i * 16 + lane % 16, ks * 4 + lane / 16));
+                for (int i = 0; i < TM; ++i)
+                    af[i] = *reinterpret_cast<const b8_t *>(lds + k * BM * 128 + moved<1>(aat, i, ks));
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j], af, acc[i][j], 0, 0, 0);
-                }
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
+            }
         }
     }
+};
+
+template <typename T, typename O, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
+    using G = GradTile<T, ALONG_R, GROUPED, BM, BN, WM, WN>;
+    constexpr int TM = G::TM, TN = G::TN, Q = G::Q;
+    __shared__ __align__(16) char lds[2 * G::kBytes];
+    const unsigned per = (unsigned)a.tiles_m * a.tiles_n;
+    const unsigned tile = xcd_tile(blockIdx.x, gridDim.x);
+    const unsigned job = tile / per, in = tile % per;
+    const int64_t worker = job / a.split;
+    const int part = (int)(job % a.split);
+    const int64_t m0 = (int64_t)(in / a.tiles_n) * BM;
+    const int n0 = (int)(in % a.tiles_n) * BN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+    const int aat = read_at<1>(wm, lane), bat = G::kA + read_at<Q>(wn, lane);
+    // This part's share of the contracted axis, in whole steps.
+    const int64_t steps = (a.r + G::BR - 1) / G::BR;
+    const int64_t s0 = steps * part / a.split, s1 = steps * (part + 1) / a.split;
+    f4_t acc[TM][TN] = {};
+    if (s0 < s1) {
+        typename G::Held h;
+        // Steps that are loaded in whole chunks: not the one that the axis ends
+        // in, and none where the result's edge cuts a chunk of dY.
+        const int64_t whole = ALONG_R && a.m % 4 && m0 + BM > a.m ? 0 : a.r / G::BR;
+        int cur = 0;
+        if (s0 < whole)
+            G::template load<true>(a, worker, m0, n0, s0 * G::BR, h);
+        else
+            G::template load<false>(a, worker, m0, n0, s0 * G::BR, h);
+        G::store(h, lds);
+        __syncthreads();
+        int64_t s = s0 + 1;
+        for (; s < min(s1, whole); ++s) {
+            G::template load<true>(a, worker, m0, n0, s * G::BR, h);
+            G::multiply(lds + cur, aat, bat, acc);
+            cur ^= G::kBytes;
+            G::store(h, lds + cur);
+            __syncthreads();
+        }
+        for (; s < s1; ++s) {
+            G::template load<false>(a, worker, m0, n0, s * G::BR, h);
+            G::multiply(lds + cur, aat, bat, acc);
+            cur ^= G::kBytes;
+            G::store(h, lds + cur);
+            __syncthreads();
+        }
+        G::multiply(lds + cur, aat, bat, acc);
+    }
+    // A lane has 4 * Q neighbouring columns of one row in Q accumulators.
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t m = m0 + wm + i * 16 + lane % 16;
         if (m >= a.m) continue;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int c0 = n0 + wn + j * 16 + lane / 16 * 4;
+        for (int j0 = 0; j0 < TN; j0 += Q) {
+            const int c0 = n0 + wn + tile_row<Q>(j0, lane / 16 * 4);
+            if (a.split > 1)
+                write_entries<Q>(a.partial + (((int64_t)part * a.workers + worker) * a.m + m) * a.cols, c0, a.cols,
+                                 &acc[i][j0]);
+            else
+                write_entries<Q>(row_at<O>(a.out, worker, m), c0, a.cols, &acc[i][j0]);
+        }
+    }
+}
+
+// The sum of the parts of a split product, in ascending order: four
+// neighbouring entries of [n][rows][cols] for each thread, given to
+// f(worker, row, column, sum) one by one.
+template <typename V, typename F>
+__device__ __forceinline__ void join_parts(const V *partial, int split, int64_t workers, int64_t rows, int cols, F f) {
+    const int64_t all = workers * rows * cols;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (int64_t)gridDim.x * 1024) {
+        V v[4] = {0, 0, 0, 0};
+        if (i + 4 <= all) {
+            for (int s = 0; s < split; ++s) {
+                V p[4];
+                __builtin_memcpy(p, partial + s * all + i, sizeof p);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (c0 + k >= a.cols) continue;
-                if (a.split > 1)
-                    a.partial[(((int64_t)part * a.workers + worker) * a.m + m) * a.cols + c0 + k] = acc[i][j][k];
-                else
-                    row_at<O>(a.out, worker, m)[c0 + k] = (O)acc[i][j][k];
+                for (int k = 0; k < 4; ++k) v[k] += p[k];
+            }
+        } else {
+            for (int s = 0; s < split; ++s)
+                for (int k = 0; i + k < all; ++k) v[k] += partial[s * all + i + k];
+        }
+        int64_t row = i / cols;
+        int col = (int)(i - row * cols);
+        int64_t worker = row / rows;
+        row -= worker * rows;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i + k >= all) break;
+            f(worker, row, col, v[k]);
+            if (++col == cols) {
+                col = 0;
+                if (++row == rows) row = 0, ++worker;
             }
         }
     }
 }
 
-// The sum of the parts of a split product, in ascending order.
-__global__ __launch_bounds__(256) void join_kernel(GradArgs a) {
-    const int64_t per = a.m * a.cols, all = per * a.workers;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        float v = 0.0f;
-        for (int s = 0; s < a.split; ++s) v += a.partial[s * all + i];
-        const int64_t worker = i / per, at = i - worker * per, m = at / a.cols;
-        row_at<float>(a.out, worker, m)[at - m * a.cols] = v;
-    }
+template <typename T>
+__global__ __launch_bounds__(256) void join_linear_kernel(LinearArgs a) {
+    join_parts(a.partial, a.split, a.workers, a.tokens, a.channels, [&](int64_t worker, int64_t t, int c, int v) {
+        const int ex = a.x.exps[worker * a.tokens + t], ew = a.w.exps[worker * a.channels + c];
+        const float f = ldexpf((float)v, ex + ew);
+        row_at<T>(a.y, worker, t)[c] = (T)(ex == kNotANumber || ew == kNotANumber ? float_of(0x7fc00000u) : f);
+    });
+}
+
+template <typename O>
+__global__ __launch_bounds__(256) void join_grad_kernel(GradArgs a) {
+    join_parts(a.partial, a.split, a.workers, a.m, a.cols,
+               [&](int64_t worker, int64_t m, int c, float v) { row_at<O>(a.out, worker, m)[c] = (O)v; });
 }
 
 // ---- host side -------------------------------------------------------------------------
@@ -707,6 +971,8 @@ int done(const char *what) {
     g_error[0] = '\0';
     return RELAYSUM_OK;
 }
+
+constexpr int64_t kMaxBlocks = 0x3fffff;   // workgroups of a launch: fewer than 2^32 threads
 
 int64_t code_stride(int64_t width) { return (width + kGroup - 1) / kGroup * kGroup; }
 
@@ -753,6 +1019,16 @@ struct Call {
         else if ((__int128)n * (tokens + width) * channels > ((__int128)1 << 50))
             fail(refuse("n * (tokens + width) * channels is more than 2^50"));
         return code == RELAYSUM_OK;
+    }
+
+    // A product's workgroups and workspace.
+    template <typename P>
+    void product_launch(const P &plan, const void *workspace, size_t bytes) {
+        if (code != RELAYSUM_OK) return;
+        if (plan.blocks > kMaxBlocks) return fail(refuse("the result has more than %d tiles", (int)kMaxBlocks));
+        if (plan.workspace > bytes)
+            return fail(refuse("the workspace has %zu bytes, %zu are needed", bytes, plan.workspace));
+        span("workspace", workspace, plan.workspace, 16, true);
     }
 
     void span(const char *name, const void *p, size_t bytes, size_t align, bool out,
@@ -884,7 +1160,6 @@ void with_type(int32_t type, F f) {
     else f((_Float16)0);
 }
 
-constexpr int64_t kMaxBlocks = 0x3fffff;   // a launch has fewer than 2^32 threads
 constexpr int64_t kMaxGrid = 1 << 20;   // workgroups; kernels over rows loop beyond
 
 unsigned row_grid(int64_t rows, int per) {
@@ -900,16 +1175,74 @@ int norm_parts(int32_t n, int64_t rows) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(want, (rows + 15) / 16));
 }
 
-constexpr int kTile = 128;
-
 int64_t tiles(int64_t size, int64_t tile) { return (size + tile - 1) / tile; }
 
-// Parts of the contracted axis of dW: where the result has fewer tiles than
-// there are CUs, so many that every CU has one, each at least 8 steps of 64 tokens.
-int weight_split(int32_t n, int64_t tokens, int64_t width, int64_t channels) {
-    const int64_t have = n * tiles(width, kTile) * tiles(channels, kTile);
-    const int64_t want = (kCus + have - 1) / have;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(want, tokens / 512));
+// How a product is cut up: the tile of a workgroup, and the parts that the
+// contracted axis is split into where there would be too few workgroups.
+struct TileCost {
+    int bm, bn;
+    float step_us, fixed_us;   // one step of the contracted axis; what a workgroup takes besides
+    int resident;              // workgroups of a CU at a time
+};
+
+struct Plan {
+    int tile = 0, split = 1;
+    int64_t tiles_m = 0, tiles_n = 0, blocks = 0;
+    size_t workspace = 0;
+};
+
+// The cheapest of the tiles and splits by the time that the last CU ends, with
+// what joining the parts costs: a launch, and every part written and read.
+Plan plan_product(const TileCost *tile, int count, int64_t n, int64_t m, int64_t cols, int64_t steps) {
+    static const int splits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    Plan best;
+    float best_us = 0.0f;
+    for (int c = 0; c < count; ++c) {
+        const int64_t tm = tiles(m, tile[c].bm), tn = tiles(cols, tile[c].bn);
+        for (const int split : splits) {
+            if (split > steps && split > 1) break;
+            const int64_t blocks = n * tm * tn * split;
+            const float rounds = (float)tiles(blocks, kCus * tile[c].resident);
+            float us = rounds * (tile[c].fixed_us + (float)tiles(steps, split) * tile[c].step_us);
+            if (split > 1) us += 4.0f + (float)(split + 1) * (float)n * (float)m * (float)cols * 4.0f / 3.5e6f;
+            if (best.blocks && us >= best_us) continue;
+            best_us = us;
+            best = Plan{c, split, tm, tn, blocks, split > 1 ? (size_t)split * n * m * cols * 4 : 0};
+        }
+    }
+    return best;
+}
+
+Plan plan_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels) {
+    static const TileCost tile[] = {{256, 256, 2.0f, 6.0f, 1}, {64, 128, 1.0f, 3.0f, 3}, {16, 128, 0.8f, 3.0f, 4}};
+    return plan_product(tile, 3, n, tokens, channels, tiles(width, 128));
+}
+
+// The gradients' tiles: the first as large as two of its steps fit in LDS.
+Plan plan_grad(int32_t type, int64_t n, int64_t m, int64_t cols, int64_t r) {
+    static const TileCost tile[3][2] = {{{128, 128, 1.6f, 4.0f, 1}, {64, 128, 2.0f, 3.0f, 2}},
+                                        {{256, 256, 2.4f, 5.0f, 1}, {64, 128, 1.2f, 3.0f, 3}},
+                                        {{128, 256, 2.2f, 4.0f, 1}, {64, 128, 1.5f, 3.0f, 2}}};
+    return plan_product(tile[type], 2, n, m, cols, tiles(r, 64));
+}
+
+// Calls f with the large or the small tile of a type: BM, BN, WM, WN.
+template <typename T, typename F>
+void with_grad_tile(int tile, F f) {
+    constexpr int P = Parts<T>::n;
+    if (tile == 0) f(Int<P == 1 ? 256 : 128>(), Int<P == 3 ? 128 : 256>(), Int<2>(), Int<4>());
+    else f(Int<64>(), Int<128>(), Int<2>(), Int<2>());
+}
+
+template <typename F>
+void with_linear_tile(int tile, F f) {
+    if (tile == 0) f(Int<256>(), Int<256>(), Int<2>(), Int<4>());
+    else if (tile == 1) f(Int<64>(), Int<128>(), Int<2>(), Int<2>());
+    else f(Int<16>(), Int<128>(), Int<1>(), Int<4>());
+}
+
+unsigned join_grid(int64_t entries) {
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((entries + 1023) / 1024, 8 * kCus));
 }
 
 }  // namespace
@@ -1083,63 +1416,87 @@ int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const re
     return done("relaysum_rmsnorm_backward");
 }
 
+int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels, int32_t type) {
+    Call c;
+    if (!c.product(n, tokens, width, channels)) return -1;
+    if (type < RELAYSUM_FLOAT || type > RELAYSUM_HALF) {
+        refuse("unknown type %d", type);
+        return -1;
+    }
+    return (int64_t)std::max({plan_linear(n, tokens, width, channels).workspace,
+                              plan_grad(type, n, tokens, width, channels).workspace,
+                              plan_grad(type, n, channels, width, tokens).workspace});
+}
+
 int relaysum_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                     const relaysum_packed *x, const relaysum_packed *w, const relaysum_rows *y,
-                    void *hip_stream) {
+                    void *workspace, size_t workspace_bytes, void *hip_stream) {
     Call c;
+    Plan p;
     if (c.product(n, tokens, width, channels)) {
         c.packed("x", x, n, tokens, width, false);
         c.packed("w", w, n, channels, width, false);
         if (c.code == RELAYSUM_OK && !(whole_rows(x, width) && whole_rows(w, width)))
             c.fail(refuse("the product takes rows packed whole (group 0)"));
         c.rows("y", y, n, tokens, channels, true);
+        p = plan_linear(n, tokens, width, channels);
+        c.product_launch(p, workspace, workspace_bytes);
     }
     if (!c.ready()) return c.code;
     if (tokens == 0) return done("relaysum_linear");
-    LinearArgs a{packed_of(x, width), packed_of(w, width), rows_of(y, n, tokens), tokens,
-                 (int32_t)width, (int32_t)code_stride(width), (int32_t)channels,
-                 tiles(tokens, kTile), (int32_t)tiles(channels, kTile)};
-    const int64_t grid = n * a.tiles_m * a.tiles_n;
-    if (grid > kMaxBlocks) return refuse("the result has more than %d tiles", (int)kMaxBlocks);
+    const LinearArgs a{packed_of(x, width), packed_of(w, width), rows_of(y, n, tokens),
+                       static_cast<int32_t *>(workspace), tokens, (int32_t)code_stride(width),
+                       (int32_t)channels, p.split, (int32_t)p.tiles_m, (int32_t)p.tiles_n, n};
+    const hipStream_t st = (hipStream_t)hip_stream;
     with_type(y->type, [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_kernel<T, kTile, kTile, 2, 2>), dim3((unsigned)grid), dim3(256),
-                           0, (hipStream_t)hip_stream, a);
+        with_linear_tile(p.tile, [&](auto bm, auto bn, auto wm, auto wn) {
+            constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
+            constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value;
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_kernel<T, BM, BN, WM, WN>), dim3((unsigned)p.blocks),
+                               dim3(64 * WM * WN), 0, st, a);
+        });
+        if (p.split > 1)
+            hipLaunchKernelGGL(join_linear_kernel<T>, dim3(join_grid(n * tokens * channels)), dim3(256), 0, st, a);
     });
     return done("relaysum_linear");
 }
 
 int relaysum_linear_backward_input(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                                    const relaysum_rows *dy, const relaysum_packed *w,
-                                   const relaysum_rows *dx, void *hip_stream) {
+                                   const relaysum_rows *dx, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream) {
     Call c;
+    Plan p;
     if (c.product(n, tokens, width, channels)) {
         c.rows("dy", dy, n, tokens, channels, false);
         c.packed("w", w, n, channels, width, false);
         c.rows("dx", dx, n, tokens, width, true);
         if (c.code == RELAYSUM_OK && dy->type != dx->type)
             c.fail(refuse("dy and dx must have one type"));
+        if (c.code == RELAYSUM_OK && !whole_rows(w, width))
+            c.fail(refuse("w must be packed by whole rows (group 0)"));
+        if (c.code == RELAYSUM_OK) p = plan_grad(dy->type, n, tokens, width, channels);
+        c.product_launch(p, workspace, workspace_bytes);
     }
     if (!c.ready()) return c.code;
     if (tokens == 0) return done("relaysum_linear_backward_input");
-    GradArgs a{rows_of(dy, n, tokens), packed_of(w, width), rows_of(dx, n, tokens), nullptr,
-               tokens, channels, (int32_t)width, (int32_t)code_stride(width), 1,
-               tiles(tokens, kTile), (int32_t)tiles(width, kTile), n};
-    const int64_t grid = n * a.tiles_m * a.tiles_n;
-    if (grid > kMaxBlocks) return refuse("the result has more than %d tiles", (int)kMaxBlocks);
+    const GradArgs a{rows_of(dy, n, tokens), packed_of(w, width), rows_of(dx, n, tokens),
+                     static_cast<float *>(workspace), tokens, channels, (int32_t)width,
+                     (int32_t)code_stride(width), p.split, (int32_t)p.tiles_m, (int32_t)p.tiles_n, n};
+    const hipStream_t st = (hipStream_t)hip_stream;
     with_type(dy->type, [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kernel<T, T, false, kTile, kTile, 2, 2>), dim3((unsigned)grid),
-                           dim3(256), 0, (hipStream_t)hip_stream, a);
+        with_grad_tile<T>(p.tile, [&](auto bm, auto bn, auto wm, auto wn) {
+            constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
+            constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value;
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kernel<T, T, false, false, BM, BN, WM, WN>),
+                               dim3((unsigned)p.blocks), dim3(64 * WM * WN), 0, st, a);
+        });
+        if (p.split > 1)
+            hipLaunchKernelGGL(join_grad_kernel<T>, dim3(join_grid(n * tokens * width)), dim3(256), 0, st, a);
     });
     return done("relaysum_linear_backward_input");
-}
-
-int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels) {
-    Call c;
-    if (!c.product(n, tokens, width, channels)) return -1;
-    const int split = weight_split(n, tokens, width, channels);
-    return split > 1 ? (int64_t)split * n * width * channels * 4 : 0;
 }
 
 int relaysum_linear_backward_weight(int32_t n, int64_t tokens, int64_t width, int64_t channels,
@@ -1147,36 +1504,36 @@ int relaysum_linear_backward_weight(int32_t n, int64_t tokens, int64_t width, in
                                     const relaysum_rows *weight_grad, void *workspace,
                                     size_t workspace_bytes, void *hip_stream) {
     Call c;
-    int split = 1;
+    Plan p;
     if (c.product(n, tokens, width, channels)) {
         c.rows("dy", dy, n, tokens, channels, false);
         c.packed("x", x, n, tokens, width, false);
         c.rows("weight_grad", weight_grad, n, channels, width, true);
         if (c.code == RELAYSUM_OK && weight_grad->type != RELAYSUM_FLOAT)
             c.fail(refuse("weight_grad must be of type float"));
-        split = weight_split(n, tokens, width, channels);
-        const size_t need = split > 1 ? (size_t)split * n * width * channels * 4 : 0;
-        if (need > workspace_bytes)
-            c.fail(refuse("the workspace has %zu bytes, %zu are needed", workspace_bytes, need));
-        c.span("workspace", workspace, need, 16, true);
+        if (c.code == RELAYSUM_OK) p = plan_grad(dy->type, n, channels, width, tokens);
+        c.product_launch(p, workspace, workspace_bytes);
     }
     if (!c.ready()) return c.code;
-    GradArgs a{rows_of(dy, n, tokens), packed_of(x, width), rows_of(weight_grad, n, channels),
-               static_cast<float *>(workspace), channels, tokens, (int32_t)width,
-               (int32_t)code_stride(width), split, tiles(channels, kTile), (int32_t)tiles(width, kTile), n};
-    const int64_t grid = n * split * a.tiles_m * a.tiles_n;
-    if (grid > kMaxBlocks) return refuse("the result has more than %d tiles", (int)kMaxBlocks);
+    const GradArgs a{rows_of(dy, n, tokens), packed_of(x, width), rows_of(weight_grad, n, channels),
+                     static_cast<float *>(workspace), channels, tokens, (int32_t)width,
+                     (int32_t)code_stride(width), p.split, (int32_t)p.tiles_m, (int32_t)p.tiles_n, n};
+    const bool grouped = !whole_rows(x, width);
     const hipStream_t st = (hipStream_t)hip_stream;
     with_type(dy->type, [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kernel<T, float, true, kTile, kTile, 2, 2>), dim3((unsigned)grid),
-                           dim3(256), 0, st, a);
+        with_grad_tile<T>(p.tile, [&](auto bm, auto bn, auto wm, auto wn) {
+            constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
+            constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value;
+            const dim3 grid((unsigned)p.blocks), block(64 * WM * WN);
+            if (grouped)
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kernel<T, float, true, true, BM, BN, WM, WN>), grid, block, 0, st, a);
+            else
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kernel<T, float, true, false, BM, BN, WM, WN>), grid, block, 0, st, a);
+        });
     });
-    if (split > 1) {
-        const int64_t all = (int64_t)n * channels * width;
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)std::min<int64_t>((all + 255) / 256, 16 * kCus)), dim3(256),
-                           0, st, a);
-    }
+    if (p.split > 1)
+        hipLaunchKernelGGL(join_grad_kernel<float>, dim3(join_grid(n * channels * width)), dim3(256), 0, st, a);
     return done("relaysum_linear_backward_weight");
 }
 

@@ -102,10 +102,10 @@ def _lib():
             "relaysum_rmsnorm_workspace": (i64, [i32, i64, i64]),
             "relaysum_rmsnorm_backward": (ctypes.c_int, [i32, i64, i64, rows, rows, packed, vp, vp,
                                                          i64, rows, rows, vp, sz, vp]),
-            "relaysum_linear": (ctypes.c_int, [i32, i64, i64, i64, packed, packed, rows, vp]),
+            "relaysum_linear": (ctypes.c_int, [i32, i64, i64, i64, packed, packed, rows, vp, sz, vp]),
             "relaysum_linear_backward_input": (ctypes.c_int, [i32, i64, i64, i64, rows, packed,
-                                                              rows, vp]),
-            "relaysum_linear_workspace": (i64, [i32, i64, i64, i64]),
+                                                              rows, vp, sz, vp]),
+            "relaysum_linear_workspace": (i64, [i32, i64, i64, i64, i32]),
             "relaysum_linear_backward_weight": (ctypes.c_int, [i32, i64, i64, i64, rows, packed,
                                                                rows, vp, sz, vp]),
             "relaysum_layer_error": (ctypes.c_char_p, []),
@@ -252,8 +252,11 @@ def linear(x: Packed, w: Packed, dtype=torch.bfloat16):
     n, tokens, width = x.shape
     channels = w.shape[1]
     y = torch.empty((n, tokens, channels), dtype=dtype, device=x.codes.device)
-    _check(_lib().relaysum_linear(n, tokens, width, channels, x._c(), w._c(),
-                                  _rows(y, "y", y.shape), _current_stream()), "relaysum_linear")
+    lib = _lib()
+    need = lib.relaysum_linear_workspace(n, tokens, width, channels, TYPES[dtype])
+    ws = _workspace(need, y.device)
+    _check(lib.relaysum_linear(n, tokens, width, channels, x._c(), w._c(), _rows(y, "y", y.shape),
+                               _ptr(ws), max(need, 0), _current_stream()), "relaysum_linear")
     return y
 
 
@@ -264,8 +267,12 @@ def linear_backward_input(dy, w: Packed):
         raise ValueError(f"dy of {list(dy.shape)} does not go with packed rows of {list(w.shape)}")
     rdy = _rows(dy, "dy", dy.shape)
     dx = torch.empty((n, tokens, w.width), dtype=dy.dtype, device=dy.device)
-    _check(_lib().relaysum_linear_backward_input(n, tokens, w.width, channels, rdy, w._c(),
-                                                 _rows(dx, "dx", dx.shape), _current_stream()),
+    lib = _lib()
+    need = lib.relaysum_linear_workspace(n, tokens, w.width, channels, rdy.type)
+    ws = _workspace(need, dy.device)
+    _check(lib.relaysum_linear_backward_input(n, tokens, w.width, channels, rdy, w._c(),
+                                              _rows(dx, "dx", dx.shape), _ptr(ws), max(need, 0),
+                                              _current_stream()),
            "relaysum_linear_backward_input")
     return dx
 
@@ -279,7 +286,7 @@ def linear_backward_weight(dy, x: Packed, weight_grad) -> None:
     rdy = _rows(dy, "dy", dy.shape)
     rg = _rows(weight_grad, "weight_grad", (n, channels, x.width), torch.float32)
     lib = _lib()
-    need = lib.relaysum_linear_workspace(n, tokens, x.width, channels)
+    need = lib.relaysum_linear_workspace(n, tokens, x.width, channels, rdy.type)
     ws = _workspace(need, dy.device)
     _check(lib.relaysum_linear_backward_weight(n, tokens, x.width, channels, rdy, x._c(), rg,
                                                _ptr(ws), max(need, 0), _current_stream()),

@@ -353,7 +353,7 @@ def test_linear_gradients(n, tokens, width, channels, dtype):
 def test_weight_gradient_over_many_tokens(n, tokens, width, channels, dtype):
     """A long sum for few results, in parts that are joined."""
     announce(f"weight gradient {n} {tokens} {width} {channels} {dtype}")
-    assert layer._lib().relaysum_linear_workspace(n, tokens, width, channels) > 0
+    assert layer._lib().relaysum_linear_workspace(n, tokens, width, channels, layer.TYPES[dtype]) > 0
     x, dy = codes_of(4, n, tokens, width), normal(3, n, tokens, channels, std=1e-2, dtype=dtype)
     dw, around = in_model(torch.zeros(n, channels, width, device="cuda"))
     layer.linear_backward_weight(dy, x, dw)

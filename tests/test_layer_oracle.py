@@ -153,13 +153,14 @@ def test_gradients_refuse():
     assert lib.relaysum_rmsnorm_backward(*args, None, need, None) == bad and "workspace" in _text()
     args = args[:10] + (_rows(0x700000000, 1, 512, 0), 0x800000000, need, None)
     assert lib.relaysum_rmsnorm_backward(*args) == bad and "float" in _text()
-    assert lib.relaysum_linear(1, 1, 64, 0, _packed(), _packed(), _rows(), None) == bad
+    assert lib.relaysum_linear(1, 1, 64, 0, _packed(), _packed(), _rows(), None, 0, None) == bad
     assert "channels" in _text()
     assert lib.relaysum_linear(1, 1, 256, 64, _packed(group=128), _packed(3 << 30, 7 << 30), _rows(),
-                               None) == bad and "whole" in _text()
+                               None, 0, None) == bad and "whole" in _text()
     assert lib.relaysum_linear_backward_input(1, 1, 64, 64, _rows(type=1), _packed(),
-                                              _rows(2 << 20), None) == bad and "type" in _text()
-    assert lib.relaysum_linear_workspace(0, 1, 64, 64) == -1
+                                              _rows(2 << 20), None, 0, None) == bad and "type" in _text()
+    assert lib.relaysum_linear_workspace(0, 1, 64, 64, 0) == -1
+    assert lib.relaysum_linear_workspace(1, 1, 64, 64, 3) == -1
     assert lib.relaysum_rmsnorm_workspace(1, -1, 64) == -1
 
 
