@@ -397,19 +397,30 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs a
     }
 }
 
-// out[i][c] = sum over parts of partial[i][p][c], p ascending: the order is
-// fixed, so equal inputs give equal bits.
+// out[i][c] = sum over parts of partial[i][p][c].  A workgroup has 32 columns
+// of one worker and 8 sums of every eighth part each, added in a fixed order,
+// so equal inputs give equal bits.
 __global__ __launch_bounds__(256) void sum_parts_kernel(const float *partial, float *out,
                                                         int64_t out_stride, int32_t parts,
                                                         int32_t width) {
-    const int per = (width + 255) / 256;
+    __shared__ float sums[8][32];
+    const unsigned per = (width + 31) / 32;
     const int64_t worker = blockIdx.x / per;
-    const int c = (int)(blockIdx.x % per) * 256 + threadIdx.x;
-    if (c >= width) return;
-    const float *p = partial + worker * parts * (int64_t)width + c;
+    const int lane = threadIdx.x % 32, group = threadIdx.x / 32;
+    const int c = (int)(blockIdx.x % per) * 32 + lane;
     float v = 0.0f;
-    for (int k = 0; k < parts; ++k) v += p[(int64_t)k * width];
-    out[worker * out_stride + c] = v;
+    if (c < width) {
+        const float *p = partial + worker * parts * (int64_t)width + c;
+#pragma unroll 4
+        for (int k = group; k < parts; k += 8) v += p[(int64_t)k * width];
+    }
+    sums[group][lane] = v;
+    __syncthreads();
+    if (group == 0 && c < width) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) v += sums[k][lane];
+        out[worker * out_stride + c] = v;
+    }
 }
 
 // ---- products ------------------------------------------------------------------------
@@ -451,6 +462,8 @@ __device__ __forceinline__ int moved(int at, int j, int ks) {
     const int row = tile_row<Q>(j, 0);
     return (at ^ ((ks * 4 ^ swizzle(row)) << 4)) + row * 128;
 }
+// From a chunk's place in a row that 4 divides to the same chunk x < 4 rows on.
+__device__ __forceinline__ int column_at(int at, int x) { return (at ^ (swizzle(x) << 4)) + x * 128; }
 __device__ __forceinline__ int fresh(int v) {
     asm volatile("" : "+v"(v));
     return v;
@@ -488,7 +501,7 @@ __device__ __forceinline__ void write_entries(O *row, int c0, int cols, const V 
 }
 
 // Kinds of instructions for the scheduler's groups.
-constexpr int kMfma = 0x8, kDsRead = 0x100;
+constexpr int kVector = 0x2, kMfma = 0x8, kLoad = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
 
 struct LinearArgs {
     Packed x, w;
@@ -773,7 +786,7 @@ struct GradTile {
         for (int i = 0; i < UB; ++i) {
             const int u = i * kThreads + threadIdx.x;
             if (kUnitsB % kThreads && u >= kUnitsB) break;
-            const int nn = u % (BN / 4) * 4, rr = u / (BN / 4) * 8;
+            const int at = tile_at(u % (BN / 4) * 4, u / (BN / 4));
             float scale[8];
 #pragma unroll
             for (int y = 0; y < 8; ++y)
@@ -783,14 +796,14 @@ struct GradTile {
                 b8_t v;
 #pragma unroll
                 for (int y = 0; y < 8; ++y) v[y] = (__bf16)(code_at(h.q[i][y], x) * scale[y]);
-                *reinterpret_cast<b8_t *>(lds + kA + tile_at(nn + x, rr / 8)) = v;
+                *reinterpret_cast<b8_t *>(lds + kA + column_at(at, x)) = v;
             }
         }
 #pragma unroll
         for (int i = 0; i < UA; ++i) {
             const int u = i * kThreads + threadIdx.x;
             if (kUnitsA % kThreads && u >= kUnitsA) break;
-            const int mm = ALONG_R ? u % (BM / 4) * 4 : u / 8, ch = ALONG_R ? u / (BM / 4) : u % 8;
+            const int at = ALONG_R ? tile_at(u % (BM / 4) * 4, u / (BM / 4)) : tile_at(u / 8, u % 8);
 #pragma unroll
             for (int x = 0; x < (ALONG_R ? 4 : 1); ++x) {
                 b8_t v[P];
@@ -803,7 +816,7 @@ struct GradTile {
                 }
 #pragma unroll
                 for (int k = 0; k < P; ++k)
-                    *reinterpret_cast<b8_t *>(lds + tile_at(k * BM + mm + x, ch)) = v[k];
+                    *reinterpret_cast<b8_t *>(lds + k * BM * 128 + column_at(at, x)) = v[k];
             }
         }
     }
@@ -828,6 +841,30 @@ struct GradTile {
                     for (int j = 0; j < TN; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
             }
+        }
+    }
+
+    // The order of a step's instructions: the next step's loads, the first
+    // half's reads, the second half's among the first products; the loaded
+    // rows' conversions among the last eighth, as late as leaves them hidden:
+    // a step takes about as long as a load (dX of 16 x 2048 x 4096 -> 1024:
+    // 303 us in the compiler's order, 276 with the conversions among the last
+    // quarter, 271 among the last eighth; dW 391, 346, 339).
+    static __device__ __forceinline__ void interleave() {
+        constexpr int M = TM * TN * P;   // products of one half
+        __builtin_amdgcn_sched_group_barrier(kLoad, 64, 0);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, TN + P * TM, 0);
+#pragma unroll
+        for (int q = 0; q < M / 2; ++q) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMfma, M * 3 / 4, 0);
+#pragma unroll
+        for (int q = 0; q < M / 4; ++q) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kVector, 18, 0);
+            __builtin_amdgcn_sched_group_barrier(kDsWrite, 1, 0);
         }
     }
 };
@@ -869,6 +906,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
             G::multiply(lds + cur, aat, bat, acc);
             cur ^= G::kBytes;
             G::store(h, lds + cur);
+            G::interleave();
             __syncthreads();
         }
         for (; s < s1; ++s) {
@@ -1411,7 +1449,7 @@ int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const re
         });
     });
     if (parts > 1)
-        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)(n * ((width + 255) / 256))), dim3(256), 0, st,
+        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)(n * ((width + 31) / 32))), dim3(256), 0, st,
                            a.partial, reinterpret_cast<float *>(grad.data), grad.ws, parts, (int32_t)width);
     return done("relaysum_rmsnorm_backward");
 }

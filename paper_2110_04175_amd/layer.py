@@ -12,11 +12,10 @@ the tensor given for them.  Work is queued on torch's current stream.
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
 
 import torch
 
-from . import RELAYSUM_OK, RelaySumError, _current_stream, load_library
+from . import RELAYSUM_OK, RelaySumError, load_library
 
 RELAYSUM_FLOAT = 0
 RELAYSUM_BFLOAT = 1
@@ -44,36 +43,75 @@ class Packed:
     int8 [n, rows, groups], for rows of ``width`` entries; groups is 1 (whole
     rows share a scale) or stride / 128."""
 
-    __slots__ = ("codes", "exps", "width")
+    __slots__ = ("_codes", "_exps", "_buffer", "_n", "_rows", "_groups", "_device", "width")
 
     def __init__(self, codes, exps, width: int):
-        self.codes, self.exps, self.width = codes, exps, int(width)
-        n, rows, stride = codes.shape
-        if stride != packed_stride(self.width):
-            raise ValueError(f"rows of {self.width} entries have codes of stride "
-                             f"{packed_stride(self.width)}, not {stride}")
-        if exps.dim() != 3 or exps.shape[0] != n or exps.shape[1] != rows or \
-                exps.shape[2] not in (1, stride // GROUP):
-            raise ValueError(f"exps must have shape [{n}, {rows}, 1 or {stride // GROUP}]")
+        width = int(width)
+        stride = packed_stride(width)
         for t, name in ((codes, "codes"), (exps, "exps")):
-            if t.dtype != torch.int8 or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous int8 tensor")
-            _check_device(t, name)
-        if codes.device != exps.device:
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+            if t.dtype != torch.int8 or t.dim() != 3 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int8 tensor of three axes")
+        n, rows, held = codes.shape
+        if held != stride:
+            raise ValueError(f"rows of {width} entries have codes of stride {stride}, not {held}")
+        groups = exps.shape[2]
+        if exps.shape[0] != n or exps.shape[1] != rows or groups not in (1, stride // GROUP):
+            raise ValueError(f"exps must have shape [{n}, {rows}, 1 or {stride // GROUP}]")
+        if codes.get_device() != exps.get_device():
             raise ValueError("codes and exps must be on one device")
+        self._codes, self._exps, self._buffer = codes, exps, None
+        self._n, self._rows, self._groups, self._device = n, rows, groups, codes.get_device()
+        self.width = width
+
+    @classmethod
+    def _new(cls, n: int, rows: int, width: int, group: int, like):
+        """Room for packed rows, in one allocation: codes, then exponents."""
+        p = cls.__new__(cls)
+        stride = packed_stride(width)
+        p._n, p._rows, p._groups, p.width = n, rows, stride // GROUP if group else 1, width
+        p._codes = p._exps = None
+        p._device = like.get_device()
+        p._buffer = torch.empty(n * rows * (stride + p._groups), dtype=torch.int8, device=like.device)
+        return p
+
+    @property
+    def stride(self) -> int:
+        return -(-self.width // GROUP) * GROUP
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            size = self._n * self._rows * self.stride
+            self._codes = self._buffer[:size].view(self._n, self._rows, self.stride)
+        return self._codes
+
+    @property
+    def exps(self):
+        if self._exps is None:
+            size = self._n * self._rows * self.stride
+            self._exps = self._buffer[size:].view(self._n, self._rows, self._groups)
+        return self._exps
 
     @property
     def group(self) -> int:
         """128, or 0 for whole rows."""
-        return 0 if self.exps.shape[2] == 1 else GROUP
+        return 0 if self._groups == 1 else GROUP
 
     @property
     def shape(self):
         """(n, rows, width)."""
-        return (*self.codes.shape[:2], self.width)
+        return (self._n, self._rows, self.width)
 
-    def _c(self):
-        return _CPacked(self.codes.data_ptr(), self.exps.data_ptr(), self.group)
+    def _c(self, device: int, name: str):
+        if self._device != device:
+            raise ValueError(f"{name} must be on the current device")
+        group = 0 if self._groups == 1 else GROUP
+        if self._buffer is not None:
+            at = self._buffer.data_ptr()
+            return _CPacked(at, at + self._n * self._rows * self.stride, group)
+        return _CPacked(self._codes.data_ptr(), self._exps.data_ptr(), group)
 
 
 def packed_stride(width: int) -> int:
@@ -122,61 +160,64 @@ def _check(rc: int, what: str) -> None:
         raise RelaySumError(rc, f"{what} ({_lib().relaysum_layer_error().decode()})")
 
 
-def _check_device(t, name: str) -> None:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current device")
-
-
-def _rows(t, name: str, shape, dtype=None) -> Rows:
+def _rows(t, name: str, shape, device: int, dtype=None) -> Rows:
     """The description of a tensor [n, rows, width] (or [n, width]: one row
     for each worker) whose last axis is dense."""
-    _check_device(t, name)
-    if tuple(t.shape) != tuple(shape):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the current device")
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
-    if t.dtype not in TYPES or (dtype is not None and t.dtype != dtype):
+    code = TYPES.get(t.dtype)
+    if code is None or (dtype is not None and t.dtype != dtype):
         want = dtype if dtype is not None else "float32, bfloat16 or float16"
         raise ValueError(f"{name} must be {want}, not {t.dtype}")
     st = t.stride()
-    if t.shape[-1] > 1 and st[-1] != 1 and t.numel():
+    if st[-1] != 1 and t.shape[-1] > 1 and t.numel():
         raise ValueError(f"{name}: the last axis must be dense")
-    return Rows(t.data_ptr(), TYPES[t.dtype], st[0], st[1] if len(st) == 3 else 0)
+    return Rows(t.data_ptr(), code, st[0], st[1] if len(st) == 3 else 0)
 
 
 def _three(t, name: str):
-    _check_device(t, name)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.dim() != 3:
         raise ValueError(f"{name} must have three axes: workers, rows, width")
     return t.shape
 
 
-def _new_packed(n: int, rows: int, width: int, group: int, device) -> Packed:
-    stride = packed_stride(width)
-    codes = torch.empty((n, rows, stride), dtype=torch.int8, device=device)
-    exps = torch.empty((n, rows, stride // GROUP if group else 1), dtype=torch.int8, device=device)
-    p = Packed.__new__(Packed)   # its parts fit by construction
-    p.codes, p.exps, p.width = codes, exps, int(width)
-    return p
+def _out(n: int, rows: int, width: int, dtype, device):
+    """(a new dense tensor [n, rows, width], its description)."""
+    t = torch.empty((n, rows, width), dtype=dtype, device=device)
+    return t, Rows(t.data_ptr(), TYPES[dtype], rows * width, width)
 
 
 def _workspace(nbytes: int, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes > 0 else None
+    """(address, bytes, what keeps it) of a workspace.  Memory of torch's
+    allocator for the current stream, on which the call is queued too."""
+    if nbytes <= 0:
+        return None, 0, None
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return t.data_ptr(), nbytes, t
 
 
-def _ptr(t) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _here():
+    """The current device and the address of its current stream."""
+    device = torch.cuda.current_device()
+    return device, torch._C._cuda_getCurrentRawStream(device)
 
 
 def pack(v, group: int = 0) -> Packed:
     """Rows v[n, rows, width] in 8 bits, one scale for each row (group 0) or
     for each 128 entries of it (group 128)."""
-    n, rows, width = _three(v, "v")
+    n, rows, width = shape = _three(v, "v")
     if group not in (0, GROUP):
         raise ValueError(f"group must be 0 or {GROUP}")
-    r = _rows(v, "v", v.shape)
-    out = _new_packed(n, rows, width, group, v.device)
-    _check(_lib().relaysum_pack(n, rows, width, r, out._c(), _current_stream()), "relaysum_pack")
+    device, stream = _here()
+    r = _rows(v, "v", shape, device)
+    out = Packed._new(n, rows, width, group, v)
+    _check(_lib().relaysum_pack(n, rows, width, r, out._c(device, "out"), stream), "relaysum_pack")
     return out
 
 
@@ -185,9 +226,10 @@ def unpack(p: Packed, dtype=torch.bfloat16):
     n, rows, width = p.shape
     if dtype not in TYPES:
         raise ValueError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
-    out = torch.empty((n, rows, width), dtype=dtype, device=p.codes.device)
-    _check(_lib().relaysum_unpack(n, rows, width, p._c(), _rows(out, "out", out.shape),
-                                  _current_stream()), "relaysum_unpack")
+    device, stream = _here()
+    cp = p._c(device, "p")
+    out, ro = _out(n, rows, width, dtype, device)
+    _check(_lib().relaysum_unpack(n, rows, width, cp, ro, stream), "relaysum_unpack")
     return out
 
 
@@ -196,20 +238,21 @@ def rmsnorm(h, residual, weight, eps: float = 1e-6, keep: bool = True):
     packed by whole rows, rstd[n, tokens] = 1 / sqrt(mean(sum^2) + eps), and
     saved = sum packed by 128, for rmsnorm_backward (None without `keep`).
     weight[n, width]; residual may be None (sum is then h itself)."""
-    n, tokens, width = _three(h, "h")
-    rh = _rows(h, "h", h.shape)
-    rw = _rows(weight, "weight", (n, width), torch.float32)
+    n, tokens, width = shape = _three(h, "h")
+    device, stream = _here()
+    rh = _rows(h, "h", shape, device)
+    rw = _rows(weight, "weight", (n, width), device, torch.float32)
     out, rr, rs = h, None, None
     if residual is not None:
-        rr = _rows(residual, "residual", h.shape, h.dtype)
-        out = torch.empty((n, tokens, width), dtype=h.dtype, device=h.device)
-        rs = _rows(out, "sum", out.shape)
-    y = _new_packed(n, tokens, width, 0, h.device)
-    saved = _new_packed(n, tokens, width, GROUP, h.device) if keep else None
-    rstd = torch.empty((n, tokens), dtype=torch.float32, device=h.device)
-    _check(_lib().relaysum_rmsnorm(n, tokens, width, rh, rr, rw.data, rw.worker_stride, float(eps),
-                                   rs, y._c(), rstd.data_ptr(), saved._c() if keep else None,
-                                   _current_stream()), "relaysum_rmsnorm")
+        rr = _rows(residual, "residual", shape, device, h.dtype)
+        out, rs = _out(n, tokens, width, h.dtype, device)
+    y = Packed._new(n, tokens, width, 0, h)
+    saved = Packed._new(n, tokens, width, GROUP, h) if keep else None
+    rstd = torch.empty((n, tokens), dtype=torch.float32, device=device)
+    _check(_lib().relaysum_rmsnorm(n, tokens, width, rh, rr, rw.data, rw.worker_stride, eps, rs,
+                                   y._c(device, "y"), rstd.data_ptr(),
+                                   saved._c(device, "saved") if keep else None, stream),
+           "relaysum_rmsnorm")
     return out, y, rstd, saved
 
 
@@ -217,77 +260,75 @@ def rmsnorm_backward(dy, dsum, saved: Packed, rstd, weight, weight_grad):
     """The gradient of h and residual alike, as a new tensor, from the
     gradients dy of y and dsum of the sum (None: the sum is not used
     elsewhere); the weight's gradient overwrites weight_grad[n, width]."""
-    n, tokens, width = _three(dy, "dy")
-    rdy = _rows(dy, "dy", dy.shape)
-    rd = None if dsum is None else _rows(dsum, "dsum", dy.shape, dy.dtype)
+    n, tokens, width = shape = _three(dy, "dy")
+    device, stream = _here()
+    rdy = _rows(dy, "dy", shape, device)
+    rd = None if dsum is None else _rows(dsum, "dsum", shape, device, dy.dtype)
     if saved.shape != (n, tokens, width):
         raise ValueError(f"saved must hold rows [{n}, {tokens}, {width}], not {list(saved.shape)}")
-    rw = _rows(weight, "weight", (n, width), torch.float32)
-    rg = _rows(weight_grad, "weight_grad", (n, width), torch.float32)
-    _rows(rstd, "rstd", (n, tokens), torch.float32)
+    rw = _rows(weight, "weight", (n, width), device, torch.float32)
+    rg = _rows(weight_grad, "weight_grad", (n, width), device, torch.float32)
+    _rows(rstd, "rstd", (n, tokens), device, torch.float32)
     if not rstd.is_contiguous():
         raise ValueError("rstd must be contiguous")
-    ds = torch.empty((n, tokens, width), dtype=dy.dtype, device=dy.device)
+    ds, rs = _out(n, tokens, width, dy.dtype, device)
     lib = _lib()
-    need = lib.relaysum_rmsnorm_workspace(n, tokens, width)
-    ws = _workspace(need, dy.device)
-    _check(lib.relaysum_rmsnorm_backward(n, tokens, width, rdy, rd, saved._c(), rstd.data_ptr(),
-                                         rw.data, rw.worker_stride, _rows(ds, "ds", ds.shape), rg,
-                                         _ptr(ws), max(need, 0), _current_stream()),
-           "relaysum_rmsnorm_backward")
+    ws, size, _keep = _workspace(lib.relaysum_rmsnorm_workspace(n, tokens, width), device)
+    _check(lib.relaysum_rmsnorm_backward(n, tokens, width, rdy, rd, saved._c(device, "saved"),
+                                         rstd.data_ptr(), rw.data, rw.worker_stride, rs, rg, ws,
+                                         size, stream), "relaysum_rmsnorm_backward")
     return ds
-
-
-def _same_width(x: Packed, w: Packed) -> None:
-    if x.shape[0] != w.shape[0] or x.width != w.width:
-        raise ValueError(f"packed rows of {list(x.shape)} and {list(w.shape)} do not go together")
 
 
 def linear(x: Packed, w: Packed, dtype=torch.bfloat16):
     """y[n, tokens, channels] = x w^T of rows packed whole: tokens x[n, tokens,
     width], channels w[n, channels, width]."""
-    _same_width(x, w)
+    n, tokens, width = x.shape
+    if w.shape[0] != n or w.width != width:
+        raise ValueError(f"packed rows of {list(x.shape)} and {list(w.shape)} do not go together")
     if dtype not in TYPES:
         raise ValueError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
-    n, tokens, width = x.shape
     channels = w.shape[1]
-    y = torch.empty((n, tokens, channels), dtype=dtype, device=x.codes.device)
+    device, stream = _here()
+    cx, cw = x._c(device, "x"), w._c(device, "w")
+    y, ry = _out(n, tokens, channels, dtype, device)
     lib = _lib()
-    need = lib.relaysum_linear_workspace(n, tokens, width, channels, TYPES[dtype])
-    ws = _workspace(need, y.device)
-    _check(lib.relaysum_linear(n, tokens, width, channels, x._c(), w._c(), _rows(y, "y", y.shape),
-                               _ptr(ws), max(need, 0), _current_stream()), "relaysum_linear")
+    ws, size, _keep = _workspace(
+        lib.relaysum_linear_workspace(n, tokens, width, channels, ry.type), device)
+    _check(lib.relaysum_linear(n, tokens, width, channels, cx, cw, ry, ws, size, stream),
+           "relaysum_linear")
     return y
 
 
 def linear_backward_input(dy, w: Packed):
     """dx[n, tokens, width] = dy w, for dy[n, tokens, channels]."""
-    n, tokens, channels = _three(dy, "dy")
+    n, tokens, channels = shape = _three(dy, "dy")
     if w.shape[:2] != (n, channels):
-        raise ValueError(f"dy of {list(dy.shape)} does not go with packed rows of {list(w.shape)}")
-    rdy = _rows(dy, "dy", dy.shape)
-    dx = torch.empty((n, tokens, w.width), dtype=dy.dtype, device=dy.device)
+        raise ValueError(f"dy of {list(shape)} does not go with packed rows of {list(w.shape)}")
+    width = w.width
+    device, stream = _here()
+    rdy, cw = _rows(dy, "dy", shape, device), w._c(device, "w")
+    dx, rdx = _out(n, tokens, width, dy.dtype, device)
     lib = _lib()
-    need = lib.relaysum_linear_workspace(n, tokens, w.width, channels, rdy.type)
-    ws = _workspace(need, dy.device)
-    _check(lib.relaysum_linear_backward_input(n, tokens, w.width, channels, rdy, w._c(),
-                                              _rows(dx, "dx", dx.shape), _ptr(ws), max(need, 0),
-                                              _current_stream()),
-           "relaysum_linear_backward_input")
+    ws, size, _keep = _workspace(
+        lib.relaysum_linear_workspace(n, tokens, width, channels, rdy.type), device)
+    _check(lib.relaysum_linear_backward_input(n, tokens, width, channels, rdy, cw, rdx, ws, size,
+                                              stream), "relaysum_linear_backward_input")
     return dx
 
 
 def linear_backward_weight(dy, x: Packed, weight_grad) -> None:
     """weight_grad[n, channels, width] = dy^T x, for dy[n, tokens, channels]
     and packed x[n, tokens, width] of either group."""
-    n, tokens, channels = _three(dy, "dy")
+    n, tokens, channels = shape = _three(dy, "dy")
     if x.shape[:2] != (n, tokens):
-        raise ValueError(f"dy of {list(dy.shape)} does not go with packed rows of {list(x.shape)}")
-    rdy = _rows(dy, "dy", dy.shape)
-    rg = _rows(weight_grad, "weight_grad", (n, channels, x.width), torch.float32)
+        raise ValueError(f"dy of {list(shape)} does not go with packed rows of {list(x.shape)}")
+    width = x.width
+    device, stream = _here()
+    rdy, cx = _rows(dy, "dy", shape, device), x._c(device, "x")
+    rg = _rows(weight_grad, "weight_grad", (n, channels, width), device, torch.float32)
     lib = _lib()
-    need = lib.relaysum_linear_workspace(n, tokens, x.width, channels, rdy.type)
-    ws = _workspace(need, dy.device)
-    _check(lib.relaysum_linear_backward_weight(n, tokens, x.width, channels, rdy, x._c(), rg,
-                                               _ptr(ws), max(need, 0), _current_stream()),
-           "relaysum_linear_backward_weight")
+    ws, size, _keep = _workspace(
+        lib.relaysum_linear_workspace(n, tokens, width, channels, rdy.type), device)
+    _check(lib.relaysum_linear_backward_weight(n, tokens, width, channels, rdy, cx, rg, ws, size,
+                                               stream), "relaysum_linear_backward_weight")

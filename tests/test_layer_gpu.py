@@ -216,11 +216,12 @@ def test_norm_in_place():
     want = layer.rmsnorm(h, r, w, EPS)
     for over in (0, 1):
         a, b = h.clone(), r.clone()
-        y = layer._new_packed(n, t, k, 0, h.device)
+        y = layer.pack(torch.zeros_like(h))
         rstd = torch.empty(n, t, device="cuda")
-        ra, rb = layer._rows(a, "h", a.shape), layer._rows(b, "r", b.shape)
+        ra, rb = (layer.Rows(v.data_ptr(), 0, t * k, k) for v in (a, b))
+        cy = layer._CPacked(y.codes.data_ptr(), y.exps.data_ptr(), 0)
         rc = layer._lib().relaysum_rmsnorm(n, t, k, ra, rb, w.data_ptr(), k, EPS, (ra, rb)[over],
-                                           y._c(), rstd.data_ptr(), None, rs._current_stream())
+                                           cy, rstd.data_ptr(), None, rs._current_stream())
         assert rc == 0
         assert torch.equal((a, b)[over], want[0]) and torch.equal(y.codes, want[1].codes)
 
