@@ -439,9 +439,12 @@ __device__ __forceinline__ int tile_at(int row, int chunk) {
     return row * 128 + ((chunk ^ swizzle(row)) << 4);
 }
 
-// Which result a matrix instruction's row r of tile j is: tiles go by fours
-// (Q), and a lane's 4 rows of each of them are neighbours, so that a lane ends
-// up with 4 * Q entries in a row of the result.
+// Which result a matrix instruction's row r of tile j is: tiles go by Q, and a
+// lane's 4 rows of each of them are neighbours, so that a lane ends up with
+// 4 * Q entries in a row of the result, 32 bytes of it (dW of 16 x 2048 x 4096
+// -> 1024: 304 us, 325 with 64 bytes; the product in bfloat16 184 us, 195 with 16).
+template <typename O>
+constexpr int kFours = 8 / (int)sizeof(O);
 template <int Q>
 __device__ __forceinline__ int tile_row(int j, int r) {
     return j / Q * 16 * Q + r / 4 * 4 * Q + j % Q * 4 + r % 4;
@@ -501,7 +504,7 @@ __device__ __forceinline__ void write_entries(O *row, int c0, int cols, const V 
 }
 
 // Kinds of instructions for the scheduler's groups.
-constexpr int kVector = 0x2, kMfma = 0x8, kLoad = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
+constexpr int kMfma = 0x8, kDsRead = 0x100;
 
 struct LinearArgs {
     Packed x, w;
@@ -515,10 +518,10 @@ struct LinearArgs {
 
 // Y[t][c] = 2^(ex[t] + ew[c]) * sum_k qx[t][k] qw[c][k]: whole numbers until
 // the one conversion (rounded to 24 bits from 2^24 on, then to the type).
-template <int BM, int BN, int WM, int WN>
+template <int BM, int BN, int WM, int WN, int QMAX>
 struct LinearTile {
     static constexpr int kThreads = 64 * WM * WN, kBytes = (BM + BN) * 128;
-    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, Q = TN < 4 ? TN : 4;
+    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, Q = TN < QMAX ? TN : QMAX;
     static constexpr int kCopies = ((BM + BN) * 8 + kThreads - 1) / kThreads;
     static_assert(BM % 8 == 0 && BN % 8 == 0, "a wave's copy, 8 rows, is of one operand");
 
@@ -563,7 +566,7 @@ struct LinearTile {
 
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void linear_kernel(LinearArgs a) {
-    using L = LinearTile<BM, BN, WM, WN>;
+    using L = LinearTile<BM, BN, WM, WN, kFours<T>>;
     constexpr int TM = L::TM, TN = L::TN, Q = L::Q;
     __shared__ __align__(16) char lds[2 * L::kBytes];
     const unsigned tile = xcd_tile(blockIdx.x, gridDim.x);
@@ -691,11 +694,11 @@ template <> struct Parts<float> { static constexpr int n = 3; };
 // (dX: m tokens, r channels) or dY[r][m] (ALONG_R, dW: m channels, r tokens).
 // Both operands are brought into LDS as bfloat16 rows along r, 64 of r a step:
 // 8 x 4 blocks of codes, and of dY for dW, are turned in registers on the way.
-template <typename T, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
+template <typename T, int QMAX, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
 struct GradTile {
     static constexpr int kThreads = 64 * WM * WN, P = Parts<T>::n, BR = 64;
     static constexpr int kA = P * BM * 128, kBytes = kA + BN * 128;
-    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, Q = TN < 4 ? TN : 4;
+    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16, Q = TN < QMAX ? TN : QMAX;
     // Units of one thread: 8 r of one m (dX), or 8 r of 4 m (dW); 8 r of 4 columns.
     static constexpr int kUnitsA = BM * BR / (ALONG_R ? 32 : 8), kUnitsB = BN * BR / 32;
     static constexpr int UA = (kUnitsA + kThreads - 1) / kThreads, UB = (kUnitsB + kThreads - 1) / kThreads;
@@ -787,10 +790,19 @@ struct GradTile {
             const int u = i * kThreads + threadIdx.x;
             if (kUnitsB % kThreads && u >= kUnitsB) break;
             const int at = tile_at(u % (BN / 4) * 4, u / (BN / 4));
+            // The exponents are the same for a wave where its rows are; taken from
+            // the first lane here and not, with a wait for memory, where they
+            // are loaded.
+            u2_t e = GROUPED ? u2_t{0, 0} : h.e[i];
+            if (!GROUPED) {
+                asm volatile("" : "+v"(e));
+                if (BN / 4 % kWave == 0)
+                    e = u2_t{(unsigned)__builtin_amdgcn_readfirstlane(e.x), (unsigned)__builtin_amdgcn_readfirstlane(e.y)};
+            }
             float scale[8];
 #pragma unroll
             for (int y = 0; y < 8; ++y)
-                scale[y] = scale_of(GROUPED ? h.eg[i][y] : (int)(int8_t)(h.e[i][y / 4] >> (8 * (y % 4))));
+                scale[y] = scale_of(GROUPED ? h.eg[i][y] : (int)(int8_t)(e[y / 4] >> (8 * (y % 4))));
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 b8_t v;
@@ -842,36 +854,20 @@ struct GradTile {
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
             }
         }
-    }
-
-    // The order of a step's instructions: the next step's loads, the first
-    // half's reads, the second half's among the first products; the loaded
-    // rows' conversions among the last eighth, as late as leaves them hidden:
-    // a step takes about as long as a load (dX of 16 x 2048 x 4096 -> 1024:
-    // 303 us in the compiler's order, 276 with the conversions among the last
-    // quarter, 271 among the last eighth; dW 391, 346, 339).
-    static __device__ __forceinline__ void interleave() {
-        constexpr int M = TM * TN * P;   // products of one half
-        __builtin_amdgcn_sched_group_barrier(kLoad, 64, 0);
+        // All of the first half's reads, then the second half's among the products.
+        constexpr int M = TM * TN * P;
         __builtin_amdgcn_sched_group_barrier(kDsRead, TN + P * TM, 0);
 #pragma unroll
         for (int q = 0; q < M / 2; ++q) {
             __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
             __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(kMfma, M * 3 / 4, 0);
-#pragma unroll
-        for (int q = 0; q < M / 4; ++q) {
-            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(kVector, 18, 0);
-            __builtin_amdgcn_sched_group_barrier(kDsWrite, 1, 0);
-        }
     }
 };
 
 template <typename T, typename O, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
-    using G = GradTile<T, ALONG_R, GROUPED, BM, BN, WM, WN>;
+    using G = GradTile<T, kFours<O>, ALONG_R, GROUPED, BM, BN, WM, WN>;
     constexpr int TM = G::TM, TN = G::TN, Q = G::Q;
     __shared__ __align__(16) char lds[2 * G::kBytes];
     const unsigned per = (unsigned)a.tiles_m * a.tiles_n;
@@ -893,30 +889,36 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
         // Steps that are loaded in whole chunks: not the one that the axis ends
         // in, and none where the result's edge cuts a chunk of dY.
         const int64_t whole = ALONG_R && a.m % 4 && m0 + BM > a.m ? 0 : a.r / G::BR;
+        auto load = [&](int64_t s) {
+            if (s < whole) G::template load<true>(a, worker, m0, n0, s * G::BR, h);
+            else G::template load<false>(a, worker, m0, n0, s * G::BR, h);
+        };
+        // Two waves share a SIMD: one multiplies step s first and then brings
+        // s + 1 into LDS, the other the other way round, so that one's vector
+        // instructions run beside the other's matrix instructions.
+        const bool late = WM * WN == 8 && wave >= 4;
         int cur = 0;
-        if (s0 < whole)
-            G::template load<true>(a, worker, m0, n0, s0 * G::BR, h);
-        else
-            G::template load<false>(a, worker, m0, n0, s0 * G::BR, h);
+        load(s0);
         G::store(h, lds);
+        if (late && s0 + 1 < s1) load(s0 + 1);
         __syncthreads();
-        int64_t s = s0 + 1;
-        for (; s < min(s1, whole); ++s) {
-            G::template load<true>(a, worker, m0, n0, s * G::BR, h);
+        int64_t s = s0;
+        for (; s + 2 < min(s1, whole); ++s) {
+            if (late) G::store(h, lds + (cur ^ G::kBytes));
+            G::template load<true>(a, worker, m0, n0, (s + 1 + late) * G::BR, h);
             G::multiply(lds + cur, aat, bat, acc);
             cur ^= G::kBytes;
-            G::store(h, lds + cur);
-            G::interleave();
+            if (!late) G::store(h, lds + cur);
             __syncthreads();
         }
         for (; s < s1; ++s) {
-            G::template load<false>(a, worker, m0, n0, s * G::BR, h);
+            if (late && s + 1 < s1) G::store(h, lds + (cur ^ G::kBytes));
+            if (s + 1 + late < s1) load(s + 1 + late);
             G::multiply(lds + cur, aat, bat, acc);
             cur ^= G::kBytes;
-            G::store(h, lds + cur);
+            if (!late && s + 1 < s1) G::store(h, lds + cur);
             __syncthreads();
         }
-        G::multiply(lds + cur, aat, bat, acc);
     }
     // A lane has 4 * Q neighbouring columns of one row in Q accumulators.
 #pragma unroll
@@ -1271,9 +1273,9 @@ Plan plan_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels) {
 
 // The gradients' tiles: the first as large as two of its steps fit in LDS.
 Plan plan_grad(int32_t type, int64_t n, int64_t m, int64_t cols, int64_t r) {
-    static const TileCost tile[3][2] = {{{128, 128, 1, 1.9f, 2.0f, 4.5f}, {64, 128, 2, 1.5f, 2.5f, 4.0f}},
-                                        {{256, 256, 1, 1.85f, 2.3f, 5.0f}, {64, 128, 3, 0.8f, 1.5f, 3.5f}},
-                                        {{128, 256, 1, 2.1f, 2.5f, 4.5f}, {64, 128, 2, 1.35f, 1.8f, 3.5f}}};
+    static const TileCost tile[3][2] = {{{128, 128, 1, 1.65f, 1.95f, 4.5f}, {64, 128, 2, 1.35f, 2.3f, 4.0f}},
+                                        {{256, 256, 1, 1.65f, 2.0f, 5.0f}, {64, 128, 3, 0.75f, 1.45f, 3.5f}},
+                                        {{128, 256, 1, 1.8f, 2.3f, 4.5f}, {64, 128, 2, 1.25f, 1.8f, 3.5f}}};
     return plan_product(tile[type], 2, n, m, cols, tiles(r, 64));
 }
 
