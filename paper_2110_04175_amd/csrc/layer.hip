@@ -204,6 +204,13 @@ __device__ __forceinline__ void write_whole(const Packed &out, int64_t row, int3
     }
 }
 
+// Packing: one pass, the row in registers between its maximum and its codes.
+// Bound by memory: an entry's bytes in, one byte out.  16 x 4096 x 2048
+// bfloat16 by 128: 403 MB in 73 us, 5.5 TB/s (a copy of 1 GiB: 5.1); a weight
+// of 16 workers, 2048 x 1024 out of model rows of odd length: 168 MB in 24 us.
+// Rows of up to 128 entries take 16 lanes, up to 2048 a wave, wider ones a
+// workgroup: the fewer threads share a row, the fewer steps its maximum takes,
+// but 4 chunks of 8 entries a thread are what the registers hold well.
 template <typename T, int TPR, int J, bool GROUPED>
 __global__ __launch_bounds__(block_of(TPR)) void pack_kernel(PackArgs a) {
     __shared__ unsigned red[16];
@@ -226,6 +233,7 @@ __global__ __launch_bounds__(block_of(TPR)) void pack_kernel(PackArgs a) {
     }
 }
 
+// Unpacking: a byte in, an entry out; 403 MB in 71 us, 5.7 TB/s.
 template <typename T, int TPR>
 __global__ __launch_bounds__(256) void unpack_kernel(PackArgs a) {
     constexpr int kRows = 256 / TPR;
@@ -261,7 +269,10 @@ struct NormArgs {
 
 // s = h + r, rounded to the rows' type because that is what the stream goes on
 // with; y = s * rstd * w is not rounded before it is packed.  One pass: the row
-// stays in registers between the sum of squares and the codes.
+// stays in registers between the sum of squares and the codes.  Bound by
+// memory: 16 x 2048 x 1024 bfloat16 with s kept reads 4 bytes of an entry and
+// writes 4: 268 MB in 49 us, 5.5 TB/s.  The weights, a row for each worker,
+// come from the caches.
 template <typename T, int TPR, int J, bool RESIDUAL, bool KEEP>
 __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs a) {
     __shared__ float redf[16];
@@ -320,8 +331,14 @@ struct NormGradArgs {
     int32_t width, stride, parts;
 };
 
-// A workgroup owns every parts-th block of rows of one worker: threads keep
-// their columns' weights and sums of dy * xh in registers over all of them.
+// ds = dsum + rstd * (u - xh * mean(u * xh)), u = dy * w, xh = rstd * s, and this
+// part's share of dw = sum of dy * xh.  A workgroup owns every parts-th block of
+// rows of one worker: threads keep their columns' weights and sums of dy * xh
+// in registers over all of them, so dw costs no memory traffic but one row for
+// each workgroup.  Bound by memory: 16 x 2048 x 1024 bfloat16, 7 bytes of an
+// entry, 235 MB in 47 us with the sum of the parts (4.8 us of it), 5.0 TB/s.
+// From 16385 entries on a row does not fit the 128 registers that 1024 threads
+// have each, and part of it goes to scratch.
 template <typename T, int TPR, int J, bool DSUM>
 __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs a) {
     constexpr int kRows = block_of(TPR) / TPR;
@@ -518,6 +535,21 @@ struct LinearArgs {
 
 // Y[t][c] = 2^(ex[t] + ew[c]) * sum_k qx[t][k] qw[c][k]: whole numbers until
 // the one conversion (rounded to 24 bits from 2^24 on, then to the type).
+//
+// A step multiplies 128 codes of every row of the tile while the next 128 are
+// copied into the other half of LDS.  With 256 x 256 results and 8 waves of
+// 128 x 64 a step reads 192 KB of LDS and writes 64, 2048 cycles at 128 bytes,
+// for 2062 cycles of matrix instructions; reads of the second half of a step
+// are placed among the products of the first.  Measured: 16 x 2048 x 1024 ->
+// 4096 bfloat16 in 181 us, 1520 TOP/s; 4 x 8192 x 4096 -> 1024 in 125 us, 2190
+// (the library's 8192^3 product of int8: 2077).  What the shorter one lacks is
+// its 268 MB of results, written at the end of every tile with nothing to
+// compute beside: two workgroups of 4 waves of 64 x 128 on a CU, one buffer each, took 187 us,
+// 128 x 128 tiles 235, 4 waves of 128 x 128 241.
+//
+// Few tokens: tiles of 16 x 128 (4 to a CU), so that 16 workers' weights for
+// one token are spread over all CUs: 25 MB in 4.8 us, 5.2 TB/s.  In between:
+// 64 x 128 (3 to a CU).  plan_product has the rule.
 template <int BM, int BN, int WM, int WN, int QMAX>
 struct LinearTile {
     static constexpr int kThreads = 64 * WM * WN, kBytes = (BM + BN) * 128;
@@ -693,7 +725,18 @@ template <> struct Parts<float> { static constexpr int n = 3; };
 // out[m][k] = sum_r A(m, r) * q[r][k] 2^e[r][k / group], with A(m, r) = dY[m][r]
 // (dX: m tokens, r channels) or dY[r][m] (ALONG_R, dW: m channels, r tokens).
 // Both operands are brought into LDS as bfloat16 rows along r, 64 of r a step:
-// 8 x 4 blocks of codes, and of dY for dW, are turned in registers on the way.
+// 8 x 4 blocks of codes, and of dY for dW, are turned in registers on the way,
+// codes converted once for the workgroup and not by each wave that reads them.
+// The products are exact in 32 bits; sums are bfloat16 matrix instructions'
+// 32-bit ones.  dY of 16 or 32 bits goes in as 2 or 3 bfloat16 that add up to it.
+//
+// Bound by the matrix unit together with the conversions: of a step of 256 x
+// 256 (2048 cycles of matrix instructions on each SIMD) the vector unit has
+// about 1200.  16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 260
+// us, 1054 TFLOP/s; dW, which also writes 268 MB, in 304 us, 904 (the library's
+// bfloat16 product of 8192^3: 1134).  Float gradients (three products each):
+// 974 and 1212 us; binary16 (two): 531 and 691.  The tile is as large as two
+// steps of all parts fit in LDS.
 template <typename T, int QMAX, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
 struct GradTile {
     static constexpr int kThreads = 64 * WM * WN, P = Parts<T>::n, BR = 64;
@@ -937,7 +980,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
     }
 }
 
-// The sum of the parts of a split product, in ascending order: four
+// The sum of the parts of a split product, in ascending order, so that equal
+// inputs give equal bits: four
 // neighbouring entries of [n][rows][cols] for each thread, given to
 // f(worker, row, column, sum) one by one.
 template <typename V, typename F>
@@ -1205,10 +1249,12 @@ void with_type(int32_t type, F f) {
     else f((_Float16)0);
 }
 
-constexpr int64_t kMaxGrid = 1 << 20;   // workgroups; kernels over rows loop beyond
-
-unsigned row_grid(int64_t rows, int per) {
-    return (unsigned)std::min<int64_t>((rows + per - 1) / per, kMaxGrid);
+// Workgroups of a kernel over rows.  Packing and the norm loop over rows from
+// 16 a CU on (16 x 2048 x 1024 bfloat16: 49 us with 4096 workgroups, 52 with
+// one for every 4 rows; 16 x 4096 x 2048 packed by 128: 73 and 81); unpacking
+// has nothing to keep between rows and does better without (71 and 75).
+unsigned row_grid(int64_t rows, int per, int64_t most = 16 * kCus) {
+    return (unsigned)std::min<int64_t>((rows + per - 1) / per, most);
 }
 
 int chunks_layout(int64_t stride) { return stride <= 128 ? 16 : stride <= 2048 ? 64 : 256; }
@@ -1243,15 +1289,16 @@ struct Plan {
 // 65,536 and widths of 96 to 8,192; the choice took at most 1.25 times
 // the best one's time there.
 Plan plan_product(const TileCost *tile, int count, int64_t n, int64_t m, int64_t cols, int64_t steps) {
-    static const int splits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     Plan best;
     float best_us = 0.0f;
     for (int c = 0; c < count; ++c) {
         const TileCost &t = tile[c];
-        const int64_t tm = tiles(m, t.bm), tn = tiles(cols, t.bn);
-        for (const int split : splits) {
-            if (split > steps && split > 1) break;
-            const int64_t blocks = n * tm * tn * split, places = kCus * t.resident;
+        const int64_t tm = tiles(m, t.bm), tn = tiles(cols, t.bn), places = kCus * t.resident;
+        // The last one fills the chip just once.
+        const int once = (int)std::min<int64_t>(64, places / std::max<int64_t>(1, n * tm * tn));
+        for (const int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, once}) {
+            if (split < 1 || (split > steps && split > 1)) continue;
+            const int64_t blocks = n * tm * tn * split;
             const float fill = std::min(1.0f, (float)blocks / (float)places);
             const float step = t.alone_us + (t.full_us - t.alone_us) * fill;
             float us = (float)tiles(blocks, places) * (t.fixed_us + (float)tiles(steps, split) * step);
@@ -1346,7 +1393,7 @@ int relaysum_unpack(int32_t n, int64_t rows, int64_t width, const relaysum_packe
     with_type(out->type, [&](auto zero) {
         using T = decltype(zero);
         const int tpr = chunks_layout(a.stride);
-        const dim3 grid(row_grid(a.total, 256 / tpr));
+        const dim3 grid(row_grid(a.total, 256 / tpr, 1 << 20));
         const hipStream_t st = (hipStream_t)hip_stream;
         if (tpr == 16) hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<T, 16>), grid, dim3(256), 0, st, a);
         else if (tpr == 64) hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<T, 64>), grid, dim3(256), 0, st, a);
