@@ -89,11 +89,11 @@ __device__ __forceinline__ int exponent_of(unsigned maxbits) {
 // 2^-e, or 0 for a group that is not a number (every code is then 0: NaN and
 // infinity times 0 is NaN, which converts to 0).
 __device__ __forceinline__ float inverse_scale(int e) {
-    return e == kNotANumber ? 0.0f : float_of((unsigned)(127 - e) << 23);
+    return float_of(e == kNotANumber ? 0u : (unsigned)(127 - e) << 23);
 }
 
 __device__ __forceinline__ float scale_of(int e) {
-    return e == kNotANumber ? float_of(0x7fc00000u) : float_of((unsigned)(127 + e) << 23);
+    return float_of(e == kNotANumber ? 0x7fc00000u : (unsigned)(127 + e) << 23);
 }
 
 __device__ __forceinline__ u2_t codes8(const float (&v)[8], float inv) {
@@ -102,6 +102,13 @@ __device__ __forceinline__ u2_t codes8(const float (&v)[8], float inv) {
     for (int i = 0; i < 8; ++i)
         w[i / 4] |= ((unsigned)__float2int_rn(v[i] * inv) & 0xffu) << (8 * (i % 4));
     return u2_t{w[0], w[1]};
+}
+
+// Two floats as two bfloat16, the first in the lower half.
+__device__ __forceinline__ unsigned bf16_pair(float a, float b) {
+    typedef float f2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2_t{a, b}), b2_t));
 }
 
 __device__ __forceinline__ float code_at(unsigned w, int byte) {
@@ -544,8 +551,8 @@ struct LinearArgs {
 // 4096 bfloat16 in 181 us, 1520 TOP/s; 4 x 8192 x 4096 -> 1024 in 125 us, 2190
 // (the library's 8192^3 product of int8: 2077).  What the shorter one lacks is
 // its 268 MB of results, written at the end of every tile with nothing to
-// compute beside: two workgroups of 4 waves of 64 x 128 on a CU, one buffer each, took 187 us,
-// 128 x 128 tiles 235, 4 waves of 128 x 128 241.
+// compute beside: two workgroups of 4 waves of 64 x 128 on a CU, one buffer
+// each, took 187 us, 128 x 128 tiles 235, 4 waves of 128 x 128 241.
 //
 // Few tokens: tiles of 16 x 128 (4 to a CU), so that 16 workers' weights for
 // one token are spread over all CUs: 25 MB in 4.8 us, 5.2 TB/s.  In between:
@@ -706,15 +713,19 @@ struct GradArgs {
     int32_t workers;
 };
 
-// A float as a sum of P bfloat16: exactly, for the 8, 11 and 24 significant
-// bits of the three types and P = 1, 2, 3.
+// Two floats as sums of P bfloat16 each: exactly, for the 8, 11 and 24
+// significant bits of the three types and P = 1, 2, 3.
 template <int P>
-__device__ __forceinline__ void split(float v, __bf16 (&part)[P]) {
+__device__ __forceinline__ void split_pair(float a, float b, unsigned (&part)[P]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        part[p] = (__bf16)v;
-        // An infinity has no rest.
-        if (p + 1 < P) v = (bits_of((float)part[p]) & 0x7f800000u) == 0x7f800000u ? 0.0f : v - (float)part[p];
+        part[p] = bf16_pair(a, b);
+        if (p + 1 < P) {
+            // An infinity has no rest.
+            const unsigned x = part[p] << 16, y = part[p] & 0xffff0000u;
+            a = (x & 0x7f800000u) == 0x7f800000u ? 0.0f : a - float_of(x);
+            b = (y & 0x7f800000u) == 0x7f800000u ? 0.0f : b - float_of(y);
+        }
     }
 }
 
@@ -730,12 +741,13 @@ template <> struct Parts<float> { static constexpr int n = 3; };
 // The products are exact in 32 bits; sums are bfloat16 matrix instructions'
 // 32-bit ones.  dY of 16 or 32 bits goes in as 2 or 3 bfloat16 that add up to it.
 //
-// Bound by the matrix unit together with the conversions: of a step of 256 x
-// 256 (2048 cycles of matrix instructions on each SIMD) the vector unit has
-// about 1200.  16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 260
-// us, 1054 TFLOP/s; dW, which also writes 268 MB, in 304 us, 904 (the library's
+// Bound by the matrix unit together with what feeds it: of a step of 256 x 256
+// (2048 cycles of matrix instructions on each SIMD) the conversions take about
+// 900 cycles of the vector unit, and LDS is busy for as long as the matrix
+// unit.  16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 252 us,
+// 1090 TFLOP/s; dW, which also writes 268 MB, in 287 us, 960 (the library's
 // bfloat16 product of 8192^3: 1134).  Float gradients (three products each):
-// 974 and 1212 us; binary16 (two): 531 and 691.  The tile is as large as two
+// 937 and 1214 us; binary16 (two): 516 and 670.  The tile is as large as two
 // steps of all parts fit in LDS.
 template <typename T, int QMAX, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
 struct GradTile {
@@ -848,10 +860,11 @@ struct GradTile {
                 scale[y] = scale_of(GROUPED ? h.eg[i][y] : (int)(int8_t)(e[y / 4] >> (8 * (y % 4))));
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                b8_t v;
+                u4_t v;
 #pragma unroll
-                for (int y = 0; y < 8; ++y) v[y] = (__bf16)(code_at(h.q[i][y], x) * scale[y]);
-                *reinterpret_cast<b8_t *>(lds + kA + column_at(at, x)) = v;
+                for (int y = 0; y < 8; y += 2)
+                    v[y / 2] = bf16_pair(code_at(h.q[i][y], x) * scale[y], code_at(h.q[i][y + 1], x) * scale[y + 1]);
+                *reinterpret_cast<u4_t *>(lds + kA + column_at(at, x)) = v;
             }
         }
 #pragma unroll
@@ -861,17 +874,21 @@ struct GradTile {
             const int at = ALONG_R ? tile_at(u % (BM / 4) * 4, u / (BM / 4)) : tile_at(u / 8, u % 8);
 #pragma unroll
             for (int x = 0; x < (ALONG_R ? 4 : 1); ++x) {
-                b8_t v[P];
+                u4_t v[P];
 #pragma unroll
-                for (int y = 0; y < 8; ++y) {
-                    __bf16 p[P];
-                    split<P>((float)(ALONG_R ? h.at[i][y][x] : h.a[i][y]), p);
+                for (int y = 0; y < 8; y += 2) {
+                    const T a = ALONG_R ? h.at[i][y][x] : h.a[i][y], b = ALONG_R ? h.at[i][y + 1][x] : h.a[i][y + 1];
+                    unsigned p[P];
+                    if constexpr (P == 1)
+                        p[0] = __builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16;
+                    else
+                        split_pair<P>((float)a, (float)b, p);
 #pragma unroll
-                    for (int k = 0; k < P; ++k) v[k][y] = p[k];
+                    for (int k = 0; k < P; ++k) v[k][y / 2] = p[k];
                 }
 #pragma unroll
                 for (int k = 0; k < P; ++k)
-                    *reinterpret_cast<b8_t *>(lds + k * BM * 128 + column_at(at, x)) = v[k];
+                    *reinterpret_cast<u4_t *>(lds + k * BM * 128 + column_at(at, x)) = v[k];
             }
         }
     }
@@ -1260,10 +1277,11 @@ unsigned row_grid(int64_t rows, int per, int64_t most = 16 * kCus) {
 int chunks_layout(int64_t stride) { return stride <= 128 ? 16 : stride <= 2048 ? 64 : 256; }
 
 // Workgroups per worker of the norm's gradient: enough for four on each CU, no
-// more than one for 16 rows.
+// more than one for 8 rows (5 x 777 x 1001 floats 14.3 us; one for 16 rows 16.2,
+// for 4 rows 14.9).
 int norm_parts(int32_t n, int64_t rows) {
     const int64_t want = (4 * kCus + n - 1) / n;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(want, (rows + 15) / 16));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(want, (rows + 7) / 8));
 }
 
 int64_t tiles(int64_t size, int64_t tile) { return (size + tile - 1) / tile; }
