@@ -368,6 +368,51 @@ def test_weight_gradient_over_many_tokens(n, tokens, width, channels, dtype):
     assert torch.equal(again, want_)
 
 
+def in_64(packed):
+    """Held rows in 64 bits on the GPU."""
+    span = packed.codes.shape[2] // packed.exps.shape[2]
+    powers = torch.tensor([2.0 ** e for e in range(-128, 128)], dtype=torch.float64, device="cuda")
+    scale = powers[packed.exps.long() + 128].repeat_interleave(span, dim=2)
+    return (packed.codes.double() * scale)[:, :, :packed.width].contiguous()
+
+
+def random_codes(seed, n, rows, width, group=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    v = torch.randn(n, rows, width, generator=g, device="cuda")
+    v *= torch.exp2(torch.randint(-4, 5, (n, rows, 1), generator=g, device="cuda").float())
+    return layer.pack(v, group)
+
+
+@pytest.mark.parametrize("n,tokens,width,channels", [(16, 515, 1030, 1027), (12, 1030, 516, 2052), (1, 40000, 512, 512),
+                                                     (8, 1100, 770, 1288)])
+def test_large_products(n, tokens, width, channels):
+    """Sizes that fill the chip: large tiles with ragged edges on every side,
+    sums of many steps, results whose rows 4 does not divide."""
+    x, w = random_codes(1, n, tokens, width), random_codes(2, n, channels, width)
+    x64, w64 = in_64(x), in_64(w)
+    announce(f"large product {n} {tokens} {width} {channels}")
+    want = torch.matmul(x64, w64.transpose(1, 2).contiguous())
+    for dtype in TYPES:
+        assert torch.equal(layer.linear(x, w, dtype), want.float().to(dtype))
+    for dtype in TYPES:
+        announce(f"large gradients {n} {tokens} {width} {channels} {dtype}")
+        g = torch.Generator(device="cuda").manual_seed(3)
+        dy = (torch.randn(n, tokens, channels, generator=g, device="cuda") * 1e-2).to(dtype)
+        d64 = dy.double()
+        want, size = torch.matmul(d64, w64), torch.matmul(d64.abs(), w64.abs())
+        bound = 2 * (channels + 8) * ULP * size + 1.01 * ROUND[dtype] * want.abs() + TINY[dtype]
+        assert bool(((layer.linear_backward_input(dy, w).double() - want).abs() <= bound).all())
+        turned = d64.transpose(1, 2).contiguous()
+        for group in (0, 128):
+            xg = x if group == 0 else random_codes(4, n, tokens, width, 128)
+            dw, around = in_model(torch.zeros(n, channels, width, device="cuda"))
+            layer.linear_backward_weight(dy, xg, dw)
+            v64 = in_64(xg)
+            want, size = torch.matmul(turned, v64), torch.matmul(turned.abs(), v64.abs())
+            assert bool(((dw.double() - want).abs() <= 2 * (tokens + 8) * ULP * size).all())
+            assert untouched(dw, around)
+
+
 def test_gradients_without_tokens():
     """No tokens: the weight gradients are zeros, and nothing else is touched."""
     announce("gradients without tokens")
@@ -405,8 +450,12 @@ def test_gradients_pass_on_what_is_no_number(dtype):
     ones[0, 69, 39] = float("nan")
     layer.linear_backward_weight(torch.ones_like(dy), layer.pack(ones), dw)
     assert torch.isnan(dw).all()
-    layer.linear_backward_weight(torch.ones_like(dy), layer.pack(ones.repeat(1, 1, 5), 128), big := torch.zeros(n, c, 5 * k, device="cuda"))
-    assert torch.isfinite(big[0, :, 128:]).sum() == 0 or torch.isnan(big[0, :, :128]).all()
+    # By groups: a NaN in the second 128 entries of a token leaves the first.
+    wide = torch.ones(n, t, 200, device="cuda")
+    wide[0, 69, 130] = float("nan")
+    dw = torch.zeros(n, c, 200, device="cuda")
+    layer.linear_backward_weight(torch.ones_like(dy), layer.pack(wide, 128), dw)
+    assert (dw[0, :, :128] == t).all() and torch.isnan(dw[0, :, 128:]).all()
 
 
 def test_gradient_strides():
