@@ -457,7 +457,7 @@ int relaysum_unpack(int32_t n, int64_t rows, int64_t width, const relaysum_packe
  *            be NULL (s = h).  sum may be h's or residual's own rows.
  *   weight   float[width] of worker i at weight + i*weight_stride
  *   y        out, group 0: what the product reads, and its gradient keeps
- *   rstd     out, float[n][tokens]
+ *   rstd     out, float[n][tokens]; 0 where mean(s^2) passes binary32's range
  *   saved    out, group 128, or NULL: s, for relaysum_rmsnorm_backward */
 int relaysum_rmsnorm(int32_t n, int64_t tokens, int64_t width, const relaysum_rows *h,
                      const relaysum_rows *residual, const float *weight, int64_t weight_stride,
@@ -491,7 +491,9 @@ int relaysum_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                     const relaysum_packed *x, const relaysum_packed *w, const relaysum_rows *y,
                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* dx[t][k] = sum_c dy[t][c] * w[c][k]; dx has dy's type, w is group 0. */
+/* dx[t][k] = sum_c dy[t][c] * w[c][k]; dx has dy's type, w is group 0.  Here
+ * and below dy's entries enter exactly, floats to a multiple of 2^-133 (and as
+ * infinities from 2^128 * (1 - 2^-9) on). */
 int relaysum_linear_backward_input(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                                    const relaysum_rows *dy, const relaysum_packed *w,
                                    const relaysum_rows *dx, void *workspace, size_t workspace_bytes,

@@ -714,7 +714,10 @@ struct GradArgs {
 };
 
 // Two floats as sums of P bfloat16 each: exactly, for the 8, 11 and 24
-// significant bits of the three types and P = 1, 2, 3.
+// significant bits of the three types and P = 1, 2, 3, as long as the last part
+// is not below the smallest bfloat16, 2^-133, to whose multiples floats are
+// rounded (a float of 1e-34 keeps 22 bits); floats that round to 2^128 in
+// bfloat16, the last 2^-9 of their range, count as infinite.
 template <int P>
 __device__ __forceinline__ void split_pair(float a, float b, unsigned (&part)[P]) {
 #pragma unroll

@@ -46,24 +46,24 @@ class Packed:
     __slots__ = ("_codes", "_exps", "_buffer", "_n", "_rows", "_groups", "_device", "width")
 
     def __init__(self, codes, exps, width: int):
-        width = int(width)
         stride = packed_stride(width)
-        for t, name in ((codes, "codes"), (exps, "exps")):
-            if not isinstance(t, torch.Tensor) or not t.is_cuda:
-                raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-            if t.dtype != torch.int8 or t.dim() != 3 or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous int8 tensor of three axes")
-        n, rows, held = codes.shape
+        if not (isinstance(codes, torch.Tensor) and codes.is_cuda and isinstance(exps, torch.Tensor)
+                and exps.is_cuda):
+            raise TypeError("codes and exps must be CUDA (HIP) tensors")
+        if codes.dtype != torch.int8 or exps.dtype != torch.int8 or codes.dim() != 3 or \
+                not codes.is_contiguous() or not exps.is_contiguous():
+            raise ValueError("codes and exps must be contiguous int8 tensors of three axes")
+        n, rows, held = shape = codes.shape
         if held != stride:
             raise ValueError(f"rows of {width} entries have codes of stride {stride}, not {held}")
-        groups = exps.shape[2]
-        if exps.shape[0] != n or exps.shape[1] != rows or groups not in (1, stride // GROUP):
+        groups = exps.shape[-1] if exps.dim() == 3 else 0
+        if exps.shape[:-1] != shape[:-1] or (groups != 1 and groups != stride // GROUP):
             raise ValueError(f"exps must have shape [{n}, {rows}, 1 or {stride // GROUP}]")
-        if codes.get_device() != exps.get_device():
+        self._device = codes.get_device()
+        if exps.get_device() != self._device:
             raise ValueError("codes and exps must be on one device")
         self._codes, self._exps, self._buffer = codes, exps, None
-        self._n, self._rows, self._groups, self._device = n, rows, groups, codes.get_device()
-        self.width = width
+        self._n, self._rows, self._groups, self.width = n, rows, groups, width
 
     @classmethod
     def _new(cls, n: int, rows: int, width: int, group: int, like):
@@ -163,20 +163,26 @@ def _check(rc: int, what: str) -> None:
 def _rows(t, name: str, shape, device: int, dtype=None) -> Rows:
     """The description of a tensor [n, rows, width] (or [n, width]: one row
     for each worker) whose last axis is dense."""
+    if isinstance(t, torch.Tensor) and t.get_device() == device and t.shape == shape:
+        code = TYPES.get(t.dtype)
+        if code is not None and (dtype is None or t.dtype == dtype):
+            st = t.stride()
+            if st[-1] == 1 or shape[-1] <= 1 or not t.numel():
+                return Rows(t.data_ptr(), code, st[0], st[1] if len(st) == 3 else 0)
+    _refuse(t, name, shape, device, dtype)
+
+
+def _refuse(t, name: str, shape, device: int, dtype) -> None:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.get_device() != device:
         raise ValueError(f"{name} must be on the current device")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
-    code = TYPES.get(t.dtype)
-    if code is None or (dtype is not None and t.dtype != dtype):
+    if t.dtype not in TYPES or (dtype is not None and t.dtype != dtype):
         want = dtype if dtype is not None else "float32, bfloat16 or float16"
         raise ValueError(f"{name} must be {want}, not {t.dtype}")
-    st = t.stride()
-    if st[-1] != 1 and t.shape[-1] > 1 and t.numel():
-        raise ValueError(f"{name}: the last axis must be dense")
-    return Rows(t.data_ptr(), code, st[0], st[1] if len(st) == 3 else 0)
+    raise ValueError(f"{name}: the last axis must be dense")
 
 
 def _three(t, name: str):
