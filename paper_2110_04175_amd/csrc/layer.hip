@@ -842,6 +842,23 @@ struct GradTile {
         }
     }
 
+    // Chunks of dY that the result's edge would cut were loaded from up to 3
+    // columns before (load<true>): moves their entries to their places.
+    static __device__ __forceinline__ void align_edge(const GradArgs &g, int64_t m0, Held &h) {
+#pragma unroll
+        for (int i = 0; i < (ALONG_R ? UA : 0); ++i) {
+            const int64_t before = m0 + (i * kThreads + threadIdx.x) % (BM / 4) * 4 - (g.m - 4);
+            const int by = (int)max((int64_t)0, min(before, (int64_t)3));
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const t4_t v = h.at[i][y];
+#pragma unroll
+                for (int x = 0; x < 3; ++x)
+                    h.at[i][y][x] = by == 0 ? v[x] : by == 1 ? v[x + 1] : by == 2 && x < 2 ? v[x + 2 & 3] : v[3];
+            }
+        }
+    }
+
     static __device__ __forceinline__ void store(const Held &h, char *lds) {
 #pragma unroll
         for (int i = 0; i < UB; ++i) {
@@ -950,8 +967,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
     if (s0 < s1) {
         typename G::Held h;
         // Steps that are loaded in whole chunks: not the one that the axis ends
-        // in, and none where the result's edge cuts a chunk of dY.
-        const int64_t whole = ALONG_R && a.m % 4 && m0 + BM > a.m ? 0 : a.r / G::BR;
+        // in, and none of a result with fewer rows than a chunk.
+        const int64_t whole = ALONG_R && a.m < 4 ? 0 : a.r / G::BR;
+        const bool edge = ALONG_R && a.m % 4 && m0 + BM > a.m;
         auto load = [&](int64_t s) {
             if (s < whole) G::template load<true>(a, worker, m0, n0, s * G::BR, h);
             else G::template load<false>(a, worker, m0, n0, s * G::BR, h);
@@ -960,26 +978,30 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void grad_kernel(GradArgs a) {
         // s + 1 into LDS, the other the other way round, so that one's vector
         // instructions run beside the other's matrix instructions.
         const bool late = WM * WN == 8 && wave >= 4;
+        auto store = [&](int64_t s, char *to) {
+            if (edge && s < whole) G::align_edge(a, m0, h);
+            G::store(h, to);
+        };
         int cur = 0;
         load(s0);
-        G::store(h, lds);
+        store(s0, lds);
         if (late && s0 + 1 < s1) load(s0 + 1);
         __syncthreads();
         int64_t s = s0;
         for (; s + 2 < min(s1, whole); ++s) {
-            if (late) G::store(h, lds + (cur ^ G::kBytes));
+            if (late) store(s + 1, lds + (cur ^ G::kBytes));
             G::template load<true>(a, worker, m0, n0, (s + 1 + late) * G::BR, h);
             G::multiply(lds + cur, aat, bat, acc);
             cur ^= G::kBytes;
-            if (!late) G::store(h, lds + cur);
+            if (!late) store(s + 1, lds + cur);
             __syncthreads();
         }
         for (; s < s1; ++s) {
-            if (late && s + 1 < s1) G::store(h, lds + (cur ^ G::kBytes));
+            if (late && s + 1 < s1) store(s + 1, lds + (cur ^ G::kBytes));
             if (s + 1 + late < s1) load(s + 1 + late);
             G::multiply(lds + cur, aat, bat, acc);
             cur ^= G::kBytes;
-            if (!late && s + 1 < s1) G::store(h, lds + cur);
+            if (!late && s + 1 < s1) store(s + 1, lds + cur);
             __syncthreads();
         }
     }
