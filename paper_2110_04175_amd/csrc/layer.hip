@@ -545,9 +545,9 @@ struct LinearArgs {
 //
 // A step multiplies 128 codes of every row of the tile while the next 128 are
 // copied into the other half of LDS.  With 256 x 256 results and 8 waves of
-// 128 x 64 a step reads 192 KB of LDS and writes 64, 2048 cycles at 128 bytes,
-// for 2062 cycles of matrix instructions; reads of the second half of a step
-// are placed among the products of the first.  Measured: 16 x 2048 x 1024 ->
+// 128 x 64 a step reads 192 KB of LDS, 768 cycles of it by the counters, and
+// copies 64 KB in, for 2048 cycles of matrix instructions; reads of the second
+// half of a step are placed among the products of the first.  Measured: 16 x 2048 x 1024 ->
 // 4096 bfloat16 in 181 us, 1520 TOP/s; 4 x 8192 x 4096 -> 1024 in 125 us, 2190
 // (the library's 8192^3 product of int8: 2077).  What the shorter one lacks is
 // its 268 MB of results, written at the end of every tile with nothing to
@@ -745,9 +745,9 @@ template <> struct Parts<float> { static constexpr int n = 3; };
 // 32-bit ones.  dY of 16 or 32 bits goes in as 2 or 3 bfloat16 that add up to it.
 //
 // Bound by the matrix unit together with what feeds it: of a step of 256 x 256
-// (2048 cycles of matrix instructions on each SIMD) the conversions take about
-// 900 cycles of the vector unit, and LDS is busy for as long as the matrix
-// unit.  16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 252 us,
+// (2048 cycles of matrix instructions on each SIMD) the conversions and
+// addresses take about 900 cycles of the vector unit, and LDS is busy for 1280.
+// 16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 252 us,
 // 1090 TFLOP/s; dW, which also writes 268 MB, in 287 us, 960 (the library's
 // bfloat16 product of 8192^3: 1134).  Float gradients (three products each):
 // 937 and 1214 us; binary16 (two): 516 and 670.  The tile is as large as two
