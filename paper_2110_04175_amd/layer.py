@@ -12,6 +12,7 @@ the tensor given for them.  Work is queued on torch's current stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -208,6 +209,17 @@ def _workspace(nbytes: int, device):
     return t.data_ptr(), nbytes, t
 
 
+# A workspace's size follows from the call's sizes alone.
+@functools.lru_cache(maxsize=1024)
+def _linear_workspace(n: int, tokens: int, width: int, channels: int, code: int) -> int:
+    return _lib().relaysum_linear_workspace(n, tokens, width, channels, code)
+
+
+@functools.lru_cache(maxsize=1024)
+def _rmsnorm_workspace(n: int, tokens: int, width: int) -> int:
+    return _lib().relaysum_rmsnorm_workspace(n, tokens, width)
+
+
 def _here():
     """The current device and the address of its current stream."""
     device = torch.cuda.current_device()
@@ -279,7 +291,7 @@ def rmsnorm_backward(dy, dsum, saved: Packed, rstd, weight, weight_grad):
         raise ValueError("rstd must be contiguous")
     ds, rs = _out(n, tokens, width, dy.dtype, device)
     lib = _lib()
-    ws, size, _keep = _workspace(lib.relaysum_rmsnorm_workspace(n, tokens, width), device)
+    ws, size, _keep = _workspace(_rmsnorm_workspace(n, tokens, width), device)
     _check(lib.relaysum_rmsnorm_backward(n, tokens, width, rdy, rd, saved._c(device, "saved"),
                                          rstd.data_ptr(), rw.data, rw.worker_stride, rs, rg, ws,
                                          size, stream), "relaysum_rmsnorm_backward")
@@ -299,8 +311,7 @@ def linear(x: Packed, w: Packed, dtype=torch.bfloat16):
     cx, cw = x._c(device, "x"), w._c(device, "w")
     y, ry = _out(n, tokens, channels, dtype, device)
     lib = _lib()
-    ws, size, _keep = _workspace(
-        lib.relaysum_linear_workspace(n, tokens, width, channels, ry.type), device)
+    ws, size, _keep = _workspace(_linear_workspace(n, tokens, width, channels, ry.type), device)
     _check(lib.relaysum_linear(n, tokens, width, channels, cx, cw, ry, ws, size, stream),
            "relaysum_linear")
     return y
@@ -316,8 +327,7 @@ def linear_backward_input(dy, w: Packed):
     rdy, cw = _rows(dy, "dy", shape, device), w._c(device, "w")
     dx, rdx = _out(n, tokens, width, dy.dtype, device)
     lib = _lib()
-    ws, size, _keep = _workspace(
-        lib.relaysum_linear_workspace(n, tokens, width, channels, rdy.type), device)
+    ws, size, _keep = _workspace(_linear_workspace(n, tokens, width, channels, rdy.type), device)
     _check(lib.relaysum_linear_backward_input(n, tokens, width, channels, rdy, cw, rdx, ws, size,
                                               stream), "relaysum_linear_backward_input")
     return dx
@@ -334,7 +344,6 @@ def linear_backward_weight(dy, x: Packed, weight_grad) -> None:
     rdy, cx = _rows(dy, "dy", shape, device), x._c(device, "x")
     rg = _rows(weight_grad, "weight_grad", (n, channels, width), device, torch.float32)
     lib = _lib()
-    ws, size, _keep = _workspace(
-        lib.relaysum_linear_workspace(n, tokens, width, channels, rdy.type), device)
+    ws, size, _keep = _workspace(_linear_workspace(n, tokens, width, channels, rdy.type), device)
     _check(lib.relaysum_linear_backward_weight(n, tokens, width, channels, rdy, cx, rg, ws, size,
                                                stream), "relaysum_linear_backward_weight")
