@@ -457,7 +457,9 @@ int relaysum_unpack(int32_t n, int64_t rows, int64_t width, const relaysum_packe
  *            be NULL (s = h).  sum may be h's or residual's own rows.
  *   weight   float[width] of worker i at weight + i*weight_stride
  *   y        out, group 0: what the product reads, and its gradient keeps
- *   rstd     out, float[n][tokens]; 0 where mean(s^2) passes binary32's range
+ *   rstd     out, float[n][tokens], also of rows whose mean(s^2) lies outside
+ *            binary32's range; infinity where rstd itself does (rows of less than
+ *            2^-128 with eps = 0; their y is right)
  *   saved    out, group 128, or NULL: s, for relaysum_rmsnorm_backward */
 int relaysum_rmsnorm(int32_t n, int64_t tokens, int64_t width, const relaysum_rows *h,
                      const relaysum_rows *residual, const float *weight, int64_t weight_stride,

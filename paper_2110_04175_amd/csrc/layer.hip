@@ -274,6 +274,33 @@ struct NormArgs {
     float eps;
 };
 
+// 1 / sqrt(mean(s^2) + eps) of a row whose squares, or their sum, may lie
+// outside binary32's range: s is scaled by the power of two that brings the
+// row's largest entry, or the root of eps if that is larger, to 1 or 2.  Leaves
+// the scaled row in s and returns what it is to be multiplied by; rstd is that
+// of the row as it was, an infinity where it passes the range (rows of numbers
+// below 2^-128).  Rows of zeros, and those with a NaN or an infinity, stay.
+// Every thread of the row takes part.
+template <int TPR, int J>
+__device__ __forceinline__ float scaled_rstd(float (&s)[J][8], float width, float eps, float &rstd,
+                                             float *redf, unsigned *redu) {
+    const unsigned most = row_reduce<TPR, unsigned, pick_max>(max_bits(s), redu);
+    if (most == 0 || most >= 0x7f800000u) return rstd;
+    const int p = max(ilogbf(float_of(most)), ilogbf(eps) >> 1);
+    float sq = 0.0f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[j][i] = ldexpf(s[j][i], -p);
+            sq = fmaf(s[j][i], s[j][i], sq);
+        }
+    sq = row_reduce<TPR, float, pick_sum>(sq, redf);
+    const float inv = 1.0f / sqrtf(sq / width + ldexpf(eps, -2 * p));
+    rstd = ldexpf(inv, -p);
+    return inv;
+}
+
 // s = h + r, rounded to the rows' type because that is what the stream goes on
 // with; y = s * rstd * w is not rounded before it is packed.  One pass: the row
 // stays in registers between the sum of squares and the codes.  Bound by
@@ -313,16 +340,20 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs a) {
             }
         }
         sq = row_reduce<TPR, float, pick_sum>(sq, redf);
-        const float rstd = 1.0f / sqrtf(sq / (float)a.width + a.eps);
-        if (lane == 0) a.rstd[row] = rstd;
+        const float mean = sq / (float)a.width + a.eps;
+        float rstd = 1.0f / sqrtf(mean), inv = rstd;
         if (KEEP) write_grouped<TPR, J>(a.saved, row, a.stride, lane, s);
+        // Squares that were lost below 2^-149 are less than 2^-50 of 2^-100.
+        if (!(mean >= 0x1p-100f && mean < INFINITY))
+            inv = scaled_rstd<TPR, J>(s, (float)a.width, a.eps, rstd, redf, redu);
+        if (lane == 0) a.rstd[row] = rstd;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int at = (lane + j * TPR) * 8;
             float wv[8];
             load8(w + at, a.width - at, wv);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[j][i] = s[j][i] * rstd * wv[i];
+            for (int i = 0; i < 8; ++i) s[j][i] = s[j][i] * inv * wv[i];
         }
         write_whole<TPR, J>(a.y, row, a.stride, lane, s, redu);
     }
