@@ -494,8 +494,7 @@ int relaysum_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* dx[t][k] = sum_c dy[t][c] * w[c][k]; dx has dy's type, w is group 0.  Here
- * and below dy's entries enter exactly, floats to a multiple of 2^-133 (and as
- * infinities from 2^128 * (1 - 2^-9) on). */
+ * and below dy's entries enter exactly, floats to a multiple of 2^-133. */
 int relaysum_linear_backward_input(int32_t n, int64_t tokens, int64_t width, int64_t channels,
                                    const relaysum_rows *dy, const relaysum_packed *w,
                                    const relaysum_rows *dx, void *workspace, size_t workspace_bytes,

@@ -747,20 +747,20 @@ struct GradArgs {
 // Two floats as sums of P bfloat16 each: exactly, for the 8, 11 and 24
 // significant bits of the three types and P = 1, 2, 3, as long as the last part
 // is not below the smallest bfloat16, 2^-133, to whose multiples floats are
-// rounded (a float of 1e-34 keeps 22 bits); floats that round to 2^128 in
-// bfloat16, the last 2^-9 of their range, count as infinite.
+// rounded (a float of 1e-34 keeps 22 bits).  All parts but the last are cut and
+// not rounded: a rounded one would pass the largest bfloat16 for floats in the
+// last 2^-9 of their range.  8 bits a part are enough that way too.
 template <int P>
 __device__ __forceinline__ void split_pair(float a, float b, unsigned (&part)[P]) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        part[p] = bf16_pair(a, b);
-        if (p + 1 < P) {
-            // An infinity has no rest.
-            const unsigned x = part[p] << 16, y = part[p] & 0xffff0000u;
-            a = (x & 0x7f800000u) == 0x7f800000u ? 0.0f : a - float_of(x);
-            b = (y & 0x7f800000u) == 0x7f800000u ? 0.0f : b - float_of(y);
-        }
+    for (int p = 0; p + 1 < P; ++p) {
+        const unsigned x = bits_of(a) & 0xffff0000u, y = bits_of(b) & 0xffff0000u;
+        part[p] = x >> 16 | y;
+        // An infinity has no rest; a NaN that was cut to an infinity has a NaN.
+        a = (bits_of(a) & 0x7fffffffu) == 0x7f800000u ? 0.0f : a - float_of(x);
+        b = (bits_of(b) & 0x7fffffffu) == 0x7f800000u ? 0.0f : b - float_of(y);
     }
+    part[P - 1] = bf16_pair(a, b);
 }
 
 template <typename T> struct Parts { static constexpr int n = 1; };

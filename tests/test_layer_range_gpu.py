@@ -86,3 +86,85 @@ def test_norm_gradient_of_a_large_row():
     size = host(rstd)[:, :, None] * (u + xh * np.mean(u * xh, axis=2, keepdims=True))
     assert (np.abs(host(ds) - want) <= 70 * ULP * size + TINY[torch.float32]).all()
     assert (np.abs(host(dw) - want_dw) <= (t + 8) * ULP * np.sum(u * xh, axis=1)).all()
+
+
+# ---- the products' gradients: dY at both ends of its type's range -----------------
+
+
+def check_gradients(dy, w, x):
+    """dX and dW of the packed w and x, within the bound of their additions,
+    and of what floats lose below 2^-133."""
+    a, lost = host(dy), 2.0 ** -134 if dy.dtype == torch.float32 else 0.0
+    channels, tokens = dy.shape[2], dy.shape[1]
+    dx = layer.linear_backward_input(dy, w)
+    b = held(w)
+    want, size = np.matmul(a, b), np.matmul(np.abs(a), np.abs(b))
+    bound = 2 * (channels + 8) * ULP * size + 1.01 * ROUND[dy.dtype] * np.abs(want) + TINY[dy.dtype]
+    bound = bound + lost * np.sum(np.abs(b), axis=1, keepdims=True)
+    assert (np.abs(host(dx) - want) <= bound).all()
+    dw, _ = in_model(torch.zeros(dy.shape[0], channels, x.width, device="cuda"))
+    layer.linear_backward_weight(dy, x, dw)
+    a, b = a.transpose(0, 2, 1), held(x)
+    want, size = np.matmul(a, b), np.matmul(np.abs(a), np.abs(b))
+    bound = 2 * (tokens + 8) * ULP * size + TINY[torch.float32] + lost * np.sum(np.abs(b), axis=1, keepdims=True)
+    assert (np.abs(host(dw) - want) <= bound).all()
+
+
+def uniform(seed, *shape):
+    g = np.random.default_rng(seed).uniform(-1, 1, shape)
+    return torch.from_numpy(g.astype(np.float32)).cuda()
+
+
+@pytest.mark.parametrize("factor", [1e-34, 1e-37, 1e-39, 1e-41])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_small_entries(dtype, factor):
+    """Entries below the smallest normal number among them; the products of
+    every multiple of 2^-133 with the rows' values are whole multiples of the
+    smallest float."""
+    announce(f"gradients of entries of {factor} {dtype}")
+    n, t, k, c = 2, 70, 130, 90
+    w, x = layer.pack(normal(1, n, c, k)), layer.pack(normal(2, n, t, k), 128)
+    dy = (uniform(3, n, t, c).double() * factor).to(dtype)
+    # 1e-41 lies below half of the smallest bfloat16: all of it rounds to 0.
+    assert bool((dy != 0).any()) == (dtype == torch.float32 or factor > 1e-40)
+    check_gradients(dy, w, x)
+
+
+def test_gradients_of_the_smallest_halves():
+    announce("gradients of the smallest binary16")
+    n, t, k, c = 2, 70, 130, 90
+    w, x = layer.pack(normal(1, n, c, k)), layer.pack(normal(2, n, t, k), 128)
+    check_gradients((uniform(3, n, t, c) * 1e-6).half(), w, x)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_gradients_of_the_largest_entries(dtype):
+    """Finite entries up to the type's largest number: small values take them
+    back into the range, and zeros (a channel, a token, single entries) give
+    zeros of them."""
+    announce(f"gradients of the largest {dtype}")
+    n, t, k, c = 2, 70, 130, 90
+    top = torch.finfo(dtype).max
+    wv, xv = normal(1, n, c, k, std=2.0 ** -20), normal(2, n, t, k, std=2.0 ** -20)
+    wv[:, 5] = 0
+    xv[:, 7] = 0
+    wv[:, :, 100:] = 0
+    xv[:, :, 100:] = 0
+    dy = (uniform(3, n, t, c).double() * top).to(dtype)
+    dy[0, 2:9, 1:40] = top
+    dy[1, :, 5] = -top
+    dy[:, 7] = top
+    assert bool(torch.isfinite(dy).all())
+    for group in (0, 128):
+        check_gradients(dy, layer.pack(wv), layer.pack(xv, group))
+    dx = layer.linear_backward_input(dy, layer.pack(wv))
+    assert bool((dx[:, :, 100:] == 0).all())
+
+
+def test_what_is_no_number_in_a_floats_last_bits():
+    """NaN whose payload lies in the lower half of its bits."""
+    announce("NaN in the last bits")
+    dy = torch.ones(1, 40, 24, device="cuda")
+    dy.view(torch.int32)[0, 3, 4] = 0x7f800001
+    dx = layer.linear_backward_input(dy, layer.pack(torch.ones(1, 24, 40, device="cuda")))
+    assert bool(torch.isnan(dx[0, 3]).all()) and bool((dx[0, 4:] == 24).all())
