@@ -1140,14 +1140,35 @@ int64_t code_stride(int64_t width) { return (width + kGroup - 1) / kGroup * kGro
 
 size_t type_bytes(int32_t type) { return type == RELAYSUM_FLOAT ? 4 : 2; }
 
-// One array of a call: where it lies, for the checks that follow.
+// One array of a call: where it lies, for the checks that follow.  Row t of
+// worker i is the `row` bytes at p + i * ws + t * rs; a dense array is one row.
 struct Span {
     const char *name;
     const char *p;
-    size_t bytes;
+    size_t bytes;     // from the first row's start to the last one's end
     bool out;
-    int64_t ws, rs;   // strides of typed rows; -1 for other arrays
+    bool typed;       // rows of a type, which a call may allow to be written in place
+    int64_t row, ws, rs, n, rows;
+
+    // The bytes that rows reach over when all of them are moved by multiples of
+    // m to where the first lies.
+    int64_t reach(int64_t m) const {
+        return row + (ws % m ? (n - 1) * ws : 0) + (rs % m ? (rows - 1) * rs : 0);
+    }
 };
+
+// Whether no byte is in both: one array ends before the other starts, or both
+// keep to their own part of every stretch of m bytes, m a stride of either
+// (models and gradients as halves of one tensor, say).
+bool apart(const Span &a, const Span &b) {
+    if (a.p >= b.p + b.bytes || b.p >= a.p + a.bytes) return true;
+    for (const int64_t m : {a.ws, a.rs, b.ws, b.rs}) {
+        if (m <= 0) continue;
+        const int64_t from = (int64_t)(b.p - a.p) % m, start = from < 0 ? from + m : from;
+        if (start >= a.reach(m) && start + b.reach(m) <= m) return true;
+    }
+    return false;
+}
 
 // Collects a call's arrays and says what is wrong with them.
 struct Call {
@@ -1193,15 +1214,28 @@ struct Call {
         span("workspace", workspace, plan.workspace, 16, true);
     }
 
-    void span(const char *name, const void *p, size_t bytes, size_t align, bool out,
-              int64_t ws = -1, int64_t rs = -1) {
-        if (code != RELAYSUM_OK || !bytes) return;
-        if (!p)
-            fail(refuse("%s must not be NULL", name));
-        else if ((uintptr_t)p % align)
-            fail(refuse("%s must be %d-byte aligned", name, (int)align));
+    void span(const char *name, const void *p, size_t bytes, size_t align, bool out) {
+        add(Span{name, static_cast<const char *>(p), bytes, out, false, (int64_t)bytes, 0, 0, 1, 1}, align);
+    }
+
+    void add(const Span &s, size_t align) {
+        if (code != RELAYSUM_OK || !s.bytes) return;
+        if (!s.p)
+            fail(refuse("%s must not be NULL", s.name));
+        else if ((uintptr_t)s.p % align)
+            fail(refuse("%s must be %d-byte aligned", s.name, (int)align));
         else
-            spans[count++] = Span{name, static_cast<const char *>(p), bytes, out, ws, rs};
+            spans[count++] = s;
+    }
+
+    // The norm's weights: a row of floats for each worker.
+    void weights(const float *w, int32_t n, int64_t stride, int64_t width) {
+        if (code != RELAYSUM_OK) return;
+        if (n == 1) stride = 0;
+        if (stride < 0 || stride > ((int64_t)1 << 44) / n)
+            return fail(refuse("weight_stride is negative or reaches past 2^44 entries"));
+        const size_t entries = (size_t)((n - 1) * stride + width);
+        add(Span{"weight", reinterpret_cast<const char *>(w), entries * 4, false, false, width * 4, stride * 4, 0, n, 1}, 4);
     }
 
     void rows(const char *name, const relaysum_rows *r, int32_t n, int64_t rows, int64_t width,
@@ -1221,7 +1255,9 @@ struct Call {
         const bool across = (n == 1 || ws >= width) && (rows == 1 || rs >= (n - 1) * ws + width);
         if (out && !within && !across) return fail(refuse("%s: its rows overlap", name));
         const size_t entries = (size_t)((n - 1) * ws + (rows - 1) * rs + width);
-        span(name, r->data, entries * type_bytes(r->type), type_bytes(r->type), out, ws, rs);
+        const int64_t b = (int64_t)type_bytes(r->type);
+        add(Span{name, static_cast<const char *>(r->data), entries * b, out, true, width * b, ws * b, rs * b, n, rows},
+            type_bytes(r->type));
     }
 
     void packed(const char *name, const relaysum_packed *p, int32_t n, int64_t rows, int64_t width,
@@ -1241,8 +1277,8 @@ struct Call {
         for (int i = 0; i < count; ++i)
             for (int j = 0; j < i; ++j) {
                 const Span &a = spans[i], &b = spans[j];
-                if (!(a.out || b.out) || a.p >= b.p + b.bytes || b.p >= a.p + a.bytes) continue;
-                if (in_place && a.out != b.out && a.p == b.p && a.bytes == b.bytes && a.ws >= 0 &&
+                if (!(a.out || b.out) || apart(a, b)) continue;
+                if (in_place && a.out != b.out && a.p == b.p && a.bytes == b.bytes && a.typed && b.typed &&
                     a.ws == b.ws && a.rs == b.rs)
                     continue;
                 fail(refuse("%s and %s share memory", b.name, a.name));
@@ -1492,10 +1528,7 @@ int relaysum_rmsnorm(int32_t n, int64_t tokens, int64_t width, const relaysum_ro
             c.rows("residual", residual, n, tokens, width, false);
             c.rows("sum", sum, n, tokens, width, true);
         }
-        if (c.code == RELAYSUM_OK && n > 1 && (weight_stride < 0 || weight_stride > ((int64_t)1 << 44) / n))
-            c.fail(refuse("weight_stride is negative or reaches past 2^44 entries"));
-        const int64_t wspan = (n > 1 ? (n - 1) * weight_stride : 0) + width;
-        c.span("weight", weight, c.code == RELAYSUM_OK ? (size_t)wspan * 4 : 0, 4, false);
+        c.weights(weight, n, weight_stride, width);
         if (y && !whole_rows(y, width)) c.fail(refuse("y is packed by whole rows (group 0)"));
         c.packed("y", y, n, tokens, width, true);
         c.span("rstd", rstd, (size_t)n * tokens * 4, 4, true);
@@ -1551,10 +1584,7 @@ int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const re
         if (dsum) c.rows("dsum", dsum, n, tokens, width, false);
         c.packed("saved", saved, n, tokens, width, false);
         c.span("rstd", rstd, (size_t)n * tokens * 4, 4, false);
-        if (c.code == RELAYSUM_OK && n > 1 && (weight_stride < 0 || weight_stride > ((int64_t)1 << 44) / n))
-            c.fail(refuse("weight_stride is negative or reaches past 2^44 entries"));
-        const int64_t wspan = (n > 1 ? (n - 1) * weight_stride : 0) + width;
-        c.span("weight", weight, c.code == RELAYSUM_OK ? (size_t)wspan * 4 : 0, 4, false);
+        c.weights(weight, n, weight_stride, width);
         c.rows("ds", ds, n, tokens, width, true);
         c.rows("weight_grad", weight_grad, n, 1, width, true);
         if (weight_grad && weight_grad->type != RELAYSUM_FLOAT)
