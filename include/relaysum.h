@@ -415,7 +415,10 @@ const char *relaysum_last_error(const relaysum_t *h);
  *
  * Limits: 1 <= n <= RELAYSUM_MAX_WORKERS, 0 <= rows or tokens (0: nothing to
  * do, but weight gradients are set to 0), 1 <= width <= 32768 (up to there
- * an integer sum of products fits 32 bits), 1 <= channels <= 2^24. */
+ * an integer sum of products fits 32 bits), 1 <= channels <= 2^24.  A launch
+ * takes 2^22 - 1 workgroups: n of the norm's gradient, and of the products n
+ * times the tiles of a worker's result (256 x 256; of gradients from floats
+ * 128 x 128, from binary16 128 x 256). */
 
 typedef enum relaysum_type {
     RELAYSUM_FLOAT = 0,    /* binary32 */
