@@ -29,7 +29,8 @@ FLAGS = [
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    """Compile the library (always recompiles) and return its path."""
+    """Compile the library (always recompiles) and return its path.  `extra`
+    goes to every compilation and to the link."""
     tmp = LIB + ".tmp"
     # One process for each source, side by side; then the link.
     objects = [os.path.splitext(src)[0] + ".o" for src in SOURCES]
@@ -44,7 +45,7 @@ def build(verbose: bool = False, extra=()) -> str:
             for _, other in running:
                 other.wait()
             raise subprocess.CalledProcessError(p.returncode, cmd)
-    cmd = [HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects]
+    cmd = [HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects, *extra]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True, cwd=PKG)
