@@ -484,9 +484,19 @@ int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const re
                               const relaysum_rows *ds, const relaysum_rows *weight_grad,
                               void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* Bytes that the three calls below may need as workspace, 16-byte aligned,
+typedef enum relaysum_product {
+    RELAYSUM_LINEAR = 0,                   /* relaysum_linear */
+    RELAYSUM_LINEAR_BACKWARD_INPUT = 1,
+    RELAYSUM_LINEAR_BACKWARD_WEIGHT = 2
+} relaysum_product;
+
+/* Bytes that a call (relaysum_product) needs as workspace, 16-byte aligned,
  * for rows of this type (y's, or dy's); 0: none, and NULL will do.  Few
- * results with a long sum are made in parts, which are kept there. */
+ * results with a long sum are made in parts, which are kept there.
+ * relaysum_linear_workspace is the most of the three, for callers that keep
+ * one workspace for all of them.  -1 for bad arguments. */
+int64_t relaysum_linear_workspace_of(int32_t product, int32_t n, int64_t tokens, int64_t width,
+                                     int64_t channels, int32_t type);
 int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels, int32_t type);
 
 /* y[t][c] = sum_k x[t][k] * w[c][k] for every worker: x packed rows of tokens,

@@ -47,7 +47,7 @@ EXPORTED = (
     # Layers on 8-bit rows, bound in layer.py.
     "relaysum_packed_stride", "relaysum_pack", "relaysum_unpack", "relaysum_rmsnorm",
     "relaysum_rmsnorm_workspace", "relaysum_rmsnorm_backward", "relaysum_linear",
-    "relaysum_linear_workspace", "relaysum_linear_backward_input",
+    "relaysum_linear_workspace_of", "relaysum_linear_workspace", "relaysum_linear_backward_input",
     "relaysum_linear_backward_weight", "relaysum_layer_error",
 )
 

@@ -1561,16 +1561,29 @@ int relaysum_rmsnorm_backward(int32_t n, int64_t tokens, int64_t width, const re
     return done("relaysum_rmsnorm_backward");
 }
 
-int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels, int32_t type) {
+int64_t relaysum_linear_workspace_of(int32_t product, int32_t n, int64_t tokens, int64_t width,
+                                     int64_t channels, int32_t type) {
     Call c;
     if (!c.product(n, tokens, width, channels)) return -1;
     if (type < RELAYSUM_FLOAT || type > RELAYSUM_HALF) {
         refuse("unknown type %d", type);
         return -1;
     }
-    return (int64_t)std::max({plan_linear(n, tokens, width, channels).workspace,
-                              plan_grad(type, n, tokens, width, channels).workspace,
-                              plan_grad(type, n, channels, width, tokens).workspace});
+    g_error[0] = '\0';
+    switch (product) {
+    case RELAYSUM_LINEAR: return (int64_t)plan_linear(n, tokens, width, channels).workspace;
+    case RELAYSUM_LINEAR_BACKWARD_INPUT: return (int64_t)plan_grad(type, n, tokens, width, channels).workspace;
+    case RELAYSUM_LINEAR_BACKWARD_WEIGHT: return (int64_t)plan_grad(type, n, channels, width, tokens).workspace;
+    }
+    refuse("unknown product %d", product);
+    return -1;
+}
+
+int64_t relaysum_linear_workspace(int32_t n, int64_t tokens, int64_t width, int64_t channels, int32_t type) {
+    int64_t most = -1;
+    for (const int32_t product : {RELAYSUM_LINEAR, RELAYSUM_LINEAR_BACKWARD_INPUT, RELAYSUM_LINEAR_BACKWARD_WEIGHT})
+        most = std::max(most, relaysum_linear_workspace_of(product, n, tokens, width, channels, type));
+    return most;
 }
 
 int relaysum_linear(int32_t n, int64_t tokens, int64_t width, int64_t channels,

@@ -22,6 +22,11 @@ RELAYSUM_FLOAT = 0
 RELAYSUM_BFLOAT = 1
 RELAYSUM_HALF = 2
 
+# relaysum_product
+LINEAR = 0
+LINEAR_BACKWARD_INPUT = 1
+LINEAR_BACKWARD_WEIGHT = 2
+
 TYPES = {torch.float32: RELAYSUM_FLOAT, torch.bfloat16: RELAYSUM_BFLOAT,
          torch.float16: RELAYSUM_HALF}
 GROUP = 128
@@ -145,6 +150,7 @@ def _lib():
             "relaysum_linear_backward_input": (ctypes.c_int, [i32, i64, i64, i64, rows, packed,
                                                               rows, vp, sz, vp]),
             "relaysum_linear_workspace": (i64, [i32, i64, i64, i64, i32]),
+            "relaysum_linear_workspace_of": (i64, [i32, i32, i64, i64, i64, i32]),
             "relaysum_linear_backward_weight": (ctypes.c_int, [i32, i64, i64, i64, rows, packed,
                                                                rows, vp, sz, vp]),
             "relaysum_layer_error": (ctypes.c_char_p, []),
@@ -209,10 +215,10 @@ def _workspace(nbytes: int, device):
     return t.data_ptr(), nbytes, t
 
 
-# A workspace's size follows from the call's sizes alone.
+# A workspace's size follows from the call and its sizes alone.
 @functools.lru_cache(maxsize=1024)
-def _linear_workspace(n: int, tokens: int, width: int, channels: int, code: int) -> int:
-    return _lib().relaysum_linear_workspace(n, tokens, width, channels, code)
+def _linear_workspace(product: int, n: int, tokens: int, width: int, channels: int, code: int) -> int:
+    return _lib().relaysum_linear_workspace_of(product, n, tokens, width, channels, code)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -311,7 +317,7 @@ def linear(x: Packed, w: Packed, dtype=torch.bfloat16):
     cx, cw = x._c(device, "x"), w._c(device, "w")
     y, ry = _out(n, tokens, channels, dtype, device)
     lib = _lib()
-    ws, size, _keep = _workspace(_linear_workspace(n, tokens, width, channels, ry.type), device)
+    ws, size, _keep = _workspace(_linear_workspace(LINEAR, n, tokens, width, channels, ry.type), device)
     _check(lib.relaysum_linear(n, tokens, width, channels, cx, cw, ry, ws, size, stream),
            "relaysum_linear")
     return y
@@ -327,7 +333,7 @@ def linear_backward_input(dy, w: Packed):
     rdy, cw = _rows(dy, "dy", shape, device), w._c(device, "w")
     dx, rdx = _out(n, tokens, width, dy.dtype, device)
     lib = _lib()
-    ws, size, _keep = _workspace(_linear_workspace(n, tokens, width, channels, rdy.type), device)
+    ws, size, _keep = _workspace(_linear_workspace(LINEAR_BACKWARD_INPUT, n, tokens, width, channels, rdy.type), device)
     _check(lib.relaysum_linear_backward_input(n, tokens, width, channels, rdy, cw, rdx, ws, size,
                                               stream), "relaysum_linear_backward_input")
     return dx
@@ -344,6 +350,6 @@ def linear_backward_weight(dy, x: Packed, weight_grad) -> None:
     rdy, cx = _rows(dy, "dy", shape, device), x._c(device, "x")
     rg = _rows(weight_grad, "weight_grad", (n, channels, width), device, torch.float32)
     lib = _lib()
-    ws, size, _keep = _workspace(_linear_workspace(n, tokens, width, channels, rdy.type), device)
+    ws, size, _keep = _workspace(_linear_workspace(LINEAR_BACKWARD_WEIGHT, n, tokens, width, channels, rdy.type), device)
     _check(lib.relaysum_linear_backward_weight(n, tokens, width, channels, rdy, cx, rg, ws, size,
                                                stream), "relaysum_linear_backward_weight")
