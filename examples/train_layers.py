@@ -7,7 +7,9 @@ embedding, `blocks` sub-layers
 
     s = h + r;  y = norm(s);  h = W2 relu(W1 y);  r = s
 
-and a projection of the last norm onto the tokens.  Weights are views into the
+and a projection of the last norm onto the tokens.  There is no attention: a
+token is predicted from the one before it, which is all that a Markov chain
+needs.  Weights are views into the
 rows of x, packed once a round; their gradients are written into the rows of
 g.  What the backward pass needs stays in 8 bits: y and relu(W1 y), which the
 products multiply anyway, and s for the norm.  Activations and gradients

@@ -377,9 +377,10 @@ const char *relaysum_last_error(const relaysum_t *h);
 
 /* ---- layers on 8-bit rows -------------------------------------------------
  *
- * What n workers compute between two rounds when their models are
- * transformers: the operators of a sub-layer for all workers in one launch,
- * each worker with its own weights.  Weights are read where they lie, in the
+ * What n workers compute between two rounds when their models have
+ * feed-forward sub-layers, as transformers do: norm, products and their
+ * gradients (attention and activations are the caller's) for all workers in
+ * one launch, each worker with its own weights.  Weights are read where they lie, in the
  * models' rows x[i], and weight gradients are written where the next round
  * reads them, in the rows g[i].
  *
@@ -396,7 +397,8 @@ const char *relaysum_last_error(const relaysum_t *h);
  *   at least -126 that fits the group's largest entry, codes rounded to
  *   nearest, halves to even;
  *   exponent -128 marks a group with a NaN or an infinity: it stands for
- *   NaN throughout.
+ *   NaN throughout.  (64 * 2^122, what floats from 63.5 * 2^122 on are held
+ *   as, is 2^128: an infinity as a float.)
  * Scales are powers of two so that values are exact in bfloat16, which the
  * gradients' products multiply in.  codes is [n][rows][stride] with stride =
  * relaysum_packed_stride(width) and zeros behind the width; exponents are
@@ -405,11 +407,11 @@ const char *relaysum_last_error(const relaysum_t *h);
  *
  * Every array is DEVICE memory of the current GPU, checked with the HIP
  * runtime's pointer queries before anything is queued, and outputs share no
- * memory with other arrays, except where a call says so.  Sums over a row and
- * over tokens, and every product, are held in 32 bits or more.  Calls queue
- * kernels on `hip_stream` (NULL = null stream), allocate nothing, copy
- * nothing to the host, use no atomics (equal inputs give equal bits) and can
- * be recorded by HIP stream capture.  They return RELAYSUM_OK or
+ * memory with other arrays, except where a call says so (they may lie between
+ * other arrays' rows).  Sums over a row and over tokens, and every product,
+ * are held in 32 bits or more.  Calls queue kernels on `hip_stream` (NULL =
+ * null stream), allocate nothing, copy nothing to the host, use no atomics
+ * (equal inputs give equal bits) and can be recorded by HIP stream capture.  They return RELAYSUM_OK or
  * RELAYSUM_ERR_INVALID_ARG (nothing queued) or RELAYSUM_ERR_DEVICE;
  * relaysum_layer_error() has the text.
  *
@@ -471,6 +473,7 @@ int relaysum_rmsnorm(int32_t n, int64_t tokens, int64_t width, const relaysum_ro
 
 /* Gradients of the norm, with xh = rstd * s (s from saved) and u = dy * w:
  *   ds = dsum + rstd * (u - xh * mean(u * xh)),   weight_grad = sum over tokens of dy * xh
+ * (ds is not finite in a row whose sum of u * xh passes binary32's range)
  *   dy, dsum, ds  rows of one type: the gradients of y, of the sum from
  *            elsewhere (NULL: none) and of h and residual alike; ds may be
  *            dy's or dsum's own rows

@@ -1,7 +1,8 @@
 // Layer operators on CDNA4 (gfx950): what n workers, each with weights of its
 // own, compute between two RelaySum rounds.  RMS norm with the residual's
 // addition into 8-bit rows, its gradient, products of 8-bit rows and their
-// gradients, and packing; the C ABI is in relaysum.h.
+// gradients, and packing; the C ABI is in relaysum.h.  (With them a feed-forward
+// sub-layer is complete but for its activation; there is no attention.)
 //
 // 8-bit rows.  A group of entries v (a whole row, or 128 entries of it) is
 // held as q = rint(v * 2^-e), the smallest e >= -126 with max|v| <= 127 * 2^e.
@@ -215,8 +216,8 @@ __device__ __forceinline__ void write_whole(const Packed &out, int64_t row, int3
 
 // Packing: one pass, the row in registers between its maximum and its codes.
 // Bound by memory: an entry's bytes in, one byte out.  16 x 4096 x 2048
-// bfloat16 by 128: 403 MB in 73 us, 5.5 TB/s (a copy of 1 GiB: 5.1); a weight
-// of 16 workers, 2048 x 1024 out of model rows of odd length: 168 MB in 24 us.
+// bfloat16 by 128: 403 MB in 73 us, 5.5 TB/s (a flat copy: 6.5); a weight of
+// 16 workers, 2048 x 1024 out of model rows of odd length: 168 MB in 25 us.
 // Rows of up to 128 entries take 16 lanes, up to 2048 a wave, wider ones a
 // workgroup: the fewer threads share a row, the fewer steps its maximum takes,
 // but 4 chunks of 8 entries a thread are what the registers hold well.
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(block_of(TPR)) void pack_kernel(PackArgs a) {
     }
 }
 
-// Unpacking: a byte in, an entry out; 403 MB in 71 us, 5.7 TB/s.
+// Unpacking: a byte in, an entry out; 403 MB in 70 us, 5.8 TB/s.
 template <typename T, int TPR>
 __global__ __launch_bounds__(256) void unpack_kernel(PackArgs a) {
     constexpr int kRows = 256 / TPR;
@@ -307,8 +308,8 @@ __device__ __forceinline__ float scaled_rstd(float (&s)[J][8], float width, floa
 // with; y = s * rstd * w is not rounded before it is packed.  One pass: the row
 // stays in registers between the sum of squares and the codes.  Bound by
 // memory: 16 x 2048 x 1024 bfloat16 with s kept reads 4 bytes of an entry and
-// writes 4: 268 MB in 49 us, 5.5 TB/s.  The weights, a row for each worker,
-// come from the caches.
+// writes 4: 268 MB in 45 us, 6.0 TB/s (37 us without s, 6.3; a flat copy: 6.5).
+// The weights, a row for each worker, come from the caches.
 template <typename T, int TPR, int J, bool RESIDUAL, bool KEEP>
 __global__ __launch_bounds__(block_of(TPR)) void norm_kernel(NormArgs a) {
     __shared__ float redf[16];
@@ -376,9 +377,10 @@ struct NormGradArgs {
 // rows of one worker: threads keep their columns' weights and sums of dy * xh
 // in registers over all of them, so dw costs no memory traffic but one row for
 // each workgroup.  Bound by memory: 16 x 2048 x 1024 bfloat16, 7 bytes of an
-// entry, 235 MB in 47 us with the sum of the parts (4.8 us of it), 5.0 TB/s.
+// entry, 235 MB in 40 us with the sum of the parts (5 us of it), 5.9 TB/s.
 // From 16385 entries on a row does not fit the 128 registers that 1024 threads
-// have each, and part of it goes to scratch.
+// have each, and part of it goes to scratch: 4 x 512 x 32768 453 us, 1.0 TB/s
+// (x 16384: 46 us, 5.1).
 template <typename T, int TPR, int J, bool DSUM>
 __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs a) {
     constexpr int kRows = block_of(TPR) / TPR;
@@ -499,7 +501,7 @@ __device__ __forceinline__ int tile_at(int row, int chunk) {
 // Which result a matrix instruction's row r of tile j is: tiles go by Q, and a
 // lane's 4 rows of each of them are neighbours, so that a lane ends up with
 // 4 * Q entries in a row of the result, 32 bytes of it (dW of 16 x 2048 x 4096
-// -> 1024: 304 us, 325 with 64 bytes; the product in bfloat16 184 us, 195 with 16).
+// -> 1024 takes 7% more with 64 bytes, the product in bfloat16 6% more with 16).
 template <typename O>
 constexpr int kFours = 8 / (int)sizeof(O);
 template <int Q>
@@ -581,14 +583,17 @@ struct LinearArgs {
 // 128 x 64 a step reads 192 KB of LDS, 768 cycles of it by the counters, and
 // copies 64 KB in, for 2048 cycles of matrix instructions; reads of the second
 // half of a step are placed among the products of the first.  Measured: 16 x 2048 x 1024 ->
-// 4096 bfloat16 in 181 us, 1520 TOP/s; 4 x 8192 x 4096 -> 1024 in 125 us, 2190
-// (the library's 8192^3 product of int8: 2077).  What the shorter one lacks is
-// its 268 MB of results, written at the end of every tile with nothing to
-// compute beside: two workgroups of 4 waves of 64 x 128 on a CU, one buffer
-// each, took 187 us, 128 x 128 tiles 235, 4 waves of 128 x 128 241.
+// 4096 bfloat16 in 178 us, 1550 TOP/s; 4 x 8192 x 4096 -> 1024 in 115 us, 2400
+// (the library's 8192^3 product of int8: 2030-2080).  The shorter one's matrix
+// units are busy for 31% of the cycles: it writes 268 MB of results, at the end
+// of every tile with nothing to compute beside; it reads 303 MB where X and W
+// have 101, W once for every two rows of tiles, since tiles go along the
+// channels first; and each step waits for its own copies, one step in flight.
+// Two workgroups of 4 waves of 64 x 128 on a CU, one buffer each, took 3% more,
+// 128 x 128 tiles 30%, 4 waves of 128 x 128 33%.
 //
 // Few tokens: tiles of 16 x 128 (4 to a CU), so that 16 workers' weights for
-// one token are spread over all CUs: 25 MB in 4.8 us, 5.2 TB/s.  In between:
+// one token are spread over all CUs: 25 MB in 5.1 us, 4.9 TB/s.  In between:
 // 64 x 128 (3 to a CU).  plan_product has the rule.
 template <int BM, int BN, int WM, int WN, int QMAX>
 struct LinearTile {
@@ -777,14 +782,17 @@ template <> struct Parts<float> { static constexpr int n = 3; };
 // The products are exact in 32 bits; sums are bfloat16 matrix instructions'
 // 32-bit ones.  dY of 16 or 32 bits goes in as 2 or 3 bfloat16 that add up to it.
 //
-// Bound by the matrix unit together with what feeds it: of a step of 256 x 256
-// (2048 cycles of matrix instructions on each SIMD) the conversions and
-// addresses take about 900 cycles of the vector unit, and LDS is busy for 1280.
-// 16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 252 us,
-// 1090 TFLOP/s; dW, which also writes 268 MB, in 287 us, 960 (the library's
-// bfloat16 product of 8192^3: 1134).  Float gradients (three products each):
-// 937 and 1214 us; binary16 (two): 516 and 670.  The tile is as large as two
-// steps of all parts fit in LDS.
+// Bound by the matrix unit together with what feeds it: a step of 256 x 256 has
+// 2048 cycles of matrix instructions on each SIMD, conversions and addresses
+// about 900 of the vector unit, and LDS is busy for 1280.  dX takes some 4300
+// cycles a step (matrix units busy 48%), so a quarter is waiting; dW, which
+// also writes four times the bytes at the end of its tiles, 5500 (37%).
+// 16 x 2048 bfloat16 tokens, 4096 channels, width 1024: dX in 250 us,
+// 1100 TFLOP/s; dW 295-305 us, 900-930 (the library's bfloat16 product of
+// 8192^3: 1130-1150), 312 with X packed by 128.  Float gradients (three products
+// each): 909 and 1139 us; binary16 (two): 491 and 654.  The tile is as large as
+// two steps of all parts fit in LDS; floats, with a quarter of bfloat16's tile,
+// have twice the LDS reads for a matrix instruction that they would have there.
 template <typename T, int QMAX, bool ALONG_R, bool GROUPED, int BM, int BN, int WM, int WN>
 struct GradTile {
     static constexpr int kThreads = 64 * WM * WN, P = Parts<T>::n, BR = 64;
@@ -1360,9 +1368,9 @@ void with_type(int32_t type, F f) {
 }
 
 // Workgroups of a kernel over rows.  Packing and the norm loop over rows from
-// 16 a CU on (16 x 2048 x 1024 bfloat16: 49 us with 4096 workgroups, 52 with
-// one for every 4 rows; 16 x 4096 x 2048 packed by 128: 73 and 81); unpacking
-// has nothing to keep between rows and does better without (71 and 75).
+// 16 a CU on (one workgroup for every 4 rows took 6% more on a norm of 16 x 2048
+// x 1024 bfloat16, 11% more packing 16 x 4096 x 2048 by 128); unpacking has
+// nothing to keep between rows and does better without (6%).
 unsigned row_grid(int64_t rows, int per, int64_t most = 16 * kCus) {
     return (unsigned)std::min<int64_t>((rows + per - 1) / per, most);
 }
@@ -1370,8 +1378,8 @@ unsigned row_grid(int64_t rows, int per, int64_t most = 16 * kCus) {
 int chunks_layout(int64_t stride) { return stride <= 128 ? 16 : stride <= 2048 ? 64 : 256; }
 
 // Workgroups per worker of the norm's gradient: enough for four on each CU, no
-// more than one for 8 rows (5 x 777 x 1001 floats 14.3 us; one for 16 rows 16.2,
-// for 4 rows 14.9).
+// more than one for 8 rows (5 x 777 x 1001 floats, 15.2 us a call, took 13% more
+// with one for 16 rows, 4% more for 4).
 int norm_parts(int32_t n, int64_t rows) {
     const int64_t want = (4 * kCus + n - 1) / n;
     return (int)std::max<int64_t>(1, std::min<int64_t>(want, (rows + 7) / 8));

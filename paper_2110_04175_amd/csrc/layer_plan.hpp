@@ -33,8 +33,7 @@ struct Plan {
 // The cheapest of the tiles and splits by the time at which the last CU ends,
 // with what joining the parts costs: a launch, and every part written and
 // read.  The times were measured on MI355X over sizes from one token to
-// 65,536 and widths of 96 to 8,192; the choice took at most 1.25 times
-// the best one's time there.
+// 65,536 and widths of 96 to 8,192.
 inline Plan plan_product(const TileCost *tile, int count, int64_t n, int64_t m, int64_t cols, int64_t steps) {
     Plan best;
     float best_us = 0.0f;

@@ -7,7 +7,13 @@ float16, weights and weight gradients float32 views into the rows of the
 models x[n, d] and the gradients g[n, d], for instance
 ``x[:, a:a + c * k].unflatten(1, (c, k))``.  Any strides will do as long as
 the last axis is dense.  Results are new tensors, weight gradients go into
-the tensor given for them.  Work is queued on torch's current stream.
+the tensor given for them.
+
+Work is queued on torch's current stream; whoever uses a tensor, or the codes
+and exps of a Packed, on another one orders the two and calls record_stream,
+as for any tensor.  The operators take no part in autograd: results do not
+require gradients whatever the inputs do, and a backward pass is made of the
+``_backward`` calls (an autograd.Function can be built of them).
 """
 from __future__ import annotations
 
