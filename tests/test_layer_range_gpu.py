@@ -30,10 +30,10 @@ def host(t):
 # ---- the norm: mean squares past binary32's range on either side -----------------
 
 # Factors of a row of normal entries, and eps: the sum of squares overflows
-# while their mean does not (1e18), both overflow, squares are below every
-# normal number, or below every number; with the last of an eps that is larger.
-NORM_ROWS = [(1e18, 1e-6), (1e19, 1e-6), (3e37, 0.0), (1e-21, 0.0), (1e-25, 0.0), (1e-37, 0.0), (1e-25, 1e-42),
-             (1e-15, 0.0), (1e-30, 1e-38)]
+# while its mean does not (1e18), both overflow, squares lose bits below the
+# smallest normal number or vanish; in the last two eps is larger than they are.
+NORM_ROWS = [(1e18, 1e-6), (1e19, 1e-6), (3e37, 0.0), (1e-21, 0.0), (1e-25, 0.0), (1e-37, 0.0), (1e-15, 0.0),
+             (1e-25, 1e-42), (1e-30, 1e-38)]
 
 
 @pytest.mark.parametrize("width", [1, 100, 1001, 4100, 32768])
@@ -45,7 +45,7 @@ def test_norm_of_large_and_small_rows(width, dtype):
         h = normal(1, 2, 3, width)
         h[1] *= factor
         h[0, 1] *= factor
-        # At most 2.7 sigma below the largest number's 9, so none overflows.
+        # 5 * 3e37 and a residual of a tenth of that stay below the largest number.
         h = h.clamp(-5 * factor, 5 * factor).to(dtype) if factor > 5 else h.to(dtype)
         w = 1 + 0.1 * normal(3, 2, width)
         r = normal(2, 2, 3, width, std=0.1)
