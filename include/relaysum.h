@@ -523,7 +523,85 @@ int relaysum_linear_backward_weight(int32_t n, int64_t tokens, int64_t width, in
                                     const relaysum_rows *weight_grad, void *workspace,
                                     size_t workspace_bytes, void *hip_stream);
 
-/* Text of the calling thread's last failure in the calls on 8-bit rows (""
+/* ---- attention ------------------------------------------------------------
+ *
+ * What mixes the tokens of a layer: attention of n workers' sequences, all of
+ * them in one launch, and its gradients.
+ *
+ *   s_j = scale * q . k_j     for the keys j in [lo, hi) that a row sees
+ *   out = sum_j p_j v_j,      p_j = exp(s_j) / sum exp(s),   lse = log sum exp(s)
+ *
+ * q and out are heads of `tokens` rows, k and v those of `keys` rows; `heads` is
+ * a multiple of kv_heads, and heads g * heads / kv_heads and so on share key
+ * head g.  Which keys a row sees is said by ranges, int32 [n][tokens][2] of
+ * DEVICE memory: lo and hi of every row, in any order (packed sequences, prefixes,
+ * windows); what lies outside 0..keys is not seen.  Without ranges (NULL) a row t
+ * sees all keys, or with causal != 0 the keys up to t + keys - tokens: the last
+ * row sees all of them.  A row that sees nothing gives zeros, an lse of -infinity,
+ * and no gradient.  Keys and rows that do not see each other have no part in each
+ * other's results, also where they hold infinities or NaN.
+ *
+ * Scores, sums and gradients are held in 32 bits; the weights p and the gradients
+ * of the scores enter the second products rounded to the arrays' type.
+ * Errors, streams, capture and the rules for arrays are those of the layer calls
+ * above, relaysum_layer_error() has the text; equal inputs give equal bits. */
+
+/* Heads of n workers: entry k of head h of row t of worker i is entry
+ * i*worker_stride + t*row_stride + h*head_stride + k of data.  Strides count
+ * entries and are not negative; rows that are written must not overlap.  Rows may
+ * start anywhere the type can. */
+typedef struct relaysum_heads {
+    void *data;
+    int32_t type;            /* relaysum_type */
+    int64_t worker_stride;   /* ignored for n == 1 */
+    int64_t row_stride;      /* ignored for one row */
+    int64_t head_stride;     /* ignored for one head */
+} relaysum_heads;
+
+/* Ranges of packed sequences: sequence s of worker i has the rows starts[s] to
+ * starts[s + 1] - 1 and the keys key_starts[s] to key_starts[s + 1] - 1, both
+ * int32[count + 1] at + i * their stride (0: all workers have the same), in
+ * ascending order.  A row sees its sequence's keys, with causal != 0 those up to
+ * the one that is as far from their end as the row is from its own.  Rows in no
+ * sequence see nothing.  ranges is int32 [tokens][2] of each worker, ranges_stride >= tokens rows
+ * apart. */
+int relaysum_attention_ranges(int32_t n, int64_t tokens, int64_t keys, int32_t count,
+                              const int32_t *starts, int64_t starts_stride, const int32_t *key_starts,
+                              int64_t key_starts_stride, int32_t causal, int32_t *ranges,
+                              int64_t ranges_stride, void *hip_stream);
+
+/*   q, k, v, out   heads of one type, 1 <= width <= 256
+ *   ranges         8-byte aligned, or NULL; ranges_stride rows between workers'
+ *                  (0: all have the same)
+ *   scale          positive
+ *   lse            out, float[n][heads][tokens], or NULL: for the backward pass
+ *   workspace      relaysum_attention_workspace bytes, 16-byte aligned (NULL if 0):
+ *                  few rows share their keys out, and join
+ * tokens * heads and keys up to 2^30. */
+int64_t relaysum_attention_workspace(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
+                                     int32_t kv_heads, int64_t width);
+int relaysum_attention(int32_t n, int64_t tokens, int64_t keys, int32_t heads, int32_t kv_heads,
+                       int64_t width, const relaysum_heads *q, const relaysum_heads *k,
+                       const relaysum_heads *v, const int32_t *ranges, int64_t ranges_stride,
+                       int32_t causal, float scale, const relaysum_heads *out, float *lse,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* dq, dk and dv from dout, the gradient of out, and the forward pass's arguments,
+ * out and lse; all of one type.  Every row of dq, dk and dv is written (dk and dv
+ * sum over the heads that share a key head).  dq, dk and dv may be parts of the
+ * rows of one array. */
+int64_t relaysum_attention_backward_workspace(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
+                                              int32_t kv_heads, int64_t width, int32_t type);
+int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
+                                int32_t kv_heads, int64_t width, const relaysum_heads *dout,
+                                const relaysum_heads *q, const relaysum_heads *k,
+                                const relaysum_heads *v, const relaysum_heads *out, const float *lse,
+                                const int32_t *ranges, int64_t ranges_stride, int32_t causal,
+                                float scale, const relaysum_heads *dq, const relaysum_heads *dk,
+                                const relaysum_heads *dv, void *workspace, size_t workspace_bytes,
+                                void *hip_stream);
+
+/* Text of the calling thread's last failure in the layer calls (""
  * after a call that succeeded). */
 const char *relaysum_layer_error(void);
 

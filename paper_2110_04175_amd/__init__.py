@@ -49,6 +49,8 @@ EXPORTED = (
     "relaysum_rmsnorm_workspace", "relaysum_rmsnorm_backward", "relaysum_linear",
     "relaysum_linear_workspace_of", "relaysum_linear_workspace", "relaysum_linear_backward_input",
     "relaysum_linear_backward_weight", "relaysum_layer_error",
+    "relaysum_attention_ranges", "relaysum_attention_workspace", "relaysum_attention",
+    "relaysum_attention_backward_workspace", "relaysum_attention_backward",
 )
 
 PATHS = ("tile", "dtree", "wide_dtree", "cluster", "wide", "two_pass", "dtree_seq",

@@ -18,158 +18,13 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdarg>
 #include <cstdint>
-#include <cstdio>
 #include <type_traits>
 
-#include "layer_plan.hpp"
-#include "relaysum.h"
-
-using namespace layer_plan;
+#include "layer_call.hpp"
+#include "layer_sums.hpp"
 
 namespace {
-
-constexpr int kWave = 64;
-constexpr int64_t kMaxWidth = 32768;   // 127^2 * 32768 < 2^31: integer sums cannot overflow
-constexpr int64_t kMaxChannels = 1 << 24;
-constexpr int kGroup = 128;            // entries that share a scale in grouped rows, and the
-                                       // bytes a row of codes is rounded up to
-constexpr int kNotANumber = -128;      // exponent of a group that held a NaN or an infinity
-
-typedef int i4_t __attribute__((ext_vector_type(4)));
-typedef float f4_t __attribute__((ext_vector_type(4)));
-typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
-typedef unsigned u2_t __attribute__((ext_vector_type(2)));
-typedef unsigned u4_t __attribute__((ext_vector_type(4)));
-
-// ---- elements ------------------------------------------------------------------
-
-template <typename T>
-using v8_t = T __attribute__((ext_vector_type(8)));
-
-// Eight entries of a row as floats, those from `left` on as zeros.  Whole
-// chunks are one or two 16-byte loads at any alignment of the type.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int64_t left, float (&v)[8]) {
-    if (left >= 8) {
-        v8_t<T> t;
-        __builtin_memcpy(&t, p, sizeof t);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? (float)p[i] : 0.0f;
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T *p, int64_t left, const float (&v)[8]) {
-    if (left >= 8) {
-        v8_t<T> t;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = (T)v[i];
-        __builtin_memcpy(p, &t, sizeof t);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < left) p[i] = (T)v[i];
-    }
-}
-
-__device__ __forceinline__ unsigned bits_of(float f) { return __builtin_bit_cast(unsigned, f); }
-__device__ __forceinline__ float float_of(unsigned u) { return __builtin_bit_cast(float, u); }
-
-// Exponent of a group whose largest |v| has these bits.  127 = 1.984375 * 2^6:
-// |v| = m * 2^p fits 2^(p-6) if m <= 1.984375 (mantissa field 0x7e0000), else
-// 2^(p-5).  As integers, the bits of NaN are above infinity's, above every
-// number's, so one integer maximum finds the largest entry and what is none.
-__device__ __forceinline__ int exponent_of(unsigned maxbits) {
-    if (maxbits >= 0x7f800000u) return kNotANumber;
-    return max((int)((maxbits + 0x1ffffu) >> 23) - 133, -126);
-}
-
-// 2^-e, or 0 for a group that is not a number (every code is then 0: NaN and
-// infinity times 0 is NaN, which converts to 0).
-__device__ __forceinline__ float inverse_scale(int e) {
-    return float_of(e == kNotANumber ? 0u : (unsigned)(127 - e) << 23);
-}
-
-__device__ __forceinline__ float scale_of(int e) {
-    return float_of(e == kNotANumber ? 0x7fc00000u : (unsigned)(127 + e) << 23);
-}
-
-__device__ __forceinline__ u2_t codes8(const float (&v)[8], float inv) {
-    unsigned w[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        w[i / 4] |= ((unsigned)__float2int_rn(v[i] * inv) & 0xffu) << (8 * (i % 4));
-    return u2_t{w[0], w[1]};
-}
-
-// Two floats as two bfloat16, the first in the lower half.
-__device__ __forceinline__ unsigned bf16_pair(float a, float b) {
-    typedef float f2_t __attribute__((ext_vector_type(2)));
-    typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2_t{a, b}), b2_t));
-}
-
-__device__ __forceinline__ float code_at(unsigned w, int byte) {
-    return (float)(int)(int8_t)(w >> (8 * byte));
-}
-
-template <int J>
-__device__ __forceinline__ unsigned max_bits(const float (&v)[J][8]) {
-    unsigned m = 0;
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, bits_of(v[j][i]) & 0x7fffffffu);
-    return m;
-}
-
-// ---- reductions over the TPR threads that share a row ----------------------------
-//
-// 16 or 64 threads: lanes of one wave.  256 or 1024: a whole workgroup, through
-// LDS; `red` holds one value per wave.
-
-__device__ __forceinline__ float pick_sum(float a, float b) { return a + b; }
-__device__ __forceinline__ unsigned pick_max(unsigned a, unsigned b) { return max(a, b); }
-
-template <int TPR, typename V, V (*F)(V, V)>
-__device__ __forceinline__ V row_reduce(V v, V *red) {
-#pragma unroll
-    for (int m = 1; m < (TPR < kWave ? TPR : kWave); m *= 2) v = F(v, __shfl_xor(v, m));
-    if (TPR > kWave) {
-        const int wave = threadIdx.x / kWave;
-        __syncthreads();
-        if (threadIdx.x % kWave == 0) red[wave] = v;
-        __syncthreads();
-        v = red[0];
-#pragma unroll
-        for (int w = 1; w < TPR / kWave; ++w) v = F(v, red[w]);
-    }
-    return v;
-}
-
-constexpr int block_of(int tpr) { return tpr > 256 ? tpr : 256; }
-
-// ---- rows of n workers -----------------------------------------------------------
-
-struct Rows {
-    char *data;
-    int64_t ws, rs;   // strides in entries
-};
-
-template <typename T>
-__device__ __forceinline__ T *row_at(const Rows &r, int64_t worker, int64_t row) {
-    return reinterpret_cast<T *>(r.data) + worker * r.ws + row * r.rs;
-}
-
-struct Packed {
-    int8_t *codes, *exps;
-    int32_t groups;   // exponents of a row
-};
 
 struct PackArgs {
     Rows v;
@@ -177,42 +32,6 @@ struct PackArgs {
     int64_t rows, total;   // rows of a worker, of all workers
     int32_t width, stride;
 };
-
-// Codes of a row that TPR threads hold in v (chunk j of thread `lane`: entries
-// 8 * (lane + j * TPR)), as whole rows or in groups of 128 entries, which 16
-// neighbouring lanes hold.
-template <int TPR, int J>
-__device__ __forceinline__ void write_grouped(const Packed &out, int64_t row, int32_t stride,
-                                              int lane, const float (&v)[J][8]) {
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const int chunk = lane + j * TPR;
-        unsigned m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, bits_of(v[j][i]) & 0x7fffffffu);
-#pragma unroll
-        for (int s = 1; s < 16; s *= 2) m = max(m, (unsigned)__shfl_xor((int)m, s));
-        if (chunk * 8 >= stride) continue;
-        const int e = exponent_of(m);
-        if (lane % 16 == 0) out.exps[row * out.groups + chunk / 16] = (int8_t)e;
-        *reinterpret_cast<u2_t *>(out.codes + row * stride + chunk * 8) =
-            codes8(v[j], inverse_scale(e));
-    }
-}
-
-template <int TPR, int J>
-__device__ __forceinline__ void write_whole(const Packed &out, int64_t row, int32_t stride,
-                                            int lane, const float (&v)[J][8], unsigned *red) {
-    const int e = exponent_of(row_reduce<TPR, unsigned, pick_max>(max_bits(v), red));
-    const float inv = inverse_scale(e);
-    if (lane == 0) out.exps[row] = (int8_t)e;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const int chunk = lane + j * TPR;
-        if (chunk * 8 < stride)
-            *reinterpret_cast<u2_t *>(out.codes + row * stride + chunk * 8) = codes8(v[j], inv);
-    }
-}
 
 // Packing: one pass, the row in registers between its maximum and its codes.
 // Bound by memory: an entry's bytes in, one byte out.  16 x 4096 x 2048
@@ -276,33 +95,6 @@ struct NormArgs {
     int32_t width, stride;
     float eps;
 };
-
-// 1 / sqrt(mean(s^2) + eps) of a row whose squares, or their sum, may lie
-// outside binary32's range: s is scaled by the power of two that brings the
-// row's largest entry, or the root of eps if that is larger, to 1 or 2.  Leaves
-// the scaled row in s and returns what it is to be multiplied by; rstd is that
-// of the row as it was, an infinity where it passes the range (rows of numbers
-// below 2^-128).  Rows of zeros, and those with a NaN or an infinity, stay.
-// Every thread of the row takes part.
-template <int TPR, int J>
-__device__ __forceinline__ float scaled_rstd(float (&s)[J][8], float width, float eps, float &rstd,
-                                             float *redf, unsigned *redu) {
-    const unsigned most = row_reduce<TPR, unsigned, pick_max>(max_bits(s), redu);
-    if (most == 0 || most >= 0x7f800000u) return rstd;
-    const int p = max(ilogbf(float_of(most)), ilogbf(eps) >> 1);
-    float sq = 0.0f;
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            s[j][i] = ldexpf(s[j][i], -p);
-            sq = fmaf(s[j][i], s[j][i], sq);
-        }
-    sq = row_reduce<TPR, float, pick_sum>(sq, redf);
-    const float inv = 1.0f / sqrtf(sq / width + ldexpf(eps, -2 * p));
-    rstd = ldexpf(inv, -p);
-    return inv;
-}
 
 // s = h + r, rounded to the rows' type because that is what the stream goes on
 // with; y = s * rstd * w is not rounded before it is packed.  One pass: the row
@@ -456,32 +248,6 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_grad_kernel(NormGradArgs a
     }
 }
 
-// out[i][c] = sum over parts of partial[i][p][c].  A workgroup has 32 columns
-// of one worker and 8 sums of every eighth part each, added in a fixed order,
-// so equal inputs give equal bits.
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float *partial, float *out,
-                                                        int64_t out_stride, int32_t parts,
-                                                        int32_t width) {
-    __shared__ float sums[8][32];
-    const unsigned per = (width + 31) / 32;
-    const int64_t worker = blockIdx.x / per;
-    const int lane = threadIdx.x % 32, group = threadIdx.x / 32;
-    const int c = (int)(blockIdx.x % per) * 32 + lane;
-    float v = 0.0f;
-    if (c < width) {
-        const float *p = partial + worker * parts * (int64_t)width + c;
-#pragma unroll 4
-        for (int k = group; k < parts; k += 8) v += p[(int64_t)k * width];
-    }
-    sums[group][lane] = v;
-    __syncthreads();
-    if (group == 0 && c < width) {
-#pragma unroll
-        for (int k = 1; k < 8; ++k) v += sums[k][lane];
-        out[worker * out_stride + c] = v;
-    }
-}
-
 // ---- products ------------------------------------------------------------------------
 //
 // LDS tiles of both products: rows of 128 bytes (128 codes, or 64 bfloat16 of
@@ -529,22 +295,6 @@ __device__ __forceinline__ int column_at(int at, int x) { return (at ^ (swizzle(
 __device__ __forceinline__ int fresh(int v) {
     asm volatile("" : "+v"(v));
     return v;
-}
-
-// 16 bytes for each lane from memory into LDS at `to` + 16 * lane, without
-// registers in between; `to` is the same for the whole wave.
-__device__ __forceinline__ void copy_to_lds(const void *from, char *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-}
-
-__device__ __forceinline__ void wait_for_copies() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
-
-// Blocks go round the 8 XCDs; each takes a run of neighbouring tiles, which
-// share rows in its L2.
-__device__ __forceinline__ unsigned xcd_tile(unsigned block, unsigned blocks) {
-    const unsigned run = blocks / 8, rest = blocks % 8, x = block % 8;
-    return x * run + (x < rest ? x : rest) + block / 8;
 }
 
 // 4 * Q entries of a row of `cols`, from column c0 on.
@@ -1120,270 +870,6 @@ __global__ __launch_bounds__(256) void join_grad_kernel(GradArgs a) {
 }
 
 // ---- host side -------------------------------------------------------------------------
-
-thread_local char g_error[256];
-
-int refuse(const char *format, ...) __attribute__((format(printf, 1, 2)));
-int refuse(const char *format, ...) {
-    va_list ap;
-    va_start(ap, format);
-    std::vsnprintf(g_error, sizeof g_error, format, ap);
-    va_end(ap);
-    return RELAYSUM_ERR_INVALID_ARG;
-}
-
-int device_error(const char *what, hipError_t e) {
-    std::snprintf(g_error, sizeof g_error, "%s: %s", what, hipGetErrorString(e));
-    return RELAYSUM_ERR_DEVICE;
-}
-
-int done(const char *what) {
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return device_error(what, e);
-    g_error[0] = '\0';
-    return RELAYSUM_OK;
-}
-
-int64_t code_stride(int64_t width) { return (width + kGroup - 1) / kGroup * kGroup; }
-
-size_t type_bytes(int32_t type) { return type == RELAYSUM_FLOAT ? 4 : 2; }
-
-// One array of a call: where it lies, for the checks that follow.  Row t of
-// worker i is the `row` bytes at p + i * ws + t * rs; a dense array is one row.
-struct Span {
-    const char *name;
-    const char *p;
-    size_t bytes;     // from the first row's start to the last one's end
-    bool out;
-    bool typed;       // rows of a type, which a call may allow to be written in place
-    int64_t row, ws, rs, n, rows;
-
-    // The bytes that rows reach over when all of them are moved by multiples of
-    // m to where the first lies.
-    int64_t reach(int64_t m) const {
-        return row + (ws % m ? (n - 1) * ws : 0) + (rs % m ? (rows - 1) * rs : 0);
-    }
-};
-
-// Whether no byte is in both: one array ends before the other starts, or both
-// keep to their own part of every stretch of m bytes, m a stride of either
-// (models and gradients as halves of one tensor, say).
-bool apart(const Span &a, const Span &b) {
-    if (a.p >= b.p + b.bytes || b.p >= a.p + a.bytes) return true;
-    for (const int64_t m : {a.ws, a.rs, b.ws, b.rs}) {
-        if (m <= 0) continue;
-        const int64_t from = (int64_t)(b.p - a.p) % m, start = from < 0 ? from + m : from;
-        if (start >= a.reach(m) && start + b.reach(m) <= m) return true;
-    }
-    return false;
-}
-
-// Collects a call's arrays and says what is wrong with them.
-struct Call {
-    Span spans[12];
-    int count = 0;
-    int code = RELAYSUM_OK;
-    int device = 0;
-    // Whether rows may be written over rows read with the same strides: the
-    // threads of a row read all of it before they write.
-    bool in_place = false;
-
-    void fail(int c) { code = code == RELAYSUM_OK ? c : code; }
-
-    bool sizes(int32_t n, int64_t rows, int64_t width, const char *what) {
-        if (n < 1 || n > RELAYSUM_MAX_WORKERS)
-            fail(refuse("n must be in 1..%d", RELAYSUM_MAX_WORKERS));
-        else if (rows < 0 || rows > (int64_t)1 << 40)
-            fail(refuse("%s must be in 0..2^40", what));
-        else if (width < 1 || width > kMaxWidth)
-            fail(refuse("the width must be in 1..%d", (int)kMaxWidth));
-        else if ((__int128)n * (rows + 1) * width > ((__int128)1 << 50))
-            fail(refuse("n * %s * width is more than 2^50", what));
-        return code == RELAYSUM_OK;
-    }
-
-    // The product's result has a row of `channels` entries for each token.
-    bool product(int32_t n, int64_t tokens, int64_t width, int64_t channels) {
-        if (!sizes(n, tokens, width, "tokens")) return false;
-        if (channels < 1 || channels > kMaxChannels)
-            fail(refuse("channels must be in 1..%d", (int)kMaxChannels));
-        else if ((__int128)n * (tokens + width) * channels > ((__int128)1 << 50))
-            fail(refuse("n * (tokens + width) * channels is more than 2^50"));
-        return code == RELAYSUM_OK;
-    }
-
-    // A product's workgroups and workspace.
-    template <typename P>
-    void product_launch(const P &plan, const void *workspace, size_t bytes) {
-        if (code != RELAYSUM_OK) return;
-        // Not even the largest tile's fit a launch.
-        if (plan.blocks > kMaxBlocks) return fail(refuse("the result has more than %d tiles", (int)kMaxBlocks));
-        if (plan.workspace > bytes)
-            return fail(refuse("the workspace has %zu bytes, %zu are needed", bytes, plan.workspace));
-        span("workspace", workspace, plan.workspace, 16, true);
-    }
-
-    void span(const char *name, const void *p, size_t bytes, size_t align, bool out) {
-        add(Span{name, static_cast<const char *>(p), bytes, out, false, (int64_t)bytes, 0, 0, 1, 1}, align);
-    }
-
-    void add(const Span &s, size_t align) {
-        if (code != RELAYSUM_OK || !s.bytes) return;
-        if (!s.p)
-            fail(refuse("%s must not be NULL", s.name));
-        else if ((uintptr_t)s.p % align)
-            fail(refuse("%s must be %d-byte aligned", s.name, (int)align));
-        else
-            spans[count++] = s;
-    }
-
-    // The norm's weights: a row of floats for each worker.
-    void weights(const float *w, int32_t n, int64_t stride, int64_t width) {
-        if (code != RELAYSUM_OK) return;
-        if (n == 1) stride = 0;
-        if (stride < 0 || stride > ((int64_t)1 << 44) / n)
-            return fail(refuse("weight_stride is negative or reaches past 2^44 entries"));
-        const size_t entries = (size_t)((n - 1) * stride + width);
-        add(Span{"weight", reinterpret_cast<const char *>(w), entries * 4, false, false, width * 4, stride * 4, 0, n, 1}, 4);
-    }
-
-    void rows(const char *name, const relaysum_rows *r, int32_t n, int64_t rows, int64_t width,
-              bool out) {
-        if (code != RELAYSUM_OK) return;
-        if (!r) return fail(refuse("%s must not be NULL", name));
-        if (r->type < RELAYSUM_FLOAT || r->type > RELAYSUM_HALF)
-            return fail(refuse("%s: unknown type %d", name, r->type));
-        const int64_t ws = n > 1 ? r->worker_stride : 0, rs = rows > 1 ? r->row_stride : 0;
-        const int64_t most = (int64_t)1 << 44;
-        if (ws < 0 || rs < 0 || (n > 1 && ws > most / n) || (rows > 1 && rs > most / rows))
-            return fail(refuse("%s: a stride is negative or reaches past 2^44 entries", name));
-        if (!rows) return;
-        // Rows that are written must not share entries: they follow one
-        // another within a worker, or the workers follow one another in a row.
-        const bool within = (rows == 1 || rs >= width) && (n == 1 || ws >= (rows - 1) * rs + width);
-        const bool across = (n == 1 || ws >= width) && (rows == 1 || rs >= (n - 1) * ws + width);
-        if (out && !within && !across) return fail(refuse("%s: its rows overlap", name));
-        const size_t entries = (size_t)((n - 1) * ws + (rows - 1) * rs + width);
-        const int64_t b = (int64_t)type_bytes(r->type);
-        add(Span{name, static_cast<const char *>(r->data), entries * b, out, true, width * b, ws * b, rs * b, n, rows},
-            type_bytes(r->type));
-    }
-
-    void packed(const char *name, const relaysum_packed *p, int32_t n, int64_t rows, int64_t width,
-                bool out) {
-        if (code != RELAYSUM_OK) return;
-        if (!p) return fail(refuse("%s must not be NULL", name));
-        if (p->group != 0 && p->group != kGroup)
-            return fail(refuse("%s: the group must be 0 (whole rows) or %d", name, kGroup));
-        const int64_t stride = code_stride(width);
-        span(name, p->codes, (size_t)n * rows * stride, 16, out);
-        span(name, p->exps, (size_t)n * rows * (p->group ? stride / kGroup : 1), 1, out);
-    }
-
-    // Overlaps, then each array against the allocation that holds it.
-    bool ready() {
-        if (code != RELAYSUM_OK) return false;
-        for (int i = 0; i < count; ++i)
-            for (int j = 0; j < i; ++j) {
-                const Span &a = spans[i], &b = spans[j];
-                if (!(a.out || b.out) || apart(a, b)) continue;
-                if (in_place && a.out != b.out && a.p == b.p && a.bytes == b.bytes && a.typed && b.typed &&
-                    a.ws == b.ws && a.rs == b.rs)
-                    continue;
-                fail(refuse("%s and %s share memory", b.name, a.name));
-                return false;
-            }
-        hipError_t e = hipGetDevice(&device);
-        if (e != hipSuccess) {
-            fail(device_error("hipGetDevice", e));
-            return false;
-        }
-        for (int i = 0; i < count; ++i)
-            if (!on_device(spans[i].p, spans[i].bytes)) {
-                fail(refuse("%s does not lie within one allocation of device memory on the current GPU",
-                            spans[i].name));
-                return false;
-            }
-        return true;
-    }
-
-    // hipPointerGetAttributes gives the memory's kind and GPU,
-    // hipMemGetAddressRange the allocation (memory it cannot place, such as
-    // mappings made with the virtual-memory calls, passes on its kind and GPU).
-    bool on_device(const void *p, size_t bytes) const {
-        hipPointerAttribute_t at;
-        if (hipPointerGetAttributes(&at, p) != hipSuccess) {
-            (void)hipGetLastError();
-            return false;
-        }
-        if (at.type != hipMemoryTypeDevice && at.type != hipMemoryTypeManaged) return false;
-        if (at.type == hipMemoryTypeDevice && at.device != device) return false;
-        hipDeviceptr_t base = nullptr;
-        size_t size = 0;
-        if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess || !base) {
-            (void)hipGetLastError();
-            return true;
-        }
-        const uintptr_t b = (uintptr_t)base, q = (uintptr_t)p;
-        return q >= b && q - b <= size && bytes <= size - (q - b);
-    }
-};
-
-Rows rows_of(const relaysum_rows *r, int32_t n, int64_t rows) {
-    if (!r) return Rows{nullptr, 0, 0};
-    return Rows{static_cast<char *>(r->data), n > 1 ? r->worker_stride : 0, rows > 1 ? r->row_stride : 0};
-}
-
-Packed packed_of(const relaysum_packed *p, int64_t width) {
-    if (!p) return Packed{nullptr, nullptr, 0};
-    return Packed{p->codes, p->exps, (int32_t)(p->group ? code_stride(width) / kGroup : 1)};
-}
-
-// Whether a row has one exponent; up to 128 entries both groups have.
-bool whole_rows(const relaysum_packed *p, int64_t width) { return p->group == 0 || width <= kGroup; }
-
-template <int V>
-using Int = std::integral_constant<int, V>;
-
-// Calls f with the row layout for a row of `stride` codes: the threads that
-// share a row and the 8-entry chunks each of them holds.
-template <typename F>
-void with_layout(int64_t stride, F f) {
-    const int64_t chunks = stride / 8;
-    if (chunks <= 16) f(Int<16>(), Int<1>());
-    else if (chunks <= 64) f(Int<64>(), Int<1>());
-    else if (chunks <= 128) f(Int<64>(), Int<2>());
-    else if (chunks <= 256) f(Int<64>(), Int<4>());
-    else if (chunks <= 512) f(Int<256>(), Int<2>());
-    else if (chunks <= 1024) f(Int<256>(), Int<4>());
-    else if (chunks <= 2048) f(Int<1024>(), Int<2>());
-    else f(Int<1024>(), Int<4>());
-}
-
-template <typename F>
-void with_type(int32_t type, F f) {
-    if (type == RELAYSUM_FLOAT) f((float)0);
-    else if (type == RELAYSUM_BFLOAT) f((__bf16)0);
-    else f((_Float16)0);
-}
-
-// Workgroups of a kernel over rows.  Packing and the norm loop over rows from
-// 16 a CU on (one workgroup for every 4 rows took 6% more on a norm of 16 x 2048
-// x 1024 bfloat16, 11% more packing 16 x 4096 x 2048 by 128); unpacking has
-// nothing to keep between rows and does better without (6%).
-unsigned row_grid(int64_t rows, int per, int64_t most = 16 * kCus) {
-    return (unsigned)std::min<int64_t>((rows + per - 1) / per, most);
-}
-
-int chunks_layout(int64_t stride) { return stride <= 128 ? 16 : stride <= 2048 ? 64 : 256; }
-
-// Workgroups per worker of the norm's gradient: enough for four on each CU, no
-// more than one for 8 rows (5 x 777 x 1001 floats, 15.2 us a call, took 13% more
-// with one for 16 rows, 4% more for 4).
-int norm_parts(int32_t n, int64_t rows) {
-    const int64_t want = (4 * kCus + n - 1) / n;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(want, (rows + 7) / 8));
-}
 
 // Calls f with the large or the small tile of a type: BM, BN, WM, WN.
 template <typename T, typename F>

@@ -1,9 +1,9 @@
-"""Layer operators of n workers on 8-bit rows (the part of ``relaysum.h``
-under that name): RMS norm with the residual's addition, products of packed
-rows, their gradients, and packing.
+"""Layer operators of n workers (the parts of ``relaysum.h`` behind the
+round): RMS norm with the residual's addition, products of packed rows and
+packing; attention; and their gradients.
 
 Activations are CUDA tensors [n, tokens, width] in float32, bfloat16 or
-float16, weights and weight gradients float32 views into the rows of the
+float16 (heads: [n, tokens, heads, width]), weights and weight gradients float32 views into the rows of the
 models x[n, d] and the gradients g[n, d], for instance
 ``x[:, a:a + c * k].unflatten(1, (c, k))``.  Any strides will do as long as
 the last axis is dense.  Results are new tensors, weight gradients go into
@@ -43,6 +43,12 @@ class Rows(ctypes.Structure):
     """struct relaysum_rows of relaysum.h."""
     _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32),
                 ("worker_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class Heads(ctypes.Structure):
+    """struct relaysum_heads of relaysum.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32), ("worker_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class _CPacked(ctypes.Structure):
@@ -143,6 +149,7 @@ def _lib():
         lib = load_library()
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         rows, packed = ctypes.POINTER(Rows), ctypes.POINTER(_CPacked)
+        heads, f32 = ctypes.POINTER(Heads), ctypes.c_float
         sig = {
             "relaysum_packed_stride": (i64, [i64]),
             "relaysum_pack": (ctypes.c_int, [i32, i64, i64, rows, packed, vp]),
@@ -160,6 +167,15 @@ def _lib():
             "relaysum_linear_backward_weight": (ctypes.c_int, [i32, i64, i64, i64, rows, packed,
                                                                rows, vp, sz, vp]),
             "relaysum_layer_error": (ctypes.c_char_p, []),
+            "relaysum_attention_ranges": (ctypes.c_int, [i32, i64, i64, i32, vp, i64, vp, i64, i32, vp,
+                                                         i64, vp]),
+            "relaysum_attention_workspace": (i64, [i32, i64, i64, i32, i32, i64]),
+            "relaysum_attention": (ctypes.c_int, [i32, i64, i64, i32, i32, i64, heads, heads, heads, vp,
+                                                  i64, i32, f32, heads, vp, vp, sz, vp]),
+            "relaysum_attention_backward_workspace": (i64, [i32, i64, i64, i32, i32, i64, i32]),
+            "relaysum_attention_backward": (ctypes.c_int, [i32, i64, i64, i32, i32, i64, heads, heads,
+                                                           heads, heads, heads, vp, vp, i64, i32, f32,
+                                                           heads, heads, heads, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(lib, name)
@@ -359,3 +375,156 @@ def linear_backward_weight(dy, x: Packed, weight_grad) -> None:
     ws, size, _keep = _workspace(_linear_workspace(LINEAR_BACKWARD_WEIGHT, n, tokens, width, channels, rdy.type), device)
     _check(lib.relaysum_linear_backward_weight(n, tokens, width, channels, rdy, cx, rg, ws, size,
                                                stream), "relaysum_linear_backward_weight")
+
+
+# ---- attention --------------------------------------------------------------
+
+
+def _heads(t, name: str, shape, device: int, dtype) -> Heads:
+    """The description of a tensor [n, rows, heads, width] whose last axis is
+    dense."""
+    if isinstance(t, torch.Tensor) and t.get_device() == device and t.shape == shape and t.dtype == dtype:
+        code = TYPES.get(dtype)
+        if code is not None:
+            st = t.stride()
+            if st[3] == 1 or shape[3] <= 1 or not t.numel():
+                return Heads(t.data_ptr(), code, st[0], st[1], st[2])
+    _refuse(t, name, shape, device, dtype)
+
+
+def _new_heads(shape, dtype, device):
+    t = torch.empty(shape, dtype=dtype, device=device)
+    _, rows, heads, width = shape
+    return t, Heads(t.data_ptr(), TYPES[dtype], rows * heads * width, heads * width, width)
+
+
+def _four(t, name: str):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must have four axes: workers, rows, heads, width")
+    return t.shape
+
+
+def _starts(t, name: str, n: int, count, device: int):
+    """(address, stride between workers, sequences) of starts [count + 1] or
+    [n, count + 1]."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the current device")
+    if t.dtype != torch.int32:
+        raise ValueError(f"{name} must be torch.int32, not {t.dtype}")
+    if t.dim() not in (1, 2) or t.shape[-1] < 2 or (t.dim() == 2 and t.shape[0] != n) or \
+            (count is not None and t.shape[-1] != count + 1):
+        want = "sequences" if count is None else count
+        raise ValueError(f"{name} must have shape [{want} + 1] or [{n}, {want} + 1], not {list(t.shape)}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last axis must be dense")
+    return t.data_ptr(), t.stride(0) if t.dim() == 2 else 0, t.shape[-1] - 1
+
+
+def attention_ranges(starts, tokens: int, key_starts=None, keys=None, causal: bool = True):
+    """The keys that each row sees, int32 [n, tokens, 2] (first, last + 1), of
+    packed sequences: sequence s has rows starts[i, s] to starts[i, s + 1] - 1
+    of worker i, and the same keys, or those that key_starts says.  starts
+    int32 [n, count + 1], or [count + 1] for all workers alike (then ranges are
+    [1, tokens, 2]).  With `causal` a row sees the keys up to its own place,
+    counted from its sequence's end.  Rows in no sequence see nothing.  One
+    set of ranges serves all layers of a batch."""
+    if key_starts is None:
+        key_starts, keys = starts, tokens if keys is None else keys
+    elif keys is None:
+        raise ValueError("key_starts need keys, their number")
+    device, stream = _here()
+    n = max(t.shape[0] if isinstance(t, torch.Tensor) and t.dim() == 2 else 1 for t in (starts, key_starts))
+    at, stride, count = _starts(starts, "starts", n, None, device)
+    kat, kstride, _ = _starts(key_starts, "key_starts", n, count, device)
+    ranges = torch.empty((n, tokens, 2), dtype=torch.int32, device=device)
+    _check(_lib().relaysum_attention_ranges(n, tokens, keys, count, at, stride, kat, kstride, causal,
+                                            ranges.data_ptr(), tokens, stream),
+           "relaysum_attention_ranges")
+    return ranges
+
+
+def _ranges(t, n: int, tokens: int, device: int):
+    """(address, rows between workers) of ranges [n or 1, tokens, 2]."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("ranges must be a CUDA (HIP) tensor")
+    if t.get_device() != device:
+        raise ValueError("ranges must be on the current device")
+    if t.dtype != torch.int32 or t.dim() != 3 or t.shape[0] not in (1, n) or t.shape[1:] != (tokens, 2) or \
+            not t.is_contiguous():
+        raise ValueError(f"ranges must be contiguous torch.int32 of shape [{n} or 1, {tokens}, 2]")
+    return t.data_ptr(), tokens if t.shape[0] > 1 else 0
+
+
+def _attention_sizes(q, k):
+    n, tokens, heads, width = _four(q, "q")
+    _, keys, kv_heads, _ = _four(k, "k")
+    return n, tokens, keys, heads, kv_heads, width
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(*sizes) -> int:
+    return _lib().relaysum_attention_workspace(*sizes)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_backward_workspace(*sizes) -> int:
+    return _lib().relaysum_attention_backward_workspace(*sizes)
+
+
+def attention(q, k, v, ranges=None, causal: bool = True, scale=None, keep: bool = True):
+    """(out, lse): attention of q[n, tokens, heads, width] over k and v[n, keys,
+    kv_heads, width]; heads g * heads / kv_heads and so on share key head g.
+    `ranges` (attention_ranges, or any int32 [n or 1, tokens, 2]) says which
+    keys a row sees; without it a row sees all keys, or with `causal` those up
+    to its own place, where the last row sees all.  scale is 1 / sqrt(width)
+    unless given.  lse[n, heads, tokens] is what attention_backward needs (None
+    without `keep`)."""
+    sizes = n, tokens, keys, heads, kv_heads, width = _attention_sizes(q, k)
+    device, stream = _here()
+    rq = _heads(q, "q", q.shape, device, q.dtype)
+    rk = _heads(k, "k", (n, keys, kv_heads, width), device, q.dtype)
+    rv = _heads(v, "v", (n, keys, kv_heads, width), device, q.dtype)
+    at, stride = _ranges(ranges, n, tokens, device)
+    out, ro = _new_heads((n, tokens, heads, width), q.dtype, device)
+    lse = torch.empty((n, heads, tokens), dtype=torch.float32, device=device) if keep else None
+    lib = _lib()
+    ws, size, _keep = _workspace(_attention_workspace(*sizes), device)
+    _check(lib.relaysum_attention(*sizes, rq, rk, rv, at, stride, causal,
+                                  width ** -0.5 if scale is None else scale, ro,
+                                  lse.data_ptr() if keep else None, ws, size, stream),
+           "relaysum_attention")
+    return out, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, ranges=None, causal: bool = True, scale=None, into=None):
+    """(dq, dk, dv) from dout, the gradient of out, and attention's arguments
+    and results.  They are new tensors, or the three of `into`, which may be
+    views of one: ``d.split([heads, kv_heads, kv_heads], 2)``."""
+    sizes = n, tokens, keys, heads, kv_heads, width = _attention_sizes(q, k)
+    device, stream = _here()
+    row, key = (n, tokens, heads, width), (n, keys, kv_heads, width)
+    rq, rd = _heads(q, "q", row, device, q.dtype), _heads(dout, "dout", row, device, q.dtype)
+    rk, rv = _heads(k, "k", key, device, q.dtype), _heads(v, "v", key, device, q.dtype)
+    ro = _heads(out, "out", row, device, q.dtype)
+    _rows(lse, "lse", (n, heads, tokens), device, torch.float32)
+    if not lse.is_contiguous():
+        raise ValueError("lse must be contiguous")
+    at, stride = _ranges(ranges, n, tokens, device)
+    if into is None:
+        new = [_new_heads(shape, q.dtype, device) for shape in (row, key, key)]
+        into, to = tuple(t for t, _ in new), [r for _, r in new]
+    else:
+        to = [_heads(t, name, shape, device, q.dtype)
+              for t, name, shape in zip(into, ("dq", "dk", "dv"), (row, key, key), strict=True)]
+    lib = _lib()
+    ws, size, _keep = _workspace(_attention_backward_workspace(*sizes, rq.type), device)
+    _check(lib.relaysum_attention_backward(*sizes, rd, rq, rk, rv, ro, lse.data_ptr(), at, stride, causal,
+                                           width ** -0.5 if scale is None else scale, *to, ws, size,
+                                           stream), "relaysum_attention_backward")
+    return tuple(into)

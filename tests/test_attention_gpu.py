@@ -1,0 +1,420 @@
+"""GPU: attention and its gradients against the plain 64-bit implementation
+(oracle/attention.py), one row at a time.
+
+Tolerances.  u is half a step of the type.  A weight p is off by the rounding
+of its score, at most (width + 8) * 2^-24 of the sum of its terms' sizes (S),
+by its sum's, keys * 2^-24, and some 32 * 2^-24 for exponentials and scales:
+D = 2 * (width + 8) * 2^-24 * S + (keys + 32) * 2^-24, relative; and by u where
+it enters a product.  A result is a sum of terms that are off that much, added
+up with at most terms * 2^-24, and is rounded once:
+  out  (u + 2 D) * sum p |v| + u |out|
+  dv   (u + 2 D) * sum p |dout| + u |dv|
+  ds   p (dout . v - dout . out): out is off by 2 u + D of sum p |v|, p by D,
+       and ds is rounded by u: (3 u + 4 D) * p (|dout| |v| + sum p |dout| |v|)
+  dq   scale * that * |k| summed + u |dq|, dk likewise.
+binary16 holds p times 2^15 and ds times a power of two that keeps the largest
+possible one between 2^13 and 2^15: what is below 2^-14 then is off by 2^-25,
+2^-40 of 1 and 2^-38 of the largest |dout| |v|, for each term.
+The exponential instruction gives 0 for results below 2^-126.  That is of a
+weight before it is divided by its row's sum, which is at least 2^-8 (forward:
+the reference may lie 2^8 above no score, and sums are of the largest weight
+at least), and of p itself (backward): each term is off by 2^-118 at most."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2110_04175_amd as rs
+from oracle import attention as plain
+from paper_2110_04175_amd import layer
+
+pytestmark = pytest.mark.gpu
+
+ULP = 2.0 ** -24
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def announce(msg):
+    sys.__stderr__.write(f"[gpu] {msg}\n")
+    sys.__stderr__.flush()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def normal(seed, *shape, std=1.0, dtype=torch.float32):
+    g = np.random.default_rng(seed).standard_normal(shape) * std
+    return torch.from_numpy(g.astype(np.float32)).cuda().to(dtype)
+
+
+def heads(seed, n, tokens, keys, h, kv, width, dtype, std=1.0):
+    return (normal(seed, n, tokens, h, width, dtype=dtype, std=std), normal(seed + 1, n, keys, kv, width, dtype=dtype, std=std),
+            normal(seed + 2, n, keys, kv, width, dtype=dtype), normal(seed + 3, n, tokens, h, width, dtype=dtype, std=0.1))
+
+
+def near(got, want, off, what):
+    got = host(got)
+    assert got.shape == want.shape
+    assert np.isfinite(got).all(), what
+    bad = np.abs(got - want) > off
+    assert not bad.any(), (what, np.abs(got - want)[bad].max(), int(bad.sum()), np.argwhere(bad)[:4].tolist())
+
+
+def bounds(q, k, v, dout, rr, causal, c, grad):
+    """[(value, how far off)] of out, lse, dq, dk and dv."""
+    n, tokens, h, width = q.shape
+    keys = k.shape[1]
+    t, u = q.dtype, ROUND[q.dtype]
+    qh, kh, vh, doh = (np.where(np.isfinite(host(x)), host(x), 0.0) for x in (q, k, v, dout))
+    got = plain.attention(qh, kh, vh, rr, c, doh if grad else None)
+
+    def norm(x):
+        return np.sqrt((x ** 2).sum(-1).max(initial=0))
+
+    def most(x):
+        return np.abs(x).max(initial=0)
+
+    d = 2 * (width + 8) * ULP * c * norm(qh) * norm(kh) + (keys + 32) * ULP
+    want, lse, size = got[:3]
+    with np.errstate(invalid="ignore"):
+        found = [(want, (u + 2 * d) * size + u * np.abs(want) + TINY[t] + 2.0 ** -118 * keys * most(vh)), (lse, 2 * d + 4 * ULP * np.abs(lse))]
+    if not grad:
+        return found
+    half, sums = t == torch.float16, tokens * h * ULP
+    flushed = 2.0 ** -118 * max(keys, tokens * h)
+    tiny_s = 2.0 ** -37 * norm(doh) * norm(vh) * c * max(keys, tokens * h) * max(most(qh), most(kh)) if half else 0.0
+    tiny_p = 2.0 ** -40 * tokens * h * most(doh) if half else 0.0
+    (dq, dk, dv), (sq, sk, sv) = got[3], got[4]
+    tiny_s += 2 * flushed * norm(doh) * norm(vh) * c * max(most(qh), most(kh))
+    tiny_p += flushed * most(doh)
+    return found + [(dq, (3 * u + 4 * d) * sq + u * np.abs(dq) + TINY[t] + tiny_s),
+                    (dk, (3 * u + 4 * d + sums) * sk + u * np.abs(dk) + TINY[t] + tiny_s),
+                    (dv, (u + 2 * d + sums) * sv + u * np.abs(dv) + TINY[t] + tiny_p)]
+
+
+def check(q, k, v, dout, ranges=None, causal=True, scale=None, grad=True, want_ranges=None):
+    """Everything that one call and its gradients give."""
+    n, tokens, h, width = q.shape
+    keys = k.shape[1]
+    c = width ** -0.5 if scale is None else scale
+    out, lse = layer.attention(q, k, v, ranges, causal, scale)
+    rr = want_ranges if want_ranges is not None else \
+        plain.default_ranges(n, tokens, keys, causal) if ranges is None else \
+        np.broadcast_to(ranges.cpu().numpy(), (n, tokens, 2))
+    found = bounds(q, k, v, dout, rr, causal, c, grad)
+    near(out, *found[0], "out")
+    want, off = found[1]
+    some, glse = np.isfinite(want), host(lse)
+    assert np.array_equal(np.isfinite(glse), some) and (glse[~some] == want[~some]).all()
+    assert (np.abs(glse[some] - want[some]) <= off[some]).all()
+    if not grad:
+        return out, lse
+    grads = layer.attention_backward(dout, q, k, v, out, lse, ranges, causal, scale)
+    for x, (want, off), what in zip(grads, found[2:], ("dq", "dk", "dv")):
+        near(x, want, off, what)
+    return (out, lse, *grads)
+
+
+SHAPES = [
+    # n, tokens, keys, heads, kv, width
+    (1, 1, 1, 1, 1, 1),
+    (2, 1, 70, 4, 2, 64),
+    (1, 5, 300, 3, 1, 33),
+    (3, 31, 31, 2, 2, 16),
+    (1, 33, 33, 6, 2, 80),
+    (2, 64, 64, 4, 4, 128),
+    (1, 129, 129, 2, 1, 65),
+    (1, 40, 100, 5, 5, 129),
+    (1, 70, 70, 3, 3, 256),
+    (2, 100, 37, 2, 1, 40),    # more rows than keys: causal rows that see nothing
+    (1, 65, 257, 7, 1, 100),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_shapes(shape, causal, dtype):
+    announce(f"attention {shape} causal={causal} {dtype}")
+    check(*heads(1, *shape, dtype), causal=causal)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [24, 64, 100, 128, 200, 256])
+def test_many_tiles(width, dtype):
+    """Enough workgroups for the kernel that has whole tiles of rows: 260 key
+    heads, some 130 rows each."""
+    announce(f"attention tiles width={width} {dtype}")
+    n, tokens = 26, 13
+    check(*heads(2, n, tokens, tokens + 57, 100, 10, width, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_packed_sequences(dtype):
+    """Sequences of no, one and many rows, other ones for each worker, padding
+    behind them (and in front) that holds NaN."""
+    announce(f"attention packed {dtype}")
+    n, t = 3, 150
+    starts = [[0, 0, 1, 2, 40, 40, 100, 131], [3, 20, 21, 85, 85, 86, 149, 150], [0, 0, 0, 0, 0, 0, 64, 128]]
+    q, k, v, do = heads(3, n, t, t, 4, 2, 48, dtype)
+    for i, s in enumerate(starts):
+        for x in (q, k, v, do):
+            x[i, :s[0]] = float("nan")
+            x[i, s[-1]:] = float("nan")
+    st = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    for causal in (True, False):
+        ranges = layer.attention_ranges(st, t, causal=causal)
+        want = plain.ranges_of(starts, t, starts, t, causal)
+        got = ranges.cpu().numpy()
+        assert ((got == want).all(-1) | ((got[..., 0] >= got[..., 1]) & (want[..., 0] >= want[..., 1]))).all()
+        out, lse, dq, dk, dv = check(q, k, v, do, ranges, want_ranges=want)
+        for i, s in enumerate(starts):
+            for x in (out, dq, dk, dv):
+                assert (x[i, :s[0]] == 0).all() and (x[i, s[-1]:] == 0).all()
+
+
+def test_packed_sequences_with_more_keys():
+    """Each sequence's rows are the last of its keys, or more than it has."""
+    announce("attention packed, other keys")
+    starts = [[0, 3, 3, 50, 60]]
+    keys = [[0, 90, 95, 160, 163]]
+    q, k, v, do = heads(4, 2, 64, 170, 3, 1, 32, torch.bfloat16)
+    st, kst = (torch.tensor(x[0], dtype=torch.int32, device="cuda") for x in (starts, keys))
+    ranges = layer.attention_ranges(st, 64, kst, 170)
+    assert ranges.shape == (1, 64, 2)
+    check(q, k, v, do, ranges, want_ranges=plain.ranges_of(starts * 2, 64, keys * 2, 170, True))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("seed", range(4))
+def test_any_ranges(seed, dtype):
+    """Windows, prefixes, ranges in no order, empty ones and ones that reach
+    outside."""
+    announce(f"attention ranges seed={seed} {dtype}")
+    rng = np.random.default_rng(seed)
+    n, t, keys = (2, 90, 140) if seed % 2 else (1, 200, 77)
+    kind = rng.integers(0, 4, (n, t, 1))
+    lo = rng.integers(-20, keys, (n, t, 1))
+    hi = rng.integers(0, keys + 30, (n, t, 1))
+    row = np.broadcast_to(np.arange(t)[None, :, None], (n, t, 1))
+    lo = np.where(kind == 0, row - 10, np.where(kind == 1, 0, lo))
+    hi = np.where(kind == 0, row + 1, hi)
+    r = np.concatenate([lo, hi], 2).astype(np.int32)
+    check(*heads(5 + seed, n, t, keys, 4, 2, 64, dtype), torch.from_numpy(r).cuda())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides(dtype):
+    """Parts of one projection's rows, heads outside tokens, rows that start
+    anywhere, broadcast inputs, gradients into parts of one array."""
+    announce(f"attention strides {dtype}")
+    n, t, h, kv, w = 2, 75, 4, 2, 40
+    wide = normal(6, n, t, (h + 2 * kv) * w + 3, dtype=dtype)
+    q, k, v = wide[:, :, 1:-2].unflatten(2, (h + 2 * kv, w)).split([h, kv, kv], 2)
+    do = normal(7, n, h, t, w, dtype=dtype, std=0.1).transpose(1, 2)
+    out, lse, dq, dk, dv = check(q, k, v, do)
+    d = torch.full((n, t, (h + 2 * kv) * w + 3), 7.0, dtype=dtype, device="cuda")
+    into = d[:, :, 1:-2].unflatten(2, (h + 2 * kv, w)).split([h, kv, kv], 2)
+    got = layer.attention_backward(do, q, k, v, out, lse, into=into)
+    for a, b in zip(got, (dq, dk, dv)):
+        assert torch.equal(a, b)
+    assert (d[:, :, 0] == 7).all() and (d[:, :, -2:] == 7).all()
+    one = normal(8, 1, 1, 1, w, dtype=dtype)
+    check(one.expand(n, t, h, w), k, one.expand(n, t, kv, w), do)
+    check(q, k[:1].expand(n, t, kv, w), v, one.expand(n, t, h, w))
+
+
+def test_far_rows():
+    """Rows whose places pass 32 bits, of keys and of queries."""
+    announce("attention far rows")
+    keys, w = 70, 64
+    far = torch.empty(1, keys, 1 << 26, dtype=torch.bfloat16, device="cuda")
+    k, v = far[:, :, 5:5 + 2 * w].unflatten(2, (2, w)), far[:, :, -2 * w:].unflatten(2, (2, w))
+    q, a, b, do = heads(9, 1, keys, keys, 4, 2, w, torch.bfloat16)
+    k.copy_(a)
+    v.copy_(b)
+    check(q, k, v, do)
+    check(q[:, -1:], k, v, do[:, -1:])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_what_is_not_seen_has_no_part(bad, dtype):
+    """NaN and infinities in keys, values, queries and gradients of other
+    sequences and of later tokens."""
+    announce(f"attention {bad} {dtype}")
+    t, w, cut, late = 140, 48, 61, 110
+    q, k, v, do = heads(10, 2, t, t, 4, 2, w, dtype)
+    starts = torch.tensor([0, cut, t], dtype=torch.int32, device="cuda")
+    ranges = layer.attention_ranges(starts, t)
+    rr = np.broadcast_to(ranges.cpu().numpy(), (2, t, 2))
+    good = bounds(q, k, v, do, rr, True, w ** -0.5, True)
+    # The first worker's second sequence from `late` on.
+    for x in (q, k, v, do):
+        x[0, late:, :, 3] = bad
+    out, lse = layer.attention(q, k, v, ranges)
+    grads = layer.attention_backward(do, q, k, v, out, lse, ranges)
+    del good[1]
+    for got, (want, off), what in zip((out, *grads), good, ("out", "dq", "dk", "dv")):
+        near(got[1], want[1], off[1], what)
+        near(got[0, :cut], want[0, :cut], off[0, :cut], what)
+        if what in ("out", "dq"):
+            near(got[0, cut:late], want[0, cut:late], off[0, cut:late], what)
+    assert not torch.isfinite(out[0, late:, :, 3]).any()
+
+
+def test_scores_that_are_not_finite():
+    """A visible score of +infinity or NaN makes a row NaN; of -infinity takes
+    a key out, of all keys leaves 0 / 0."""
+    announce("attention infinite scores")
+    t, w = 40, 16
+    q = torch.ones(1, t, 1, w, device="cuda")
+    k = normal(11, 1, t, 1, w)
+    v = normal(12, 1, t, 1, w)
+    k[0, 5, 0, 0] = -float("inf")
+    out, lse = layer.attention(q, k, v, causal=False)
+    keep = [j for j in range(t) if j != 5]
+    want, _ = layer.attention(q, k[:, keep].contiguous(), v[:, keep].contiguous(), causal=False)
+    assert torch.allclose(out, want, rtol=1e-5, atol=1e-6)
+    k[0, :, 0, 0] = -float("inf")
+    out, lse = layer.attention(q, k, v, causal=False)
+    assert torch.isnan(out).all() and (lse == -float("inf")).all()
+    k[0, :, 0, 0] = 0
+    k[0, 30, 0, 0] = float("inf")
+    out, lse = layer.attention(q, k, v)
+    assert torch.isfinite(out[0, :30]).all() and torch.isnan(out[0, 30:]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_scores_and_small_gradients(dtype):
+    """Scores of thousands, which leave one key; gradients near the smallest
+    that the type holds well."""
+    announce(f"attention large scores {dtype}")
+    q, k, v, do = heads(13, 2, 60, 60, 2, 1, 64, dtype, std=8.0)
+    check(q, k, v, do * 1e-3)
+    q, k, v, do = heads(14, 2, 60, 60, 2, 1, 64, dtype, std=0.3)
+    check(q, k, v * 30, do)
+    check(q, k, v, do, scale=3.0)
+
+
+def test_long_sums():
+    """One row over 20,000 keys, in parts, and 1,500 rows of one head."""
+    announce("attention long")
+    q, k, v, do = heads(15, 1, 1, 20000, 2, 1, 64, torch.bfloat16)
+    check(q, k, v, do)
+    q, k, v, do = heads(16, 1, 1500, 1500, 1, 1, 16, torch.float16)
+    check(q, k, v, do)
+
+
+def test_no_rows_and_no_keys():
+    announce("attention of nothing")
+    for t, keys in ((0, 5), (5, 0), (0, 0)):
+        q, k, v, do = heads(17, 2, t, keys, 4, 2, 32, torch.float16)
+        out, lse = layer.attention(q, k, v)
+        grads = layer.attention_backward(do, q, k, v, out, lse)
+        assert out.shape == q.shape and (out == 0).all() and (lse == -float("inf")).all()
+        for g, x in zip(grads, (q, k, v)):
+            assert g.shape == x.shape and (g == 0).all()
+
+
+def test_equal_bits():
+    announce("attention twice")
+    q, k, v, do = heads(18, 3, 333, 333, 6, 2, 64, torch.bfloat16)
+    first = check(q, k, v, do, grad=False)
+    g = layer.attention_backward(do, q, k, v, *first)
+    for _ in range(3):
+        out, lse = layer.attention(q, k, v)
+        again = layer.attention_backward(do, q, k, v, out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+        assert all(torch.equal(a, b) for a, b in zip(again, g))
+
+
+def test_another_stream():
+    announce("attention on a stream")
+    q, k, v, do = heads(19, 2, 200, 200, 4, 2, 64, torch.bfloat16)
+    out, lse = layer.attention(q, k, v)
+    g = layer.attention_backward(do, q, k, v, out, lse)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        o2, l2 = layer.attention(q, k, v)
+        g2 = layer.attention_backward(do, q, k, v, o2, l2)
+    s.synchronize()
+    assert torch.equal(out, o2) and torch.equal(lse, l2) and all(torch.equal(a, b) for a, b in zip(g, g2))
+
+
+def test_two_captured_graphs():
+    """Two graphs of calls with parts, workspaces and ranges, replayed in turn
+    with new inputs and eager calls between."""
+    announce("attention in graphs")
+
+    def make(seed, t, keys):
+        q, k, v, do = heads(seed, 2, t, keys, 4, 2, 64, torch.float16)
+        starts = torch.tensor([0, t // 2, t], dtype=torch.int32, device="cuda")
+        kst = torch.tensor([0, keys // 3, keys], dtype=torch.int32, device="cuda")
+
+        def step():
+            r = layer.attention_ranges(starts, t, kst, keys)
+            out, lse = layer.attention(q, k, v, r)
+            return (out, lse, *layer.attention_backward(do, q, k, v, out, lse, r))
+        return (q, k, v, do), step
+
+    made = [make(20, 3, 900), make(30, 300, 300)]
+    graphs = []
+    for inputs, step in made:
+        step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs = step()
+        graphs.append((g, outs))
+    for turn in range(3):
+        for (inputs, step), (g, outs) in zip(made, graphs):
+            for i, x in enumerate(inputs):
+                x.copy_(normal(100 + turn * 10 + i, *x.shape, std=0.5))
+            want = step()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, outs)), turn
+
+
+def test_refusals_on_the_device():
+    announce("attention refusals")
+    q, k, v, do = heads(21, 2, 10, 12, 4, 2, 32, torch.float16)
+    out, lse = layer.attention(q, k, v)
+    with pytest.raises(ValueError):
+        layer.attention(q, k.float(), v)
+    with pytest.raises(ValueError):
+        layer.attention(q, k, v[:, :11])
+    with pytest.raises(ValueError):
+        layer.attention(q.transpose(2, 3), k, v)
+    with pytest.raises(ValueError):
+        layer.attention(q, k, v, torch.zeros(2, 10, 2, device="cuda"))
+    with pytest.raises(ValueError):
+        layer.attention(q, k, v, torch.zeros(2, 9, 2, dtype=torch.int32, device="cuda"))
+    with pytest.raises(TypeError):
+        layer.attention(q.cpu(), k, v)
+    with pytest.raises(ValueError):
+        layer.attention(q.double(), k.double(), v.double())
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(rs.RelaySumError):
+            layer.attention(q, k, v, scale=scale)
+    with pytest.raises(rs.RelaySumError):
+        layer.attention(q[:, :, :3], k, v)     # 3 heads on 2 key heads
+    wide = torch.zeros(1, 2, 1, 257, device="cuda")
+    with pytest.raises(rs.RelaySumError):
+        layer.attention(wide, wide, wide)
+    one = torch.zeros(2, 1, 4, 32, device="cuda", dtype=torch.float16)
+    with pytest.raises(rs.RelaySumError):
+        layer.attention_backward(do, q, k, v, out, lse, into=(one.expand(2, 10, 4, 32), k.clone(), v.clone()))
+    with pytest.raises(rs.RelaySumError):
+        layer.attention_backward(do, q, k, v, out, lse, into=(do, k.clone(), v.clone()))
+    with pytest.raises(ValueError):
+        layer.attention_backward(do, q, k, v, out, lse.half())
+    with pytest.raises(ValueError):
+        layer.attention_ranges(torch.tensor([0, 5], device="cuda"), 10)
