@@ -601,6 +601,46 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
                                 const relaysum_heads *dv, void *workspace, size_t workspace_bytes,
                                 void *hip_stream);
 
+/* ---- recurrence -----------------------------------------------------------
+ *
+ * The other way to mix tokens: every channel carries a state along its sequence,
+ *
+ *   h_t = a_t h_(t-1) + (1 - a_t) x_t,   a = sigmoid(gate)
+ *   dgate_t = dh_t (h_(t-1) - x_t) a_t (1 - a_t),  dx_t = (1 - a_t) dh_t
+ *
+ * where dh is the whole gradient of h_t: that of the output, and a_(t+1) times the
+ * next token's.  A worker's rows hold `count` packed sequences: sequence s has the
+ * rows starts[s] to starts[s + 1] - 1, int32[count + 1] of DEVICE memory at
+ * + i * starts_stride (0: all workers have the same), ascending, within 0..tokens;
+ * NULL: one sequence of all rows (count 1).  Each starts from its own state
+ * (initial, or zeros) and leaves its last one; one of no rows leaves the state
+ * that it has.  Rows in no sequence give zeros.  States are held in 32 bits, and
+ * the gradients come from states in 32 bits, not from the rounded h.
+ * Errors, streams, capture and the rules for arrays are those of the layer calls;
+ * equal inputs give equal bits.  tokens up to 2^30, width up to 32768.
+ *
+ *   gate, x, h     rows of one type (of the gradients too)
+ *   initial, last  float rows, `count` for each worker, or NULL
+ *   saved          out, float[n][relaysum_recurrence_chunks(tokens)][width], for the
+ *                  backward pass, or NULL
+ *   workspace      relaysum_recurrence_workspace bytes, 8-byte aligned (NULL if 0) */
+int64_t relaysum_recurrence_chunks(int64_t tokens);
+int64_t relaysum_recurrence_workspace(int32_t n, int64_t tokens, int64_t width);
+int relaysum_recurrence(int32_t n, int64_t tokens, int64_t width, int32_t count, const int32_t *starts,
+                        int64_t starts_stride, const relaysum_rows *gate, const relaysum_rows *x,
+                        const relaysum_rows *initial, const relaysum_rows *h, const relaysum_rows *last,
+                        float *saved, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* dgate, dx and dinitial (NULL: not wanted) from dh, the gradient of h, and dlast,
+ * that of last (NULL: none). */
+int relaysum_recurrence_backward(int32_t n, int64_t tokens, int64_t width, int32_t count,
+                                 const int32_t *starts, int64_t starts_stride, const relaysum_rows *dh,
+                                 const relaysum_rows *dlast, const relaysum_rows *gate,
+                                 const relaysum_rows *x, const relaysum_rows *initial, const float *saved,
+                                 const relaysum_rows *dgate, const relaysum_rows *dx,
+                                 const relaysum_rows *dinitial, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream);
+
 /* Text of the calling thread's last failure in the layer calls (""
  * after a call that succeeded). */
 const char *relaysum_layer_error(void);

@@ -51,6 +51,8 @@ EXPORTED = (
     "relaysum_linear_backward_weight", "relaysum_layer_error",
     "relaysum_attention_ranges", "relaysum_attention_workspace", "relaysum_attention",
     "relaysum_attention_backward_workspace", "relaysum_attention_backward",
+    "relaysum_recurrence_chunks", "relaysum_recurrence_workspace", "relaysum_recurrence",
+    "relaysum_recurrence_backward",
 )
 
 PATHS = ("tile", "dtree", "wide_dtree", "cluster", "wide", "two_pass", "dtree_seq",

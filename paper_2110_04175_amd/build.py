@@ -11,7 +11,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "relaysum.hip")
-SOURCES = [SRC] + [os.path.join(PKG, "csrc", name) for name in ("layer.hip", "attention.hip")]
+SOURCES = [SRC] + [os.path.join(PKG, "csrc", name) for name in ("layer.hip", "attention.hip", "recurrence.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librelaysum.so")
 

@@ -1,6 +1,6 @@
 """Layer operators of n workers (the parts of ``relaysum.h`` behind the
 round): RMS norm with the residual's addition, products of packed rows and
-packing; attention; and their gradients.
+packing; attention; a gated recurrence; and their gradients.
 
 Activations are CUDA tensors [n, tokens, width] in float32, bfloat16 or
 float16 (heads: [n, tokens, heads, width]), weights and weight gradients float32 views into the rows of the
@@ -37,6 +37,7 @@ TYPES = {torch.float32: RELAYSUM_FLOAT, torch.bfloat16: RELAYSUM_BFLOAT,
          torch.float16: RELAYSUM_HALF}
 GROUP = 128
 MAX_WIDTH = 32768
+CHUNK = 64          # tokens between the states that a recurrence keeps
 
 
 class Rows(ctypes.Structure):
@@ -176,6 +177,12 @@ def _lib():
             "relaysum_attention_backward": (ctypes.c_int, [i32, i64, i64, i32, i32, i64, heads, heads,
                                                            heads, heads, heads, vp, vp, i64, i32, f32,
                                                            heads, heads, heads, vp, sz, vp]),
+            "relaysum_recurrence_chunks": (i64, [i64]),
+            "relaysum_recurrence_workspace": (i64, [i32, i64, i64]),
+            "relaysum_recurrence": (ctypes.c_int, [i32, i64, i64, i32, vp, i64, rows, rows, rows, rows,
+                                                   rows, vp, vp, sz, vp]),
+            "relaysum_recurrence_backward": (ctypes.c_int, [i32, i64, i64, i32, vp, i64, rows, rows, rows,
+                                                            rows, rows, vp, rows, rows, rows, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(lib, name)
@@ -528,3 +535,67 @@ def attention_backward(dout, q, k, v, out, lse, ranges=None, causal: bool = True
                                            width ** -0.5 if scale is None else scale, *to, ws, size,
                                            stream), "relaysum_attention_backward")
     return tuple(into)
+
+
+# ---- recurrence -------------------------------------------------------------
+
+
+@functools.lru_cache(maxsize=1024)
+def _recurrence_workspace(n: int, tokens: int, width: int) -> int:
+    return _lib().relaysum_recurrence_workspace(n, tokens, width)
+
+
+def _sequences(starts, n: int, device: int):
+    """(address, stride, count); without starts one sequence of all rows."""
+    return (None, 0, 1) if starts is None else _starts(starts, "starts", n, None, device)
+
+
+def recurrence(gate, x, initial=None, starts=None, keep: bool = True):
+    """(h, last, saved) with h_t = a_t h_(t-1) + (1 - a_t) x_t, a = sigmoid(gate),
+    channel by channel, for gate and x[n, tokens, width].  `starts` int32
+    [n, count + 1] or [count + 1] says where packed sequences begin (and the
+    last one ends); initial[n, count, width] float32 are the states that they
+    start from (zeros without it), last[n, count, width] float32 those they
+    end with: given back as initial, a sequence goes on.  `saved` is for
+    recurrence_backward (None without `keep`)."""
+    n, tokens, width = shape = _three(gate, "gate")
+    device, stream = _here()
+    rg, rx = _rows(gate, "gate", shape, device), _rows(x, "x", shape, device, gate.dtype)
+    at, stride, count = _sequences(starts, n, device)
+    ri = None if initial is None else _rows(initial, "initial", (n, count, width), device, torch.float32)
+    h, rh = _out(n, tokens, width, gate.dtype, device)
+    last, rl = _out(n, count, width, torch.float32, device)
+    saved = None
+    lib = _lib()
+    if keep:
+        saved = torch.empty((n, max(1, -(-tokens // CHUNK)), width), dtype=torch.float32, device=device)
+    ws, size, _keep = _workspace(_recurrence_workspace(n, tokens, width), device)
+    _check(lib.relaysum_recurrence(n, tokens, width, count, at, stride, rg, rx, ri, rh, rl,
+                                   saved.data_ptr() if keep else None, ws, size, stream),
+           "relaysum_recurrence")
+    return h, last, saved
+
+
+def recurrence_backward(dh, dlast, gate, x, saved, initial=None, starts=None):
+    """(dgate, dx, dinitial) from dh, the gradient of h, and dlast, that of
+    last (None: not used elsewhere), with recurrence's arguments and `saved`."""
+    n, tokens, width = shape = _three(gate, "gate")
+    device, stream = _here()
+    rg, rx = _rows(gate, "gate", shape, device), _rows(x, "x", shape, device, gate.dtype)
+    rd = _rows(dh, "dh", shape, device, gate.dtype)
+    at, stride, count = _sequences(starts, n, device)
+    states = (n, count, width)
+    ri = None if initial is None else _rows(initial, "initial", states, device, torch.float32)
+    rl = None if dlast is None else _rows(dlast, "dlast", states, device, torch.float32)
+    _rows(saved, "saved", (n, max(1, -(-tokens // CHUNK)), width), device, torch.float32)
+    if not saved.is_contiguous():
+        raise ValueError("saved must be contiguous")
+    dgate, ro = _out(n, tokens, width, gate.dtype, device)
+    dx, rdx = _out(n, tokens, width, gate.dtype, device)
+    dinitial, rdi = _out(n, count, width, torch.float32, device)
+    lib = _lib()
+    ws, size, _keep = _workspace(_recurrence_workspace(n, tokens, width), device)
+    _check(lib.relaysum_recurrence_backward(n, tokens, width, count, at, stride, rd, rl, rg, rx, ri,
+                                            saved.data_ptr(), ro, rdx, rdi, ws, size, stream),
+           "relaysum_recurrence_backward")
+    return dgate, dx, dinitial
