@@ -641,6 +641,49 @@ int relaysum_recurrence_backward(int32_t n, int64_t tokens, int64_t width, int32
                                  const relaysum_rows *dinitial, void *workspace, size_t workspace_bytes,
                                  void *hip_stream);
 
+/* ---- norms around a block ---------------------------------------------------
+ *
+ * The norm behind a block, with its gate and the scale of the residual branch,
+ * and the norm in front of the next block, in one pass:
+ *
+ *   s = residual + scale * sigmoid(gate) * z * post_rstd * post_weight
+ *   y = s * rstd * weight,    post_rstd and rstd = 1 / sqrt(mean^2 + eps) of z and s
+ *
+ * z, gate, residual and sum are rows of one type; s is rounded to it, and the
+ * second norm is that of the rounded s.  gate may be NULL (1 in its place).
+ * post_weight and weight are float[width] of each worker, scale one float, at
+ * + i * their strides.  y leaves in 8 bits by whole rows, and s for the gradient
+ * by 128 (saved, or NULL), as relaysum_rmsnorm's; the rounding to 8 bits counts
+ * as the identity.  post_rstd and rstd are out, float[n][tokens].  sum may be
+ * the own rows of z, gate or residual.  Rows whose mean square lies outside
+ * binary32's range are treated as relaysum_rmsnorm's.  Limits, errors, streams
+ * and capture are those of the calls on 8-bit rows. */
+int relaysum_blocknorm(int32_t n, int64_t tokens, int64_t width, const relaysum_rows *z,
+                       const relaysum_rows *gate, const relaysum_rows *residual, const float *post_weight,
+                       int64_t post_weight_stride, const float *scale, int64_t scale_stride,
+                       const float *weight, int64_t weight_stride, float eps, const relaysum_rows *sum,
+                       const relaysum_packed *y, float *post_rstd, float *rstd,
+                       const relaysum_packed *saved, void *hip_stream);
+
+/* The gradients of z (dz), gate (dgate, NULL if and only if gate is) and residual
+ * (ds), and of the three parameters (float rows, one for each worker,
+ * overwritten; scale_grad's has one entry), from dy, dsum (the gradient of the sum
+ * from elsewhere, NULL: none) and what the forward pass gave.  dz, dgate and ds
+ * may each be the own rows of one of the inputs.  Equal inputs give
+ * equal bits.  workspace: relaysum_blocknorm_workspace
+ * bytes, 4-byte aligned (NULL if 0). */
+int64_t relaysum_blocknorm_workspace(int32_t n, int64_t tokens, int64_t width);
+int relaysum_blocknorm_backward(int32_t n, int64_t tokens, int64_t width, const relaysum_rows *dy,
+                                const relaysum_rows *dsum, const relaysum_rows *z,
+                                const relaysum_rows *gate, const relaysum_packed *saved,
+                                const float *post_rstd, const float *rstd, const float *post_weight,
+                                int64_t post_weight_stride, const float *scale, int64_t scale_stride,
+                                const float *weight, int64_t weight_stride, const relaysum_rows *dz,
+                                const relaysum_rows *dgate, const relaysum_rows *ds,
+                                const relaysum_rows *post_weight_grad, const relaysum_rows *scale_grad,
+                                const relaysum_rows *weight_grad, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
 /* Text of the calling thread's last failure in the layer calls (""
  * after a call that succeeded). */
 const char *relaysum_layer_error(void);

@@ -77,3 +77,40 @@ def linear_backward(dy, x, w):
     dy = dy.astype(np.float64)
     return (np.einsum("ntc,nck->ntk", dy, w.astype(np.float64)),
             np.einsum("ntc,ntk->nck", dy, x.astype(np.float64)))
+
+
+def sigmoid(f):
+    with np.errstate(over="ignore"):
+        return 1.0 / (1.0 + np.exp(-f))
+
+
+def blocknorm(z, gate, residual, post_weight, scale, eps):
+    """(sum before it is rounded, the size of what is added to residual,
+    post_rstd); what follows is rmsnorm of the rounded sum."""
+    z = z.astype(np.float64)
+    u, post_rstd = rmsnorm(z, post_weight, eps)
+    g = 1.0 if gate is None else sigmoid(gate.astype(np.float64))
+    branch = scale.astype(np.float64)[:, None, None] * g * u
+    return residual.astype(np.float64) + branch, np.abs(branch), post_rstd
+
+
+def blocknorm_backward(dy, dsum, z, gate, s, post_rstd, rstd, post_weight, scale, weight, size=np.asarray):
+    """(ds, dz, dgate, weight, post weight and scale gradients) at the given s
+    and statistics.  With size=np.abs every term is taken as large as it is:
+    what roundings are measured against."""
+    f8 = np.float64
+    dy, z, s, w, pw = (size(v.astype(f8)) for v in (dy, z, s, weight[:, None, :], post_weight[:, None, :]))
+    sc = size(scale.astype(f8)[:, None, None])
+    sign = -1.0 if size is np.asarray else 1.0
+    inv, pinv = rstd.astype(f8)[:, :, None], post_rstd.astype(f8)[:, :, None]
+    sh, zh = s * inv, z * pinv
+    u = dy * w
+    ds = inv * (u + sign * sh * np.mean(u * sh, axis=2, keepdims=True))
+    if dsum is not None:
+        ds = size(dsum.astype(f8)) + ds
+    g, rest = (1.0, 0.0) if gate is None else (sigmoid(gate.astype(f8)), sigmoid(-gate.astype(f8)))
+    v = ds * sc * g * pw
+    dz = pinv * (v + sign * zh * np.mean(v * zh, axis=2, keepdims=True))
+    dgate = None if gate is None else ds * sc * zh * pw * g * rest
+    return (ds, dz, dgate, np.sum(dy * sh, axis=1), np.sum(ds * sc * g * zh, axis=1),
+            np.sum(ds * g * zh * pw, axis=(1, 2)))

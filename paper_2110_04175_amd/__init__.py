@@ -53,6 +53,7 @@ EXPORTED = (
     "relaysum_attention_backward_workspace", "relaysum_attention_backward",
     "relaysum_recurrence_chunks", "relaysum_recurrence_workspace", "relaysum_recurrence",
     "relaysum_recurrence_backward",
+    "relaysum_blocknorm", "relaysum_blocknorm_workspace", "relaysum_blocknorm_backward",
 )
 
 PATHS = ("tile", "dtree", "wide_dtree", "cluster", "wide", "two_pass", "dtree_seq",

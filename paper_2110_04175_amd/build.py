@@ -11,7 +11,8 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "relaysum.hip")
-SOURCES = [SRC] + [os.path.join(PKG, "csrc", name) for name in ("layer.hip", "attention.hip", "recurrence.hip")]
+SOURCES = [SRC] + [os.path.join(PKG, "csrc", name + ".hip")
+                   for name in ("layer", "attention", "recurrence", "blocknorm")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librelaysum.so")
 

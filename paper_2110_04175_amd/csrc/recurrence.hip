@@ -88,25 +88,6 @@ __device__ __forceinline__ Run then(const Run &p, const Run &r) {
     return Run{r.A < 0.0f ? r.A : p.A < 0.0f ? -1.0f : p.A * r.A, r.from(p.B)};
 }
 
-// a = 1 / (1 + e), c = e a with e = exp(-f): both to a few units of the last
-// place, also where the other is near 1.
-template <typename T>
-__device__ __forceinline__ void gates(float f, float &a, float &c) {
-    constexpr float kLog2e = 1.44269504088896340736f;
-    // Below -87 a is 2^-126 or less, above 200 it is 1; a NaN stays one.
-    f = f < -87.0f ? -87.0f : f > 200.0f ? 200.0f : f;
-    const float t = -f * kLog2e;
-    float e = __builtin_amdgcn_exp2f(t);
-    if (std::is_same<T, float>::value) {
-        // What the product with log2(e) lost.
-        const float lost = fmaf(-f, kLog2e, -t) + -f * 1.925963033500e-8f;
-        e = fmaf(e, lost * 0.69314718f, e);
-    }
-    a = __builtin_amdgcn_rcpf(1.0f + e);
-    if (std::is_same<T, float>::value) a = fmaf(a, fmaf(-a, 1.0f + e, 1.0f), a);
-    c = e * a;
-}
-
 template <typename T>
 __device__ __forceinline__ void load4(const T *p, int left, float (&v)[4]) {
     typedef T t4 __attribute__((ext_vector_type(4)));

@@ -1,6 +1,7 @@
 """Layer operators of n workers (the parts of ``relaysum.h`` behind the
-round): RMS norm with the residual's addition, products of packed rows and
-packing; attention; a gated recurrence; and their gradients.
+round): RMS norm with the residual's addition, or around a block with its
+gate and residual scale; products of packed rows and packing; attention; a
+gated recurrence; and their gradients.
 
 Activations are CUDA tensors [n, tokens, width] in float32, bfloat16 or
 float16 (heads: [n, tokens, heads, width]), weights and weight gradients float32 views into the rows of the
@@ -183,6 +184,12 @@ def _lib():
                                                    rows, vp, vp, sz, vp]),
             "relaysum_recurrence_backward": (ctypes.c_int, [i32, i64, i64, i32, vp, i64, rows, rows, rows,
                                                             rows, rows, vp, rows, rows, rows, vp, sz, vp]),
+            "relaysum_blocknorm": (ctypes.c_int, [i32, i64, i64, rows, rows, rows, vp, i64, vp, i64, vp, i64,
+                                                  f32, rows, packed, vp, vp, packed, vp]),
+            "relaysum_blocknorm_workspace": (i64, [i32, i64, i64]),
+            "relaysum_blocknorm_backward": (ctypes.c_int, [i32, i64, i64, rows, rows, rows, rows, packed, vp,
+                                                           vp, vp, i64, vp, i64, vp, i64, rows, rows, rows,
+                                                           rows, rows, rows, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(lib, name)
@@ -599,3 +606,83 @@ def recurrence_backward(dh, dlast, gate, x, saved, initial=None, starts=None):
                                             saved.data_ptr(), ro, rdx, rdi, ws, size, stream),
            "relaysum_recurrence_backward")
     return dgate, dx, dinitial
+
+
+# ---- norms around a block -----------------------------------------------------
+
+
+@functools.lru_cache(maxsize=1024)
+def _blocknorm_workspace(n: int, tokens: int, width: int) -> int:
+    return _lib().relaysum_blocknorm_workspace(n, tokens, width)
+
+
+def blocknorm(z, gate, residual, post_weight, scale, weight, eps: float = 1e-6, keep: bool = True):
+    """(sum, y, post_rstd, rstd, saved) with sum = residual + scale *
+    sigmoid(gate) * z * post_rstd * post_weight and y = sum * rstd * weight
+    packed by whole rows: the norm behind a block that gave z[n, tokens,
+    width], and the norm in front of the next one.  gate may be None (1 in its
+    place); post_weight and weight [n, width], scale [n] float32.  saved is
+    sum packed by 128, for blocknorm_backward (None without `keep`)."""
+    n, tokens, width = shape = _three(z, "z")
+    device, stream = _here()
+    rz = _rows(z, "z", shape, device)
+    rg = None if gate is None else _rows(gate, "gate", shape, device, z.dtype)
+    rr = _rows(residual, "residual", shape, device, z.dtype)
+    rp = _rows(post_weight, "post_weight", (n, width), device, torch.float32)
+    rw = _rows(weight, "weight", (n, width), device, torch.float32)
+    at, stride = _scalars(scale, "scale", n, device)
+    out, rs = _out(n, tokens, width, z.dtype, device)
+    y = Packed._new(n, tokens, width, 0, z)
+    saved = Packed._new(n, tokens, width, GROUP, z) if keep else None
+    post_rstd = torch.empty((n, tokens), dtype=torch.float32, device=device)
+    rstd = torch.empty((n, tokens), dtype=torch.float32, device=device)
+    _check(_lib().relaysum_blocknorm(n, tokens, width, rz, rg, rr, rp.data, rp.worker_stride, at, stride,
+                                     rw.data, rw.worker_stride, eps, rs, y._c(device, "y"),
+                                     post_rstd.data_ptr(), rstd.data_ptr(),
+                                     saved._c(device, "saved") if keep else None, stream),
+           "relaysum_blocknorm")
+    return out, y, post_rstd, rstd, saved
+
+
+def _scalars(t, name: str, n: int, device: int):
+    """(address, stride) of a float32 tensor [n] of any stride."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.shape != (n,) or t.dtype != torch.float32:
+        _refuse(t, name, (n,), device, torch.float32)
+    return t.data_ptr(), t.stride(0)
+
+
+def blocknorm_backward(dy, dsum, z, gate, saved: Packed, post_rstd, rstd, post_weight, scale, weight,
+                       post_weight_grad, scale_grad, weight_grad):
+    """(dz, dgate, ds): the gradients of z, gate (None without one) and
+    residual, as new tensors, from dy, that of y, dsum, that of the sum from
+    elsewhere (None: it is not used elsewhere), and blocknorm's arguments and
+    results.  The parameters' gradients overwrite post_weight_grad and
+    weight_grad [n, width] and scale_grad [n]."""
+    n, tokens, width = shape = _three(z, "z")
+    device, stream = _here()
+    rz, rdy = _rows(z, "z", shape, device), _rows(dy, "dy", shape, device, z.dtype)
+    rd = None if dsum is None else _rows(dsum, "dsum", shape, device, z.dtype)
+    rg = None if gate is None else _rows(gate, "gate", shape, device, z.dtype)
+    if saved.shape != (n, tokens, width):
+        raise ValueError(f"saved must hold rows [{n}, {tokens}, {width}], not {list(saved.shape)}")
+    for t, name in ((post_rstd, "post_rstd"), (rstd, "rstd")):
+        _rows(t, name, (n, tokens), device, torch.float32)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    rp = _rows(post_weight, "post_weight", (n, width), device, torch.float32)
+    rw = _rows(weight, "weight", (n, width), device, torch.float32)
+    at, stride = _scalars(scale, "scale", n, device)
+    rpg = _rows(post_weight_grad, "post_weight_grad", (n, width), device, torch.float32)
+    rwg = _rows(weight_grad, "weight_grad", (n, width), device, torch.float32)
+    gat, gstride = _scalars(scale_grad, "scale_grad", n, device)
+    dz, rdz = _out(n, tokens, width, z.dtype, device)
+    ds, rds = _out(n, tokens, width, z.dtype, device)
+    dgate, rdg = (None, None) if gate is None else _out(n, tokens, width, z.dtype, device)
+    lib = _lib()
+    ws, size, _keep = _workspace(_blocknorm_workspace(n, tokens, width), device)
+    _check(lib.relaysum_blocknorm_backward(n, tokens, width, rdy, rd, rz, rg, saved._c(device, "saved"),
+                                           post_rstd.data_ptr(), rstd.data_ptr(), rp.data,
+                                           rp.worker_stride, at, stride, rw.data, rw.worker_stride, rdz,
+                                           rdg, rds, rpg, Rows(gat, RELAYSUM_FLOAT, gstride, 0), rwg, ws,
+                                           size, stream), "relaysum_blocknorm_backward")
+    return dz, dgate, ds
