@@ -12,7 +12,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "relaysum.hip")
 SOURCES = [SRC] + [os.path.join(PKG, "csrc", name + ".hip")
-                   for name in ("layer", "attention", "recurrence", "blocknorm")]
+                   for name in ("layer", "attention", "attention_float", "attention_bfloat",
+                                "attention_half", "recurrence", "blocknorm")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librelaysum.so")
 

@@ -1,0 +1,897 @@
+// Attention of n workers' packed sequences, and its gradients, on CDNA4
+// (gfx950); the C ABI is in relaysum.h.
+//
+//   s_j = scale * q . k_j for the keys lo <= j < hi that a row sees,
+//   p_j = exp(s_j) / sum exp(s),  out = sum p_j v_j,  lse = log sum exp(s)
+//   dv_j = sum p_j dout,  ds_j = p_j (dout . v_j - dout . out),
+//   dq = scale * sum ds_j k_j,  dk_j = scale * sum ds_j q
+//
+// The query heads that share a key head are rows of one matrix: row
+// t * group + g is token t of the group's head g.  Their keys and values are
+// then read once, and the gradients of k and v sum over the group within a
+// workgroup, without atomics.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "attention_launch.hpp"
+#include "attention_tiles.hpp"
+#include "layer_call.hpp"
+
+namespace {
+
+using namespace attention;
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// Weights of binary16 are held times 2^7 (forward, where they reach 2^8 times
+// their largest) and 2^15 (backward, where they are at most 1): below 2^-14 it
+// loses bits.
+template <typename T>
+constexpr float kForwardShift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
+template <typename T>
+constexpr float kBackwardShift = std::is_same<T, _Float16>::value ? 15.0f : 0.0f;
+
+// The keys that a token sees.
+__device__ __forceinline__ int2 seen(const AttentionArgs &a, int64_t worker, int t) {
+    if (a.ranges) {
+        const int2 r = a.ranges[worker * a.range_stride + t];
+        return int2{max(r.x, 0), min(r.y, a.keys)};
+    }
+    const int64_t last = (int64_t)t + 1 + a.keys - a.tokens;
+    return int2{0, a.causal ? (int)max((int64_t)0, min(last, (int64_t)a.keys)) : a.keys};
+}
+
+// Which workers' key head and which tile of it a workgroup has.  Tiles of one
+// key head are put on one XCD, whose L2 then holds its keys; the last tiles,
+// which see the most keys of a causal sequence, go first.
+__device__ __forceinline__ void place(const AttentionArgs &a, unsigned block, unsigned &pair, int &tile) {
+    if (a.pairs % 8 == 0) {
+        const unsigned i = block / 8;
+        pair = block % 8 + i / a.tiles * 8;
+        tile = a.tiles - 1 - (int)(i % a.tiles);
+    } else {
+        pair = block % a.pairs;
+        tile = a.tiles - 1 - (int)(block / a.pairs);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ T *head_at(const Heads &h, int64_t worker, int64_t t, int head) {
+    return reinterpret_cast<T *>(h.data) + worker * h.ws + t * h.rs + head * h.hs;
+}
+
+// Over the 32 columns that a wave's lanes have twice.
+template <typename F>
+__device__ __forceinline__ int column_reduce(int v, F f) {
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) v = f(v, __shfl_xor(v, m));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// What a wave's columns see: whether a stretch of keys is seen by all, by some.
+struct Sight {
+    int least_lo, most_lo, least_hi, most_hi;
+    __device__ __forceinline__ bool whole(int j, int count) const { return most_lo <= j && j + count <= least_hi; }
+    __device__ __forceinline__ bool any(int j, int count) const { return least_lo < j + count && j < most_hi; }
+};
+
+__device__ __forceinline__ Sight sight_of(int lo, int hi, bool valid) {
+    const bool some = valid && lo < hi;
+    Sight s;
+    s.least_lo = column_reduce(some ? lo : INT_MAX, [](int x, int y) { return min(x, y); });
+    s.most_hi = column_reduce(some ? hi : 0, [](int x, int y) { return max(x, y); });
+    s.most_lo = column_reduce(valid ? (some ? lo : INT_MAX) : 0, [](int x, int y) { return max(x, y); });
+    s.least_hi = column_reduce(valid ? hi : INT_MAX, [](int x, int y) { return min(x, y); });
+    return s;
+}
+
+// ---- forward -----------------------------------------------------------------------
+//
+// One pass over the keys: `off` is the column's reference (a maximum of its
+// scores so far, in powers of two), l this lane's sum of the weights
+// 2^(s - off), acc the sum of weighted values.  The reference moves, and acc
+// with it, only when a score passes it by more than 2^8.
+template <typename T, int DP>
+struct Softmax {
+    typedef Tile<T, DP> L;
+    u4_t q[L::kOwn];
+    f16_t acc[L::kBlocks];
+    float m, off, l;
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int b = 0; b < L::kBlocks; ++b) acc[b] = f16_t{0};
+        m = -INFINITY;
+        off = l = 0.0f;
+    }
+
+    // 32 * NB keys from j on.  APART: what a column does not see is kept out of it
+    // also where it is not finite.
+    template <int NB, bool APART>
+    __device__ __forceinline__ void step(const AttentionArgs &a, const char *kt, const char *vt, int j, int lo, int hi,
+                                         bool whole, char *room, int lane) {
+        const int h = lane / 32;
+        float p[NB][16];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const f16_t s = dots<T, DP>(kt, 32 * b, q, lane);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[b][i] = s[i];
+        }
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = j + 32 * b + 8 * (i / 4) + 4 * h + i % 4;
+                    p[b][i] = key >= lo && key < hi ? p[b][i] : -INFINITY;
+                }
+        }
+        float top = p[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, p[b][i]);
+        top = fmaxf(top, other_half(top));
+        if (__ballot(top > m + 8.0f / a.dot_scale)) {
+            const float to = fmaxf(m, top);
+            const float moved = to == -INFINITY ? 0.0f : to * a.dot_scale - kForwardShift<T>;
+            const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(off - moved);
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < L::kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[b][i] *= f;
+            m = to;
+            off = moved;
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[b][i] = __builtin_amdgcn_exp2f(fmaf(p[b][i], a.dot_scale, -off));
+                l += p[b][i];
+            }
+        if (APART && !whole) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                add_rows_apart<T, DP>(acc, vt, 32 * b, p[b], room, lane, [&](int row) {
+                    const int key = j + 32 * b + row;
+                    return key >= lo && key < hi;
+                });
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) add_rows<T, DP>(acc, vt, 32 * b, Weights<T>(p[b]), lane);
+        }
+    }
+};
+
+template <typename T, int DP>
+constexpr int kKeyTile = sizeof(T) == 4 && DP >= 128 ? 32 : 64;
+
+// Waves of a SIMD that registers are given out for: as many as the loops leave
+// room for.
+template <typename T, int DP>
+constexpr int kForwardWaves = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4;
+template <typename T, int DP>
+constexpr int kQueryWaves = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 3;
+template <typename T, int DP>
+constexpr int kKeyWaves = sizeof(T) == 4 || DP > 128 ? 1 : 2;
+
+// A workgroup's 128 rows, 32 of each wave, and the keys that they see.
+struct RowTile {
+    unsigned pair;
+    int tile, wave, lane, kvh, row, t, head, lo, hi, first, end;
+    int64_t worker;
+    bool valid;
+    Sight sight;
+
+    __device__ __forceinline__ RowTile(const AttentionArgs &a, int (&most)[4][2]) {
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+        place(a, blockIdx.x, pair, tile);
+        worker = pair / a.kv;
+        kvh = (int)(pair % a.kv);
+        row = tile * 128 + wave * 32 + lane % 32;
+        valid = row < a.rows;
+        t = valid ? row / a.group : 0, head = kvh * a.group + (valid ? row % a.group : 0);
+        const int2 range = valid ? seen(a, worker, t) : int2{0, INT_MAX};
+        lo = range.x, hi = range.y;
+        sight = sight_of(lo, hi, valid);
+        if (lane == 0) most[wave][0] = sight.least_lo, most[wave][1] = sight.most_hi;
+        __syncthreads();
+        first = min(min(most[0][0], most[1][0]), min(most[2][0], most[3][0]));
+        end = max(max(most[0][1], most[1][1]), max(most[2][1], most[3][1]));
+    }
+};
+
+// Runs `step(half, j)` over tiles of BN keys from `first` to `end`: keys in
+// lds[half][0], values in lds[half][1], the next tile's on their way meanwhile.
+template <typename T, int DP, int BN, bool DIRECT, typename F>
+__device__ __forceinline__ void over_keys(const AttentionArgs &a, const RowTile &r, char (&lds)[2][2][BN * Tile<T, DP>::kRowBytes],
+                                          F step) {
+    const int begin = r.first / BN * BN, end = r.end;
+    if (r.first >= end) return;
+    const char *kbase = reinterpret_cast<const char *>(head_at<const T>(a.k, r.worker, 0, r.kvh));
+    const char *vbase = reinterpret_cast<const char *>(head_at<const T>(a.v, r.worker, 0, r.kvh));
+    const int64_t kr = a.k.rs * (int64_t)sizeof(T), vr = a.v.rs * (int64_t)sizeof(T);
+    Stage<T, DP, BN, 256, DIRECT> ks, vs;
+    const auto kat = [&](int x) { return x * kr; };
+    const auto vat = [&](int x) { return x * vr; };
+    const auto fetch = [&](int j, int half) {
+        const int rows = min(BN, a.keys - j);
+        if (rows < BN) {
+            ks.places(rows, threadIdx.x, kat);
+            vs.places(rows, threadIdx.x, vat);
+        }
+        ks.load(kbase + j * kr, lds[half][0], a.width, rows, threadIdx.x, kat);
+        vs.load(vbase + j * vr, lds[half][1], a.width, rows, threadIdx.x, vat);
+    };
+    const auto put = [&](int half) {
+        ks.put(lds[half][0], threadIdx.x);
+        vs.put(lds[half][1], threadIdx.x);
+    };
+    if (DIRECT && a.width < DP) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ks.clear(lds[i / 2][i % 2], threadIdx.x);
+        __syncthreads();
+    }
+    ks.places(BN, threadIdx.x, kat);
+    vs.places(BN, threadIdx.x, vat);
+    fetch(begin, 0);
+    put(0);
+    int half = 0;
+    for (int j = begin; j < end; j += BN, half ^= 1) {
+        __syncthreads();
+        const bool more = j + BN < end;
+        if (more) fetch(j + BN, half ^ 1);
+        step(half, j);
+        if (more) put(half ^ 1);
+    }
+}
+
+// A column's own row in chunks.
+template <typename T, int DP>
+__device__ __forceinline__ void load_own(const T *row, u4_t (&own)[Tile<T, DP>::kOwn], int width, bool valid, int lane) {
+#pragma unroll
+    for (int i = 0; i < Tile<T, DP>::kOwn; ++i)
+        own[i] = load_chunk<T>(row, (2 * i + lane / 32) * Tile<T, DP>::E, width, valid);
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(const AttentionArgs &a, const RowTile &r, const Softmax<T, DP> &st, float sum) {
+    if (!r.valid) return;
+    const bool empty = r.lo >= r.hi;
+    store_column<T>(head_at<T>(a.out, r.worker, r.t, r.head), a.width, st.acc, empty ? 0.0f : 1.0f / sum, r.lane);
+    if (a.lse && r.lane < 32)
+        a.lse[(r.worker * a.heads + r.head) * a.tokens + r.t] =
+            empty ? -INFINITY : kLn2 * (st.off + __builtin_amdgcn_logf(sum));
+}
+
+// The rows of a workgroup in whose sums something is not finite, once more, with
+// what they do not see kept out of them.
+template <typename T, int DP>
+__device__ __noinline__ void attention_apart(const AttentionArgs a, const RowTile r,
+                                             char (&lds)[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
+    constexpr int BN = kKeyTile<T, DP>;
+    Softmax<T, DP> st;
+    load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
+    st.clear();
+    over_keys<T, DP, BN, false>(a, r, lds, [&](int half, int j) {
+        for (int b = 0; b < BN; b += 32)
+            if (r.sight.any(j + b, 32))
+                st.template step<1, true>(a, lds[half][0] + b * Tile<T, DP>::kRowBytes, lds[half][1] + b * Tile<T, DP>::kRowBytes,
+                                          j + b, r.lo, r.hi, r.sight.whole(j + b, 32), room, r.lane);
+    });
+    store_rows(a, r, st, st.l + other_half(st.l));
+}
+
+template <typename T, int DP, bool DIRECT>
+__global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_kernel(AttentionArgs a) {
+    constexpr int BN = kKeyTile<T, DP>;
+    __shared__ __align__(16) char lds[2][2][BN * Tile<T, DP>::kRowBytes];
+    __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ int most[4][2];
+    const RowTile r(a, most);
+    Softmax<T, DP> st;
+    load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
+    st.clear();
+    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](int half, int j) {
+        if (r.sight.any(j, BN))
+            st.template step<BN / 32, false>(a, lds[half][0], lds[half][1], j, r.lo, r.hi, r.sight.whole(j, BN), nullptr, r.lane);
+    });
+    const float sum = st.l + other_half(st.l);
+    if (__syncthreads_or(r.valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY))))
+        attention_apart<T, DP>(a, r, lds, room[r.wave]);
+    else
+        store_rows(a, r, st, sum);
+}
+
+// Few rows: the keys are split over workgroups (parts) and their waves, each of
+// which walks through its own keys; waves join through LDS, parts in a second
+// kernel.
+template <typename T, int DP>
+constexpr int kSplitWaves = sizeof(T) == 4 && DP == 256 ? 2 : 4;   // whose tiles fit LDS
+
+template <typename T, int DP>
+__global__ __launch_bounds__((64 * kSplitWaves<T, DP>)) void attention_split_kernel(AttentionArgs a) {
+    typedef Tile<T, DP> L;
+    constexpr int W = kSplitWaves<T, DP>;
+    constexpr int kTile = 32 * L::kRowBytes;
+    // A wave's keys and values, and later its sums.
+    constexpr int kOwnBytes = 2 * kTile > 32 * DP * 4 ? 2 * kTile : 32 * DP * 4;
+    __shared__ __align__(16) char lds[W][kOwnBytes];
+    __shared__ __align__(16) char room[W][kApartBytes<T>];
+    __shared__ float soft[W][2][32];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const unsigned part = blockIdx.x % a.parts, at = blockIdx.x / a.parts;
+    const unsigned pair = at / a.tiles;
+    const int tile = (int)(at % a.tiles);
+    const int64_t worker = pair / a.kv;
+    const int kvh = (int)(pair % a.kv);
+    const int row = tile * 32 + lane % 32;
+    const bool valid = row < a.rows;
+    const int t = valid ? row / a.group : 0, head = kvh * a.group + (valid ? row % a.group : 0);
+    const int2 range = valid ? seen(a, worker, t) : int2{0, INT_MAX};
+    const int lo = range.x, hi = range.y;
+    const Sight sight = sight_of(lo, hi, valid);
+
+    Softmax<T, DP> st;
+    const T *qrow = head_at<const T>(a.q, worker, t, head);
+#pragma unroll
+    for (int i = 0; i < L::kOwn; ++i) st.q[i] = load_chunk<T>(qrow, (2 * i + lane / 32) * L::E, a.width, valid);
+    const T *kbase = head_at<const T>(a.k, worker, 0, kvh), *vbase = head_at<const T>(a.v, worker, 0, kvh);
+    // Keys of this part, 32 at a time in turn.
+    const int64_t from = (int64_t)part * a.span, to = min(from + a.span, (int64_t)sight.most_hi);
+    char *kt = lds[wave], *vt = kt + kTile;
+    Stage<T, DP, 32, 64, false> ks, vs;
+    float sum;
+    for (int pass = 0;; ++pass) {
+        st.clear();
+        const auto fetch = [&](int j) {
+            const int rows = min(32, a.keys - j);
+            ks.load(reinterpret_cast<const char *>(kbase + j * a.k.rs), kt, a.width, rows, lane,
+                    [&](int x) { return x * a.k.rs * (int64_t)sizeof(T); });
+            vs.load(reinterpret_cast<const char *>(vbase + j * a.v.rs), vt, a.width, rows, lane,
+                    [&](int x) { return x * a.v.rs * (int64_t)sizeof(T); });
+        };
+        int64_t j = from + 32 * wave;
+        while (j < to && !sight.any((int)j, 32)) j += 32 * W;
+        if (j < to) fetch((int)j);
+        while (j < to) {
+            ks.put(kt, lane);
+            vs.put(vt, lane);
+            wave_fence();
+            int64_t next = j + 32 * W;
+            while (next < to && !sight.any((int)next, 32)) next += 32 * W;
+            if (next < to) fetch((int)next);
+            if (pass)
+                st.template step<1, true>(a, kt, vt, (int)j, lo, hi, sight.whole((int)j, 32), room[wave], lane);
+            else
+                st.template step<1, false>(a, kt, vt, (int)j, lo, hi, sight.whole((int)j, 32), nullptr, lane);
+            wave_fence();
+            j = next;
+        }
+        sum = st.l + other_half(st.l);
+        if (pass || !__ballot(valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY)))) break;
+    }
+    // Waves join: every wave's sums [entry][column], times what brings them to
+    // the largest reference.  A wave without keys has none.
+    if (lane < 32) {
+        soft[wave][0][lane] = st.m == -INFINITY ? -INFINITY : st.off;
+        soft[wave][1][lane] = sum;
+    }
+    float *sums = reinterpret_cast<float *>(lds[wave]);
+    wave_fence();
+#pragma unroll
+    for (int b = 0; b < L::kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            sums[(32 * b + 8 * (i / 4) + 4 * (lane / 32) + i % 4) * 32 + lane % 32] = st.acc[b][i];
+    __syncthreads();
+    const int col = threadIdx.x / (2 * W);
+    const int r = tile * 32 + col;
+    if (r >= a.rows) return;
+    float top = -INFINITY, all = 0.0f, f[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, soft[w][0][col]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        f[w] = soft[w][0][col] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(soft[w][0][col] - top);
+        all += soft[w][1][col] * (soft[w][0][col] == -INFINITY ? 1.0f : f[w]);
+    }
+    const int rt = r / a.group, rh = kvh * a.group + r % a.group;
+    const int2 rr = seen(a, worker, rt);
+    const bool empty = rr.x >= rr.y;
+    const float inv = a.parts > 1 ? 1.0f : empty ? 0.0f : 1.0f / all;
+    const int64_t slot = ((int64_t)pair * a.rows + r) * a.parts + part;
+    for (int k = threadIdx.x % (2 * W); k < a.width; k += 2 * W) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (soft[w][0][col] != -INFINITY) v += reinterpret_cast<const float *>(lds[w])[k * 32 + col] * f[w];
+        // All of its scores are -infinity: 0 / 0.
+        if (a.parts > 1) a.part_out[slot * a.width + k] = v;
+        else head_at<T>(a.out, worker, rt, rh)[k] = (T)(empty ? 0.0f : v * inv);
+    }
+    if (threadIdx.x % (2 * W)) return;
+    if (a.parts > 1) a.part_soft[slot] = float2{top, all};
+    else if (a.lse)
+        a.lse[(worker * a.heads + rh) * a.tokens + rt] =
+            empty ? -INFINITY : kLn2 * ((top == -INFINITY ? 0.0f : top) + __builtin_amdgcn_logf(all));
+}
+
+// Parts of a row join: a wave each.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
+    const int lane = threadIdx.x % kWave;
+    const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    if (at >= (int64_t)a.pairs * a.rows) return;
+    const int64_t pair = at / a.rows, worker = pair / a.kv;
+    const int r = (int)(at % a.rows), t = r / a.group, head = (int)(pair % a.kv) * a.group + r % a.group;
+    const int2 range = seen(a, worker, t);
+    const bool empty = range.x >= range.y;
+    const float2 *soft = a.part_soft + at * a.parts;
+    float top = -INFINITY, all = 0.0f;
+    for (int p = lane; p < a.parts; p += kWave) top = fmaxf(top, soft[p].x);
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    for (int p = lane; p < a.parts; p += kWave)
+        all += soft[p].y * (soft[p].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(soft[p].x - top));
+#pragma unroll
+    for (int m = 1; m < kWave; m *= 2) all += __shfl_xor(all, m);
+    const float inv = 1.0f / all;
+    T *out = head_at<T>(a.out, worker, t, head);
+    for (int k = lane; k < a.width; k += kWave) {
+        float v = 0.0f;
+        for (int p = 0; p < a.parts; ++p)
+            if (soft[p].x != -INFINITY)
+                v += a.part_out[(at * a.parts + p) * a.width + k] * __builtin_amdgcn_exp2f(soft[p].x - top);
+        out[k] = (T)(empty ? 0.0f : v * inv);
+    }
+    if (a.lse && lane == 0)
+        a.lse[(worker * a.heads + head) * a.tokens + t] =
+            empty ? -INFINITY : kLn2 * ((top == -INFINITY ? 0.0f : top) + __builtin_amdgcn_logf(all));
+}
+
+// ---- backward ----------------------------------------------------------------------
+
+// delta = dout . out of every row, 16 lanes each; for binary16 also the largest
+// squared norms of the rows of dout that see something and of v's.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
+    __shared__ float red[2][16];
+    const int64_t worker = blockIdx.x / a.parts;
+    const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x % 16, slot = threadIdx.x / 16;
+    float most_dout = 0.0f, most_v = 0.0f;
+    const int64_t rows = (int64_t)a.tokens * a.heads;
+    for (int64_t r = (int64_t)part * 16 + slot; r < rows; r += (int64_t)a.parts * 16) {
+        const int t = (int)(r / a.heads), head = (int)(r % a.heads);
+        const T *x = head_at<const T>(a.dout, worker, t, head), *y = head_at<const T>(a.out, worker, t, head);
+        float dot = 0.0f, norm = 0.0f;
+        for (int k = lane * 8; k < a.width; k += 128) {
+            float u[8], v[8];
+            load8(x + k, a.width - k, u);
+            load8(y + k, a.width - k, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dot = fmaf(u[i], v[i], dot), norm = fmaf(u[i], u[i], norm);
+        }
+        dot = row_reduce<16, float, pick_sum>(dot, nullptr);
+        if (lane == 0) a.delta[(worker * a.heads + head) * a.tokens + t] = dot;
+        if (std::is_same<T, _Float16>::value) {
+            norm = row_reduce<16, float, pick_sum>(norm, nullptr);
+            const int2 s = seen(a, worker, t);
+            if (s.x < s.y && norm < INFINITY) most_dout = fmaxf(most_dout, norm);
+        }
+    }
+    if (std::is_same<T, _Float16>::value) {
+        const int64_t vrows = (int64_t)a.keys * a.kv;
+        for (int64_t r = (int64_t)part * 16 + slot; r < vrows; r += (int64_t)a.parts * 16) {
+            const T *x = head_at<const T>(a.v, worker, r / a.kv, (int)(r % a.kv));
+            float norm = 0.0f;
+            for (int k = lane * 8; k < a.width; k += 128) {
+                float u[8];
+                load8(x + k, a.width - k, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) norm = fmaf(u[i], u[i], norm);
+            }
+            norm = row_reduce<16, float, pick_sum>(norm, nullptr);
+            if (norm < INFINITY) most_v = fmaxf(most_v, norm);
+        }
+        if (lane == 0) red[0][slot] = most_dout, red[1][slot] = most_v;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int i = 1; i < 16; ++i) most_dout = fmaxf(most_dout, red[0][i]), most_v = fmaxf(most_v, red[1][i]);
+            a.largest[blockIdx.x] = float2{most_dout, most_v};
+        }
+    }
+}
+
+// What blocks of 32 rows see.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_bounds_kernel(AttentionArgs a, int64_t total) {
+    const int64_t at = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    if (at >= total) return;
+    const int64_t per = (a.rows + 31) / 32, worker = at / per;
+    const int row = (int)(at % per) * 32 + threadIdx.x % 32;
+    int2 s = row < a.rows ? seen(a, worker, row / a.group) : int2{INT_MAX, 0};
+    int4 b = {row < a.rows ? s.x : INT_MAX, row < a.rows ? s.x : 0, row < a.rows ? s.y : 0, s.y};
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        b.x = min(b.x, __shfl_xor(b.x, m));
+        b.y = max(b.y, __shfl_xor(b.y, m));
+        b.z = min(b.z, __shfl_xor(b.z, m));
+        b.w = max(b.w, __shfl_xor(b.w, m));
+    }
+    if (threadIdx.x % 32 == 0) a.bounds[at] = b;
+}
+
+// Least and most lo, least and most hi of 32 rows; rows behind the last see nothing.
+__device__ __forceinline__ Sight block_sight(const AttentionArgs &a, int64_t worker, int block) {
+    if (a.ranges) {
+        const int4 b = a.bounds[worker * a.bound_stride + block];
+        return Sight{b.x, b.y, b.z, b.w};
+    }
+    const int last = min(block * 32 + 31, a.rows - 1);
+    return Sight{0, 0, block * 32 + 32 > a.rows ? 0 : seen(a, worker, block * 32 / a.group).y,
+                 seen(a, worker, last / a.group).y};
+}
+
+// The power of two that ds is held times in binary16, so that its largest is
+// below 2^15: |ds| <= 2 |dout| |v|.  Every thread of the workgroup takes part.
+template <typename T>
+__device__ __forceinline__ float gradient_scale(const AttentionArgs &a, int64_t worker, float2 *red) {
+    if (!std::is_same<T, _Float16>::value) return 1.0f;
+    float2 m = {0.0f, 0.0f};
+    for (int p = threadIdx.x; p < a.parts; p += 256) {
+        const float2 v = a.largest[worker * a.parts + p];
+        m.x = fmaxf(m.x, v.x), m.y = fmaxf(m.y, v.y);
+    }
+#pragma unroll
+    for (int s = 1; s < kWave; s *= 2) m.x = fmaxf(m.x, __shfl_xor(m.x, s)), m.y = fmaxf(m.y, __shfl_xor(m.y, s));
+    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = m;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) m.x = fmaxf(m.x, red[w].x), m.y = fmaxf(m.y, red[w].y);
+    const float bound = 2.0f * sqrtf(m.x) * sqrtf(m.y);
+    if (!(bound > 0.0f)) return 1.0f;
+    return ldexpf(1.0f, 13 - max(-80, min(80, ilogbf(bound))));
+}
+
+// The gradient of q: as forward, with the weights known from lse.
+template <typename T, int DP>
+struct QueryGradient {
+    typedef Tile<T, DP> L;
+    u4_t q[L::kOwn], dout[L::kOwn];
+    f16_t acc[L::kBlocks];
+    float off, delta, up;
+
+    __device__ __forceinline__ void start(const AttentionArgs &a, const RowTile &r, float factor) {
+        load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), q, a.width, r.valid, r.lane);
+        load_own<T, DP>(head_at<const T>(a.dout, r.worker, r.t, r.head), dout, a.width, r.valid, r.lane);
+        const int64_t stat = (r.worker * a.heads + r.head) * a.tokens + r.t;
+        off = r.valid ? a.lse[stat] * kLog2e : 0.0f, delta = r.valid ? a.delta[stat] : 0.0f;
+        up = factor;
+#pragma unroll
+        for (int b = 0; b < L::kBlocks; ++b) acc[b] = f16_t{0};
+    }
+    // 32 keys from j on.
+    template <bool APART>
+    __device__ __forceinline__ void step(const AttentionArgs &a, const RowTile &r, const char *kt, const char *vt, int j,
+                                         char *room) {
+        const bool whole = r.sight.whole(j, 32);
+        const f16_t s = dots<T, DP>(kt, 0, q, r.lane);
+        const f16_t dp = dots<T, DP>(vt, 0, dout, r.lane);
+        float ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off)) * up * (dp[i] - delta);
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = j + 8 * (i / 4) + 4 * (r.lane / 32) + i % 4;
+                ds[i] = key >= r.lo && key < r.hi ? ds[i] : 0.0f;
+            }
+        }
+        if (APART && !whole)
+            add_rows_apart<T, DP>(acc, kt, 0, ds, room, r.lane, [&](int x) { return j + x >= r.lo && j + x < r.hi; });
+        else
+            add_rows<T, DP>(acc, kt, 0, Weights<T>(ds), r.lane);
+    }
+    __device__ __forceinline__ void store(const AttentionArgs &a, const RowTile &r) const {
+        if (r.valid) store_column<T>(head_at<T>(a.dq, r.worker, r.t, r.head), a.width, acc, a.scale / up, r.lane);
+    }
+};
+
+template <typename T, int DP, bool DIRECT, bool APART>
+__device__ __forceinline__ void dq_over_keys(const AttentionArgs &a, const RowTile &r, QueryGradient<T, DP> &g,
+                                             char (&lds)[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
+    constexpr int BN = kKeyTile<T, DP>, kRowBytes = Tile<T, DP>::kRowBytes;
+    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](int half, int j) {
+#pragma unroll
+        for (int b = 0; b < BN; b += 32)
+            if (r.sight.any(j + b, 32))
+                g.template step<APART>(a, r, lds[half][0] + b * kRowBytes, lds[half][1] + b * kRowBytes, j + b, room);
+    });
+}
+
+template <typename T, int DP>
+__device__ __noinline__ void attention_dq_apart(const AttentionArgs a, const RowTile r, float up,
+                                                char (&lds)[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
+    QueryGradient<T, DP> g;
+    g.start(a, r, up);
+    dq_over_keys<T, DP, false, true>(a, r, g, lds, room);
+    g.store(a, r);
+}
+
+template <typename T, int DP, bool DIRECT>
+__global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel(AttentionArgs a) {
+    __shared__ __align__(16) char lds[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
+    __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ int most[4][2];
+    __shared__ float2 red[4];
+    const RowTile r(a, most);
+    const float up = gradient_scale<T>(a, r.worker, red);
+    QueryGradient<T, DP> g;
+    g.start(a, r, up);
+    dq_over_keys<T, DP, DIRECT, false>(a, r, g, lds, nullptr);
+    if (__syncthreads_or(r.valid && not_finite(g.acc)))
+        attention_dq_apart<T, DP>(a, r, up, lds, room[r.wave]);
+    else
+        g.store(a, r);
+}
+
+// The gradients of k and v: columns are keys, 128 of a workgroup, and rows the
+// queries that see them, 32 at a time.
+constexpr int kRowTile = 32;
+
+template <typename T, int DP>
+struct KeyLds {
+    char rows[2][2][kRowTile * Tile<T, DP>::kRowBytes];   // q, dout
+    float stats[2][2][kRowTile];                          // lse in powers of two, delta
+    int2 sees[2][kRowTile];
+};
+
+template <typename T, int DP>
+struct KeyGradient {
+    typedef Tile<T, DP> L;
+    u4_t k[L::kOwn], v[L::kOwn];
+    f16_t dk[L::kBlocks], dv[L::kBlocks];
+    int64_t worker;
+    int kvh, j0, mine, key, lane;
+    bool valid;
+    float up;
+
+    __device__ __forceinline__ void start(const AttentionArgs &a, unsigned pair, int tile, float factor) {
+        lane = threadIdx.x % kWave;
+        worker = pair / a.kv;
+        kvh = (int)(pair % a.kv);
+        j0 = tile * 128, mine = j0 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * 32;
+        key = mine + lane % 32;
+        valid = key < a.keys;
+        up = factor;
+        load_own<T, DP>(head_at<const T>(a.k, worker, valid ? key : 0, kvh), k, a.width, valid, lane);
+        load_own<T, DP>(head_at<const T>(a.v, worker, valid ? key : 0, kvh), v, a.width, valid, lane);
+#pragma unroll
+        for (int b = 0; b < L::kBlocks; ++b) dk[b] = dv[b] = f16_t{0};
+    }
+
+    template <bool APART>
+    __device__ __forceinline__ void step(const AttentionArgs &a, const KeyLds<T, DP> &lds, int half, bool whole, char *room) {
+        const float factor = ldexpf(up, -(int)kBackwardShift<T>);
+        const f16_t s = dots<T, DP>(lds.rows[half][0], 0, k, lane);
+        const f16_t dp = dots<T, DP>(lds.rows[half][1], 0, v, lane);
+        float p[16], ds[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f4_t off = *reinterpret_cast<const f4_t *>(&lds.stats[half][0][8 * g + 4 * (lane / 32)]);
+            const f4_t delta = *reinterpret_cast<const f4_t *>(&lds.stats[half][1][8 * g + 4 * (lane / 32)]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 4 * g + r;
+                p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off[r]));
+                ds[i] = p[i] * factor * (dp[i] - delta[r]);
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int2 x = lds.sees[half][8 * (i / 4) + 4 * (lane / 32) + i % 4];
+                const bool there = key >= x.x && key < x.y;
+                p[i] = there ? p[i] : 0.0f;
+                ds[i] = there ? ds[i] : 0.0f;
+            }
+        }
+        if (APART && !whole) {
+            const auto there = [&](int r) { return key >= lds.sees[half][r].x && key < lds.sees[half][r].y; };
+            add_rows_apart<T, DP>(dv, lds.rows[half][1], 0, p, room, lane, there);
+            add_rows_apart<T, DP>(dk, lds.rows[half][0], 0, ds, room, lane, there);
+        } else {
+            add_rows<T, DP>(dv, lds.rows[half][1], 0, Weights<T>(p), lane);
+            add_rows<T, DP>(dk, lds.rows[half][0], 0, Weights<T>(ds), lane);
+        }
+    }
+
+    template <bool DIRECT, bool APART>
+    __device__ __forceinline__ void over_rows(const AttentionArgs &a, KeyLds<T, DP> &lds, char *room) {
+        constexpr int BR = kRowTile;
+        const int blocks = (a.rows + BR - 1) / BR;
+        // Without ranges the rows that see a key are all from one on.
+        int block = 0;
+        if (!a.ranges && a.causal) block = (int)(max((int64_t)0, (int64_t)j0 + a.tokens - a.keys) * a.group / BR);
+        const char *qbase = reinterpret_cast<const char *>(head_at<const T>(a.q, worker, 0, kvh * a.group));
+        const char *obase = reinterpret_cast<const char *>(head_at<const T>(a.dout, worker, 0, kvh * a.group));
+        Stage<T, DP, BR, 256, DIRECT> qs, os;
+        // A group that divides 32 has its rows at the same places of every block.
+        const bool steady = BR % a.group == 0;
+        float2 stat = {0.0f, 0.0f};
+        int2 range = {0, 0};
+        const auto next = [&](int b) {
+            if (!a.ranges) return b;
+            for (; b < blocks; b += kWave) {
+                bool any = false;
+                if (b + lane < blocks) any = block_sight(a, worker, b + lane).any(j0, 128);
+                const unsigned long long m = __ballot(any);
+                if (m) return b + __ffsll((long long)m) - 1;
+            }
+            return blocks;
+        };
+        const auto fetch = [&](int b, int half) {
+            const int row0 = b * BR, t0 = row0 / a.group, rows = min(BR, a.rows - row0);
+            const auto at = [&](const Heads &x) {
+                return [&, rs = x.rs, hs = x.hs](int r) {
+                    const int row = row0 + r, t = row / a.group;
+                    return ((t - t0) * rs + (row - t * a.group) * hs) * (int64_t)sizeof(T);
+                };
+            };
+            if (!steady || rows < BR) {
+                qs.places(rows, threadIdx.x, at(a.q));
+                os.places(rows, threadIdx.x, at(a.dout));
+            }
+            qs.load(qbase + t0 * a.q.rs * (int64_t)sizeof(T), lds.rows[half][0], a.width, rows, threadIdx.x, at(a.q));
+            os.load(obase + t0 * a.dout.rs * (int64_t)sizeof(T), lds.rows[half][1], a.width, rows, threadIdx.x, at(a.dout));
+            if (threadIdx.x < BR) {
+                const int row = row0 + threadIdx.x;
+                stat = float2{0.0f, 0.0f}, range = int2{0, 0};
+                if (row < a.rows) {
+                    const int t = row / a.group;
+                    const int64_t s = (worker * a.heads + kvh * a.group + row % a.group) * a.tokens + t;
+                    stat = float2{a.lse[s] * kLog2e - kBackwardShift<T>, a.delta[s]};
+                    range = seen(a, worker, t);
+                }
+            }
+        };
+        const auto put = [&](int half) {
+            qs.put(lds.rows[half][0], threadIdx.x);
+            os.put(lds.rows[half][1], threadIdx.x);
+            if (threadIdx.x < BR) {
+                lds.stats[half][0][threadIdx.x] = stat.x;
+                lds.stats[half][1][threadIdx.x] = stat.y;
+                lds.sees[half][threadIdx.x] = range;
+            }
+        };
+        if (DIRECT && a.width < DP) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) qs.clear(lds.rows[i / 2][i % 2], threadIdx.x);
+            __syncthreads();
+        }
+        block = next(block);
+        if (block >= blocks) return;
+        if (steady) {
+            const auto at = [&](const Heads &x) {
+                return [&, rs = x.rs, hs = x.hs](int r) { return (r / a.group * rs + r % a.group * hs) * (int64_t)sizeof(T); };
+            };
+            qs.places(BR, threadIdx.x, at(a.q));
+            os.places(BR, threadIdx.x, at(a.dout));
+        }
+        fetch(block, 0);
+        put(0);
+        for (int half = 0; block < blocks; half ^= 1) {
+            __syncthreads();
+            const int then = next(block + 1);
+            if (then < blocks) fetch(then, half ^ 1);
+            const Sight sight = block_sight(a, worker, block);
+            if (sight.any(mine, 32)) step<APART>(a, lds, half, sight.whole(mine, 32), room);
+            if (then < blocks) put(half ^ 1);
+            block = then;
+        }
+    }
+
+    __device__ __forceinline__ void store(const AttentionArgs &a) const {
+        if (!valid) return;
+        store_column<T>(head_at<T>(a.dk, worker, key, kvh), a.width, dk, a.scale / up, lane);
+        store_column<T>(head_at<T>(a.dv, worker, key, kvh), a.width, dv, ldexpf(1.0f, -(int)kBackwardShift<T>), lane);
+    }
+};
+
+template <typename T, int DP>
+__device__ __noinline__ void attention_dkv_apart(const AttentionArgs a, unsigned pair, int tile, float up, KeyLds<T, DP> &lds,
+                                                 char *room) {
+    KeyGradient<T, DP> g;
+    g.start(a, pair, tile, up);
+    g.template over_rows<false, true>(a, lds, room);
+    g.store(a);
+}
+
+template <typename T, int DP, bool DIRECT>
+__global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(AttentionArgs a) {
+    __shared__ __align__(16) KeyLds<T, DP> lds;
+    __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ float2 red[4];
+    unsigned pair;
+    int tile;
+    place(a, blockIdx.x, pair, tile);
+    tile = a.tiles - 1 - tile;   // the first keys are seen by the most rows
+    const float up = gradient_scale<T>(a, pair / a.kv, red);
+    KeyGradient<T, DP> g;
+    g.start(a, pair, tile, up);
+    g.template over_rows<DIRECT, false>(a, lds, nullptr);
+    if (__syncthreads_or(g.valid && (not_finite(g.dk) || not_finite(g.dv))))
+        attention_dkv_apart<T, DP>(a, pair, tile, up, lds, room[threadIdx.x / kWave]);
+    else
+        g.store(a);
+}
+
+// ---- launches ---------------------------------------------------------------------------
+
+template <typename F>
+void with_width(int64_t width, F f) {
+    if (width <= 64) f(Int<64>());
+    else if (width <= 128) f(Int<128>());
+    else f(Int<256>());
+}
+
+// Whether rows start on 16 bytes and have whole chunks of them, and a tile's
+// places fit 32 bits.
+bool direct(const Heads &h, int64_t bytes, int64_t width) {
+    const auto whole = [&](int64_t entries) { return entries * bytes % 16 == 0; };
+    return (uintptr_t)h.data % 16 == 0 && whole(width) && whole(h.ws) && whole(h.rs) && whole(h.hs) &&
+           h.rs * bytes < 1 << 24 && h.hs * bytes < 1 << 24;
+}
+
+}  // namespace
+
+template <typename T>
+void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, hipStream_t st) {
+    with_width(a.width, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        if (p.split)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_split_kernel<T, DP>), dim3((unsigned)p.blocks),
+                               dim3(64 * kSplitWaves<T, DP>), 0, st, a);
+        else if (direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+    });
+    if (p.parts > 1)
+        hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)tiles((int64_t)a.pairs * a.rows, 4)), dim3(256), 0, st, a);
+}
+
+template <typename T>
+void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_t st) {
+    if (a.ranges && a.tokens) {
+        const int64_t total = (a.range_stride ? n : 1) * tiles(a.rows, 32);
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_bounds_kernel<T>), dim3((unsigned)tiles(total, 8)), dim3(256), 0, st, a, total);
+    }
+    if (a.tokens)
+        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)(n * a.parts)), dim3(256), 0, st, a);
+    with_width(a.width, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        const dim3 keys_grid((unsigned)(a.pairs * tiles(a.keys, 128))), rows_grid((unsigned)(a.pairs * tiles(a.rows, 128)));
+        a.tiles = (int32_t)tiles(a.keys, 128);
+        if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
+        else if (a.keys)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);
+        a.tiles = (int32_t)tiles(a.rows, 128);
+        if (a.tokens && direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, true>), rows_grid, dim3(256), 0, st, a);
+        else if (a.tokens)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
+    });
+}

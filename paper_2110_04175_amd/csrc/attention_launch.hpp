@@ -1,0 +1,52 @@
+// What the attention calls and the kernels of each type share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#define RELAYSUM_HIDDEN __attribute__((visibility("hidden")))
+
+namespace attention {
+
+// Heads of n workers: entry k of head h of row t of worker i is entry
+// i * ws + t * rs + h * hs + k.
+struct Heads {
+    char *data;
+    int64_t ws, rs, hs;
+};
+
+struct AttentionArgs {
+    Heads q, k, v, out;
+    Heads dout, dq, dk, dv;
+    float *lse;                // [n][heads][tokens]
+    float *delta;              // [n][heads][tokens]: dout . out
+    float2 *largest;           // [n][parts]: squared norms of rows of dout and v
+    int4 *bounds;              // [n or 1][ceil(rows / 32)]: least and most lo, least and most hi
+    const int2 *ranges;
+    float *part_out;           // [pairs][rows][parts][width]
+    float2 *part_soft;         // [pairs][rows][parts]
+    int64_t range_stride;      // rows between workers' ranges; 0: all have the same
+    int64_t bound_stride;
+    int32_t tokens, keys, heads, kv, group, width, rows;   // rows = tokens * group
+    int32_t causal, tiles, parts, span;
+    uint32_t pairs;            // n * kv
+    float scale, dot_scale;    // dot_scale = scale * log2(e)
+};
+
+// Tiles of the forward pass, or the parts that the keys are split into.
+struct ForwardPlan {
+    int64_t blocks;
+    int32_t tiles, parts, span;
+    bool split;
+    size_t workspace;
+};
+
+// Queue the kernels of a call; T is float, __bf16 or _Float16.
+template <typename T>
+RELAYSUM_HIDDEN void launch_attention(const AttentionArgs &a, const ForwardPlan &p, hipStream_t st);
+template <typename T>
+RELAYSUM_HIDDEN void launch_attention_backward(AttentionArgs a, int32_t n, hipStream_t st);
+
+}  // namespace attention

@@ -21,13 +21,6 @@ typedef float f16_t __attribute__((ext_vector_type(16)));
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef short s4_t __attribute__((ext_vector_type(4)));
 
-// Heads of n workers: entry k of head h of row t of worker i is entry
-// i * ws + t * rs + h * hs + k.
-struct Heads {
-    char *data;
-    int64_t ws, rs, hs;
-};
-
 // Rows of DP entries (the heads' width rounded up) of 16-byte chunks.
 template <typename T, int DP>
 struct Tile {
@@ -236,30 +229,61 @@ __device__ __forceinline__ float other_half(float v) {
     return float_of(threadIdx.x % 64 < 32 ? r.y : r.x);
 }
 
-// R rows of a tile on their way from memory into LDS through registers:
-// NT threads, any alignment.
-template <typename T, int DP, int R, int NT>
+// R rows of a tile on their way from memory into LDS, by NT threads.  DIRECT:
+// rows start on 16 bytes and have whole chunks, which are copied without
+// registers in between; a lane's LDS place is fixed, so it takes the chunk that
+// belongs there.  Rows that are not there then repeat the last one, and chunks
+// behind the width stay as they are (zeros from clear()).  Otherwise through
+// registers, at any alignment, zeros in both places.
+template <typename T, int DP, int R, int NT, bool DIRECT>
 struct Stage {
     typedef Tile<T, DP> L;
-    static constexpr int kCount = (R * L::kChunks + NT - 1) / NT;
-    u4_t v[kCount];
+    static constexpr int kCount = R * L::kChunks / NT;
+    static_assert(R * L::kChunks % NT == 0, "every thread has as many chunks");
+    u4_t v[DIRECT ? 1 : kCount];
+    unsigned off[DIRECT ? kCount : 1];
 
-    // row(r): the address of row r, or NULL.
+    static __device__ __forceinline__ void clear(char *tile, int thread) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) *reinterpret_cast<u4_t *>(tile + (i * NT + thread) * 16) = u4_t{0, 0, 0, 0};
+    }
+
+    // Where a thread's chunks lie, from a tile's base on: at(r) is where row r
+    // starts, in bytes.  Of `rows` rows, at least one.
     template <typename F>
-    __device__ __forceinline__ void load(int width, int thread, F row) {
+    __device__ __forceinline__ void places(int rows, int thread, F at) {
+        if (!DIRECT) return;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const int u = i * NT + thread;
-            if (R * L::kChunks % NT && u >= R * L::kChunks) break;
-            const T *p = row(u / L::kChunks);
-            v[i] = load_chunk<T>(p, u % L::kChunks * L::E, width, p != nullptr);
+            const int u = i * NT + thread, r = u / L::kChunks;
+            off[i] = (unsigned)at(min(r, rows - 1)) + (u % L::kChunks ^ L::swizzle(r)) * 16;
         }
     }
-    __device__ __forceinline__ void store(char *tile, int thread) const {
+
+    // Starts the way of a tile whose places are known.
+    template <typename F>
+    __device__ __forceinline__ void load(const char *base, char *tile, int width, int rows, int thread, F at) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int u = i * NT + thread, r = u / L::kChunks, place = u % L::kChunks;
+            if (DIRECT) {
+                // A wave's first place in LDS.
+                char *to = tile + (i * NT + __builtin_amdgcn_readfirstlane(thread & ~63)) * 16;
+                if ((place ^ L::swizzle(r)) * L::E < width) copy_to_lds(base + off[i], to);
+            } else {
+                v[i] = load_chunk<T>(reinterpret_cast<const T *>(base + at(min(r, rows - 1))), place * L::E, width, r < rows);
+            }
+        }
+    }
+    // Ends it: with a barrier behind, all threads can read the tile.
+    __device__ __forceinline__ void put(char *tile, int thread) const {
+        if (DIRECT) {
+            wait_for_copies();
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int u = i * NT + thread;
-            if (R * L::kChunks % NT && u >= R * L::kChunks) break;
             *reinterpret_cast<u4_t *>(tile + L::at(u / L::kChunks, u % L::kChunks)) = v[i];
         }
     }
