@@ -130,20 +130,25 @@ ForwardPlan plan_forward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
 }
 
 struct BackwardPlan {
-    int32_t parts;
-    size_t delta, largest, bounds;   // offsets
+    int32_t norms, parts;
+    size_t stats, largest, bounds, sums;   // offsets
     size_t workspace;
 };
 
-BackwardPlan plan_backward(int32_t n, int64_t tokens, int32_t heads, int32_t kv, int32_t type) {
+BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t heads, int32_t kv, int64_t width, int32_t type) {
     BackwardPlan p{};
-    const int64_t rows = tokens * heads;
-    p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles(rows, 64), std::max<int64_t>(1, 8 * kCus / n)));
-    p.parts = std::min(p.parts, 256);
+    const int64_t rows = tokens * heads, pairs = (int64_t)n * kv, blocks = pairs * tiles(keys, 128);
+    p.norms = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles(rows, 64), std::max<int64_t>(1, 8 * kCus / n)));
+    p.norms = std::min(p.norms, 256);
+    // Rows of a key head are split over workgroups where there are few of them, at
+    // least four tiles each.
+    p.parts = 1;
+    while (p.parts < 32 && blocks * p.parts < 3 * kCus && 8 * p.parts * 64 <= tokens * (heads / kv)) p.parts *= 2;
     size_t at = 0;
-    p.delta = at, at += tiles((size_t)n * rows * 4, 16) * 16;
-    p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.parts * 8, 16) * 16 : 0;
+    p.stats = at, at += tiles((size_t)n * rows * 8, 16) * 16;
+    p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.norms * 8, 16) * 16 : 0;
     p.bounds = at, at += (size_t)n * tiles(tokens * (heads / kv), 32) * 16;
+    p.sums = at, at += p.parts > 1 ? (size_t)pairs * keys * p.parts * 2 * width * 4 : 0;
     p.workspace = at;
     return p;
 }
@@ -163,6 +168,8 @@ AttentionArgs attention_args(int32_t n, int64_t tokens, int64_t keys, int32_t he
     a.tokens = (int32_t)tokens, a.keys = (int32_t)keys, a.heads = heads, a.kv = kv, a.group = heads / kv;
     a.width = (int32_t)width, a.rows = (int32_t)(tokens * a.group), a.causal = causal != 0;
     a.pairs = (uint32_t)n * kv;
+    while ((int64_t)1 << a.group_shift < a.group) ++a.group_shift;
+    a.group_factor = (uint32_t)(((((uint64_t)1 << a.group_shift) - a.group) << 32) / a.group + 1);
     a.scale = scale, a.dot_scale = scale * kLog2e;
     return a;
 }
@@ -245,7 +252,7 @@ int64_t relaysum_attention_backward_workspace(int32_t n, int64_t tokens, int64_t
         return -1;
     }
     g_error[0] = '\0';
-    return (int64_t)plan_backward(n, tokens, heads, kv_heads, type).workspace;
+    return (int64_t)plan_backward(n, tokens, keys, heads, kv_heads, width, type).workspace;
 }
 
 int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t heads, int32_t kv_heads,
@@ -270,9 +277,9 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
         c.heads("dv", dv, type, n, keys, kv_heads, width, true);
         if (!(scale > 0.0f && scale < INFINITY)) c.fail(refuse("scale must be positive"));
         if (c.code == RELAYSUM_OK) {
-            p = plan_backward(n, tokens, heads, kv_heads, type);
+            p = plan_backward(n, tokens, keys, heads, kv_heads, width, type);
             const int64_t pairs = (int64_t)n * kv_heads;
-            if (pairs * tiles(tokens * (heads / kv_heads), 128) > kMaxBlocks || pairs * tiles(keys, 128) > kMaxBlocks)
+            if (pairs * tiles(tokens * (heads / kv_heads), 128) > kMaxBlocks || pairs * tiles(keys, 128) * p.parts > kMaxBlocks)
                 c.fail(refuse("n * kv_heads is too large"));
             if (p.workspace > workspace_bytes)
                 c.fail(refuse("the workspace has %zu bytes, %zu are needed", workspace_bytes, p.workspace));
@@ -287,10 +294,11 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
     a.dk = heads_of(dk, n, keys, kv_heads);
     a.dv = heads_of(dv, n, keys, kv_heads);
     char *ws = static_cast<char *>(workspace);
-    a.delta = reinterpret_cast<float *>(ws + p.delta);
+    a.stats = reinterpret_cast<float2 *>(ws + p.stats);
     a.largest = reinterpret_cast<float2 *>(ws + p.largest);
     a.bounds = reinterpret_cast<int4 *>(ws + p.bounds);
-    a.parts = p.parts;
+    a.part_out = reinterpret_cast<float *>(ws + p.sums);
+    a.norms = p.norms, a.parts = p.parts;
     a.bound_stride = a.range_stride ? tiles(a.rows, 32) : 0;
     const hipStream_t st = (hipStream_t)hip_stream;
     with_type(q->type, [&](auto zero) { launch_attention_backward<decltype(zero)>(a, n, st); });

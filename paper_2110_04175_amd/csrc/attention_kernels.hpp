@@ -38,11 +38,16 @@ constexpr float kForwardShift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
 template <typename T>
 constexpr float kBackwardShift = std::is_same<T, _Float16>::value ? 15.0f : 0.0f;
 
+// The token of a row.
+__device__ __forceinline__ int token_of(const AttentionArgs &a, int row) {
+    return (int)((__umulhi((unsigned)row, a.group_factor) + (unsigned)row) >> a.group_shift);
+}
+
 // The keys that a token sees.
 __device__ __forceinline__ int2 seen(const AttentionArgs &a, int64_t worker, int t) {
     if (a.ranges) {
         const int2 r = a.ranges[worker * a.range_stride + t];
-        return int2{max(r.x, 0), min(r.y, a.keys)};
+        return int2{max(r.x, 0), max(0, min(r.y, a.keys))};
     }
     const int64_t last = (int64_t)t + 1 + a.keys - a.tokens;
     return int2{0, a.causal ? (int)max((int64_t)0, min(last, (int64_t)a.keys)) : a.keys};
@@ -73,6 +78,12 @@ __device__ __forceinline__ int column_reduce(int v, F f) {
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) v = f(v, __shfl_xor(v, m));
     return __builtin_amdgcn_readfirstlane(v);
+}
+
+// Whether a column that sees keys lo <= j < hi sees the one that is `far` and
+// `more` behind lo.
+__device__ __forceinline__ bool sees(int far, int more, int lo, int hi) {
+    return (unsigned)(far + more) < (unsigned)max(hi - lo, 0);
 }
 
 // What a wave's columns see: whether a stretch of keys is seen by all, by some.
@@ -130,8 +141,7 @@ struct Softmax {
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int key = j + 32 * b + 8 * (i / 4) + 4 * h + i % 4;
-                    p[b][i] = key >= lo && key < hi ? p[b][i] : -INFINITY;
+                    p[b][i] = sees(j + 4 * h - lo, 32 * b + 8 * (i / 4) + i % 4, lo, hi) ? p[b][i] : -INFINITY;
                 }
         }
         float top = p[0][0];
@@ -200,22 +210,23 @@ struct RowTile {
         kvh = (int)(pair % a.kv);
         row = tile * 128 + wave * 32 + lane % 32;
         valid = row < a.rows;
-        t = valid ? row / a.group : 0, head = kvh * a.group + (valid ? row % a.group : 0);
+        t = valid ? token_of(a, row) : 0, head = kvh * a.group + (valid ? row - t * a.group : 0);
         const int2 range = valid ? seen(a, worker, t) : int2{0, INT_MAX};
         lo = range.x, hi = range.y;
         sight = sight_of(lo, hi, valid);
         if (lane == 0) most[wave][0] = sight.least_lo, most[wave][1] = sight.most_hi;
         __syncthreads();
-        first = min(min(most[0][0], most[1][0]), min(most[2][0], most[3][0]));
-        end = max(max(most[0][1], most[1][1]), max(most[2][1], most[3][1]));
+        first = __builtin_amdgcn_readfirstlane(min(min(most[0][0], most[1][0]), min(most[2][0], most[3][0])));
+        end = __builtin_amdgcn_readfirstlane(max(max(most[0][1], most[1][1]), max(most[2][1], most[3][1])));
     }
 };
 
-// Runs `step(half, j)` over tiles of BN keys from `first` to `end`: keys in
-// lds[half][0], values in lds[half][1], the next tile's on their way meanwhile.
+// Runs `step(tile, j)` over tiles of BN keys from `first` to `end`: keys at
+// `tile` and the values behind them, the next tile's on their way meanwhile.
 template <typename T, int DP, int BN, bool DIRECT, typename F>
-__device__ __forceinline__ void over_keys(const AttentionArgs &a, const RowTile &r, char (&lds)[2][2][BN * Tile<T, DP>::kRowBytes],
+__device__ __forceinline__ void over_keys(const AttentionArgs &a, const RowTile &r, char (&lds)[2][2 * BN * Tile<T, DP>::kRowBytes],
                                           F step) {
+    constexpr int kTile = BN * Tile<T, DP>::kRowBytes;
     const int begin = r.first / BN * BN, end = r.end;
     if (r.first >= end) return;
     const char *kbase = reinterpret_cast<const char *>(head_at<const T>(a.k, r.worker, 0, r.kvh));
@@ -224,35 +235,31 @@ __device__ __forceinline__ void over_keys(const AttentionArgs &a, const RowTile 
     Stage<T, DP, BN, 256, DIRECT> ks, vs;
     const auto kat = [&](int x) { return x * kr; };
     const auto vat = [&](int x) { return x * vr; };
-    const auto fetch = [&](int j, int half) {
+    const auto fetch = [&](int j, char *to) __attribute__((always_inline)) {
         const int rows = min(BN, a.keys - j);
-        if (rows < BN) {
-            ks.places(rows, threadIdx.x, kat);
-            vs.places(rows, threadIdx.x, vat);
-        }
-        ks.load(kbase + j * kr, lds[half][0], a.width, rows, threadIdx.x, kat);
-        vs.load(vbase + j * vr, lds[half][1], a.width, rows, threadIdx.x, vat);
+        ks.load(kbase + j * kr, to, a.width, rows, threadIdx.x, kat);
+        vs.load(vbase + j * vr, to + kTile, a.width, rows, threadIdx.x, vat);
     };
-    const auto put = [&](int half) {
-        ks.put(lds[half][0], threadIdx.x);
-        vs.put(lds[half][1], threadIdx.x);
+    const auto put = [&](char *to) {
+        ks.put(to, threadIdx.x);
+        vs.put(to + kTile, threadIdx.x);
     };
     if (DIRECT && a.width < DP) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ks.clear(lds[i / 2][i % 2], threadIdx.x);
+        for (int i = 0; i < 4; ++i) ks.clear(lds[i / 2] + i % 2 * kTile, threadIdx.x);
         __syncthreads();
     }
-    ks.places(BN, threadIdx.x, kat);
-    vs.places(BN, threadIdx.x, vat);
-    fetch(begin, 0);
-    put(0);
+    ks.places(threadIdx.x, kat);
+    vs.places(threadIdx.x, vat);
+    fetch(begin, lds[0]);
+    put(lds[0]);
     int half = 0;
     for (int j = begin; j < end; j += BN, half ^= 1) {
         __syncthreads();
         const bool more = j + BN < end;
-        if (more) fetch(j + BN, half ^ 1);
-        step(half, j);
-        if (more) put(half ^ 1);
+        if (more) fetch(j + BN, lds[half ^ 1]);
+        step(lds[half], j);
+        if (more) put(lds[half ^ 1]);
     }
 }
 
@@ -278,15 +285,15 @@ __device__ __forceinline__ void store_rows(const AttentionArgs &a, const RowTile
 // what they do not see kept out of them.
 template <typename T, int DP>
 __device__ __noinline__ void attention_apart(const AttentionArgs a, const RowTile r,
-                                             char (&lds)[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
+                                             char (&lds)[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
     constexpr int BN = kKeyTile<T, DP>;
     Softmax<T, DP> st;
     load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
     st.clear();
-    over_keys<T, DP, BN, false>(a, r, lds, [&](int half, int j) {
+    over_keys<T, DP, BN, false>(a, r, lds, [&](const char *tile, int j) {
         for (int b = 0; b < BN; b += 32)
             if (r.sight.any(j + b, 32))
-                st.template step<1, true>(a, lds[half][0] + b * Tile<T, DP>::kRowBytes, lds[half][1] + b * Tile<T, DP>::kRowBytes,
+                st.template step<1, true>(a, tile + b * Tile<T, DP>::kRowBytes, tile + (BN + b) * Tile<T, DP>::kRowBytes,
                                           j + b, r.lo, r.hi, r.sight.whole(j + b, 32), room, r.lane);
     });
     store_rows(a, r, st, st.l + other_half(st.l));
@@ -295,16 +302,17 @@ __device__ __noinline__ void attention_apart(const AttentionArgs a, const RowTil
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_kernel(AttentionArgs a) {
     constexpr int BN = kKeyTile<T, DP>;
-    __shared__ __align__(16) char lds[2][2][BN * Tile<T, DP>::kRowBytes];
+    __shared__ __align__(16) char lds[2][2 * BN * Tile<T, DP>::kRowBytes];
     __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ int most[4][2];
     const RowTile r(a, most);
     Softmax<T, DP> st;
     load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
     st.clear();
-    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](int half, int j) {
+    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](const char *tile, int j) __attribute__((always_inline)) {
         if (r.sight.any(j, BN))
-            st.template step<BN / 32, false>(a, lds[half][0], lds[half][1], j, r.lo, r.hi, r.sight.whole(j, BN), nullptr, r.lane);
+            st.template step<BN / 32, false>(a, tile, tile + BN * Tile<T, DP>::kRowBytes, j, r.lo, r.hi,
+                                             r.sight.whole(j, BN), nullptr, r.lane);
     });
     const float sum = st.l + other_half(st.l);
     if (__syncthreads_or(r.valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY))))
@@ -337,7 +345,7 @@ __global__ __launch_bounds__((64 * kSplitWaves<T, DP>)) void attention_split_ker
     const int kvh = (int)(pair % a.kv);
     const int row = tile * 32 + lane % 32;
     const bool valid = row < a.rows;
-    const int t = valid ? row / a.group : 0, head = kvh * a.group + (valid ? row % a.group : 0);
+    const int t = valid ? token_of(a, row) : 0, head = kvh * a.group + (valid ? row - t * a.group : 0);
     const int2 range = valid ? seen(a, worker, t) : int2{0, INT_MAX};
     const int lo = range.x, hi = range.y;
     const Sight sight = sight_of(lo, hi, valid);
@@ -406,7 +414,7 @@ __global__ __launch_bounds__((64 * kSplitWaves<T, DP>)) void attention_split_ker
         f[w] = soft[w][0][col] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(soft[w][0][col] - top);
         all += soft[w][1][col] * (soft[w][0][col] == -INFINITY ? 1.0f : f[w]);
     }
-    const int rt = r / a.group, rh = kvh * a.group + r % a.group;
+    const int rt = token_of(a, r), rh = kvh * a.group + r - rt * a.group;
     const int2 rr = seen(a, worker, rt);
     const bool empty = rr.x >= rr.y;
     const float inv = a.parts > 1 ? 1.0f : empty ? 0.0f : 1.0f / all;
@@ -434,7 +442,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
     if (at >= (int64_t)a.pairs * a.rows) return;
     const int64_t pair = at / a.rows, worker = pair / a.kv;
-    const int r = (int)(at % a.rows), t = r / a.group, head = (int)(pair % a.kv) * a.group + r % a.group;
+    const int r = (int)(at % a.rows), t = token_of(a, r), head = (int)(pair % a.kv) * a.group + r - t * a.group;
     const int2 range = seen(a, worker, t);
     const bool empty = range.x >= range.y;
     const float2 *soft = a.part_soft + at * a.parts;
@@ -462,16 +470,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 
 // ---- backward ----------------------------------------------------------------------
 
-// delta = dout . out of every row, 16 lanes each; for binary16 also the largest
+// lse in powers of two and delta = dout . out of every row, 16 lanes each; for binary16 also the largest
 // squared norms of the rows of dout that see something and of v's.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
     __shared__ float red[2][16];
-    const int64_t worker = blockIdx.x / a.parts;
-    const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x % 16, slot = threadIdx.x / 16;
+    const int64_t worker = blockIdx.x / a.norms;
+    const int part = (int)(blockIdx.x % a.norms), lane = threadIdx.x % 16, slot = threadIdx.x / 16;
     float most_dout = 0.0f, most_v = 0.0f;
     const int64_t rows = (int64_t)a.tokens * a.heads;
-    for (int64_t r = (int64_t)part * 16 + slot; r < rows; r += (int64_t)a.parts * 16) {
+    for (int64_t r = (int64_t)part * 16 + slot; r < rows; r += (int64_t)a.norms * 16) {
         const int t = (int)(r / a.heads), head = (int)(r % a.heads);
         const T *x = head_at<const T>(a.dout, worker, t, head), *y = head_at<const T>(a.out, worker, t, head);
         float dot = 0.0f, norm = 0.0f;
@@ -483,7 +491,9 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
             for (int i = 0; i < 8; ++i) dot = fmaf(u[i], v[i], dot), norm = fmaf(u[i], u[i], norm);
         }
         dot = row_reduce<16, float, pick_sum>(dot, nullptr);
-        if (lane == 0) a.delta[(worker * a.heads + head) * a.tokens + t] = dot;
+        if (lane == 0)
+            a.stats[(worker * a.kv + head / a.group) * a.rows + (int64_t)t * a.group + head % a.group] =
+                float2{a.lse[(worker * a.heads + head) * a.tokens + t] * kLog2e, dot};
         if (std::is_same<T, _Float16>::value) {
             norm = row_reduce<16, float, pick_sum>(norm, nullptr);
             const int2 s = seen(a, worker, t);
@@ -492,7 +502,7 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
     }
     if (std::is_same<T, _Float16>::value) {
         const int64_t vrows = (int64_t)a.keys * a.kv;
-        for (int64_t r = (int64_t)part * 16 + slot; r < vrows; r += (int64_t)a.parts * 16) {
+        for (int64_t r = (int64_t)part * 16 + slot; r < vrows; r += (int64_t)a.norms * 16) {
             const T *x = head_at<const T>(a.v, worker, r / a.kv, (int)(r % a.kv));
             float norm = 0.0f;
             for (int k = lane * 8; k < a.width; k += 128) {
@@ -520,7 +530,7 @@ __global__ __launch_bounds__(256) void attention_bounds_kernel(AttentionArgs a, 
     if (at >= total) return;
     const int64_t per = (a.rows + 31) / 32, worker = at / per;
     const int row = (int)(at % per) * 32 + threadIdx.x % 32;
-    int2 s = row < a.rows ? seen(a, worker, row / a.group) : int2{INT_MAX, 0};
+    int2 s = row < a.rows ? seen(a, worker, token_of(a, row)) : int2{INT_MAX, 0};
     int4 b = {row < a.rows ? s.x : INT_MAX, row < a.rows ? s.x : 0, row < a.rows ? s.y : 0, s.y};
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) {
@@ -539,8 +549,8 @@ __device__ __forceinline__ Sight block_sight(const AttentionArgs &a, int64_t wor
         return Sight{b.x, b.y, b.z, b.w};
     }
     const int last = min(block * 32 + 31, a.rows - 1);
-    return Sight{0, 0, block * 32 + 32 > a.rows ? 0 : seen(a, worker, block * 32 / a.group).y,
-                 seen(a, worker, last / a.group).y};
+    return Sight{0, 0, block * 32 + 32 > a.rows ? 0 : seen(a, worker, token_of(a, block * 32)).y,
+                 seen(a, worker, token_of(a, last)).y};
 }
 
 // The power of two that ds is held times in binary16, so that its largest is
@@ -549,8 +559,8 @@ template <typename T>
 __device__ __forceinline__ float gradient_scale(const AttentionArgs &a, int64_t worker, float2 *red) {
     if (!std::is_same<T, _Float16>::value) return 1.0f;
     float2 m = {0.0f, 0.0f};
-    for (int p = threadIdx.x; p < a.parts; p += 256) {
-        const float2 v = a.largest[worker * a.parts + p];
+    for (int p = threadIdx.x; p < a.norms; p += 256) {
+        const float2 v = a.largest[worker * a.norms + p];
         m.x = fmaxf(m.x, v.x), m.y = fmaxf(m.y, v.y);
     }
 #pragma unroll
@@ -574,12 +584,14 @@ struct QueryGradient {
     __device__ __forceinline__ void start(const AttentionArgs &a, const RowTile &r, float factor) {
         load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), q, a.width, r.valid, r.lane);
         load_own<T, DP>(head_at<const T>(a.dout, r.worker, r.t, r.head), dout, a.width, r.valid, r.lane);
-        const int64_t stat = (r.worker * a.heads + r.head) * a.tokens + r.t;
-        off = r.valid ? a.lse[stat] * kLog2e : 0.0f, delta = r.valid ? a.delta[stat] : 0.0f;
+        const float2 stat = r.valid ? a.stats[(int64_t)r.pair * a.rows + r.row] : float2{0.0f, 0.0f};
+        off = stat.x, delta = stat.y;
         up = factor;
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) acc[b] = f16_t{0};
     }
+    __device__ __forceinline__ float weight(float p) const { return std::is_same<T, _Float16>::value ? p * up : p; }
+
     // 32 keys from j on.
     template <bool APART>
     __device__ __forceinline__ void step(const AttentionArgs &a, const RowTile &r, const char *kt, const char *vt, int j,
@@ -590,12 +602,11 @@ struct QueryGradient {
         float ds[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off)) * up * (dp[i] - delta);
+            ds[i] = weight(__builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off))) * (dp[i] - delta);
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int key = j + 8 * (i / 4) + 4 * (r.lane / 32) + i % 4;
-                ds[i] = key >= r.lo && key < r.hi ? ds[i] : 0.0f;
+                ds[i] = sees(j + 4 * (r.lane / 32) - r.lo, 8 * (i / 4) + i % 4, r.lo, r.hi) ? ds[i] : 0.0f;
             }
         }
         if (APART && !whole)
@@ -610,19 +621,19 @@ struct QueryGradient {
 
 template <typename T, int DP, bool DIRECT, bool APART>
 __device__ __forceinline__ void dq_over_keys(const AttentionArgs &a, const RowTile &r, QueryGradient<T, DP> &g,
-                                             char (&lds)[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
+                                             char (&lds)[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
     constexpr int BN = kKeyTile<T, DP>, kRowBytes = Tile<T, DP>::kRowBytes;
-    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](int half, int j) {
+    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](const char *tile, int j) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < BN; b += 32)
             if (r.sight.any(j + b, 32))
-                g.template step<APART>(a, r, lds[half][0] + b * kRowBytes, lds[half][1] + b * kRowBytes, j + b, room);
+                g.template step<APART>(a, r, tile + b * kRowBytes, tile + (BN + b) * kRowBytes, j + b, room);
     });
 }
 
 template <typename T, int DP>
 __device__ __noinline__ void attention_dq_apart(const AttentionArgs a, const RowTile r, float up,
-                                                char (&lds)[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
+                                                char (&lds)[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
     QueryGradient<T, DP> g;
     g.start(a, r, up);
     dq_over_keys<T, DP, false, true>(a, r, g, lds, room);
@@ -631,7 +642,7 @@ __device__ __noinline__ void attention_dq_apart(const AttentionArgs a, const Row
 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel(AttentionArgs a) {
-    __shared__ __align__(16) char lds[2][2][kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
+    __shared__ __align__(16) char lds[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
     __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ int most[4][2];
     __shared__ float2 red[4];
@@ -647,28 +658,75 @@ __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel
 }
 
 // The gradients of k and v: columns are keys, 128 of a workgroup, and rows the
-// queries that see them, 32 at a time.
-constexpr int kRowTile = 32;
+// queries that see them, in tiles of 32 or 64.
+template <typename T, int DP>
+constexpr int kRowTile = Tile<T, DP>::kRowBytes > 128 ? 32 : 64;
+
+// Whether the keys' own rows of v lie in LDS: at 128 entries of 16 bits the rows
+// and sums of two arrays pass the 256 registers of two waves a SIMD.
+template <typename T, int DP>
+constexpr bool kValuesInLds = sizeof(T) == 2 && DP == 128;
 
 template <typename T, int DP>
-struct KeyLds {
-    char rows[2][2][kRowTile * Tile<T, DP>::kRowBytes];   // q, dout
-    float stats[2][2][kRowTile];                          // lse in powers of two, delta
-    int2 sees[2][kRowTile];
+struct RowsInLds {
+    char rows[2][kRowTile<T, DP> * Tile<T, DP>::kRowBytes];   // q, dout
+    float stats[2][kRowTile<T, DP>];                          // lse in powers of two, delta
+    int2 sees[kRowTile<T, DP>];
+};
+
+// The tiles of rows that a workgroup walks through.  Of 64 blocks of 32 rows at a
+// time each lane looks at one: whether any of the workgroup's keys is seen from
+// it, any of this wave's, and all of them from all of its rows.
+struct Walk {
+    int64_t worker;
+    int j0, mine, base, part;
+    unsigned long long open, any, whole;
+
+    template <int BLOCKS>
+    __device__ __forceinline__ void look(const AttentionArgs &a, int lane) {
+        const int block = base + lane;
+        Sight s{0, 0, 0, 0};
+        if (block * 32 < a.rows) s = block_sight(a, worker, block);
+        open = __ballot(s.any(j0, 128));
+        any = __ballot(s.any(mine, 32));
+        whole = __ballot(s.whole(mine, 32));
+        if (BLOCKS == 2) open = (open | open >> 1) & 0x5555555555555555ull;
+        // Tiles go round the parts.
+        const int tile = (base + lane) / BLOCKS;
+        open &= __ballot(tile % a.parts == part);
+    }
+    // The first block of the next tile from `block` on, or one behind the last.
+    template <int BLOCKS>
+    __device__ __forceinline__ int next(const AttentionArgs &a, int block, int blocks, int lane) {
+        while (block < blocks) {
+            if (block >= base + 64) {
+                base = block & ~63;
+                look<BLOCKS>(a, lane);
+            }
+            const unsigned long long left = open >> (block - base);
+            if (left) return block + __builtin_ctzll(left);
+            block = base + 64;
+        }
+        return blocks;
+    }
 };
 
 template <typename T, int DP>
 struct KeyGradient {
     typedef Tile<T, DP> L;
-    u4_t k[L::kOwn], v[L::kOwn];
+    static constexpr bool kInLds = kValuesInLds<T, DP>;
+    u4_t k[L::kOwn], v[kInLds ? 1 : L::kOwn];
+    const char *values;   // 32 rows of v
     f16_t dk[L::kBlocks], dv[L::kBlocks];
     int64_t worker;
-    int kvh, j0, mine, key, lane;
+    int kvh, j0, mine, key, lane, part;
+    unsigned pair;
     bool valid;
     float up;
 
-    __device__ __forceinline__ void start(const AttentionArgs &a, unsigned pair, int tile, float factor) {
+    __device__ __forceinline__ void start(const AttentionArgs &a, unsigned at, int tile, int turn, float factor, char *own) {
         lane = threadIdx.x % kWave;
+        pair = at, part = turn;
         worker = pair / a.kv;
         kvh = (int)(pair % a.kv);
         j0 = tile * 128, mine = j0 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * 32;
@@ -676,165 +734,230 @@ struct KeyGradient {
         valid = key < a.keys;
         up = factor;
         load_own<T, DP>(head_at<const T>(a.k, worker, valid ? key : 0, kvh), k, a.width, valid, lane);
-        load_own<T, DP>(head_at<const T>(a.v, worker, valid ? key : 0, kvh), v, a.width, valid, lane);
+        const T *vrow = head_at<const T>(a.v, worker, valid ? key : 0, kvh);
+        if constexpr (kInLds) {
+            char *to = own + threadIdx.x / kWave * 32 * L::kRowBytes;
+            values = to;
+            for (int i = 0; i < L::kOwn; ++i)
+                *reinterpret_cast<u4_t *>(to + L::at(lane % 32, 2 * i + lane / 32)) =
+                    load_chunk<T>(vrow, (2 * i + lane / 32) * L::E, a.width, valid);
+        } else {
+            load_own<T, DP>(vrow, v, a.width, valid, lane);
+        }
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) dk[b] = dv[b] = f16_t{0};
     }
 
+    // A weight, held times 2^kBackwardShift, times the factor of ds.
+    __device__ __forceinline__ float scaled(float p) const {
+        return kBackwardShift<T> != 0.0f ? p * ldexpf(up, -(int)kBackwardShift<T>) : p;
+    }
+
+    // 32 rows of a tile from row0 on.
     template <bool APART>
-    __device__ __forceinline__ void step(const AttentionArgs &a, const KeyLds<T, DP> &lds, int half, bool whole, char *room) {
-        const float factor = ldexpf(up, -(int)kBackwardShift<T>);
-        const f16_t s = dots<T, DP>(lds.rows[half][0], 0, k, lane);
-        const f16_t dp = dots<T, DP>(lds.rows[half][1], 0, v, lane);
+    __device__ __forceinline__ void step(const AttentionArgs &a, const RowsInLds<T, DP> &lds, int row0, bool whole, char *room) {
+        const f16_t s = dots<T, DP>(lds.rows[0], row0, k, lane);
         float p[16], ds[16];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const f4_t off = *reinterpret_cast<const f4_t *>(&lds.stats[half][0][8 * g + 4 * (lane / 32)]);
-            const f4_t delta = *reinterpret_cast<const f4_t *>(&lds.stats[half][1][8 * g + 4 * (lane / 32)]);
+            const f4_t off = *reinterpret_cast<const f4_t *>(&lds.stats[0][row0 + 8 * g + 4 * (lane / 32)]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 4 * g + r;
-                p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off[r]));
-                ds[i] = p[i] * factor * (dp[i] - delta[r]);
+            for (int r = 0; r < 4; ++r) p[4 * g + r] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + r], a.dot_scale, -off[r]));
+        }
+        f16_t dp;
+        if constexpr (kInLds) dp = dots_in_lds<T, DP>(lds.rows[1], row0, values, 0, lane);
+        else dp = dots<T, DP>(lds.rows[1], row0, v, lane);
+        unsigned there = 0xffff;
+        if (!whole) {
+            there = 0;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const i4_t x = *reinterpret_cast<const i4_t *>(&lds.sees[row0 + 8 * (i / 4) + 4 * (lane / 32) + i % 4]);
+                const bool one = sees(key - x[0], 0, x[0], x[1]), two = sees(key - x[2], 0, x[2], x[3]);
+                p[i] = one ? p[i] : 0.0f, p[i + 1] = two ? p[i + 1] : 0.0f;
+                there |= one << i | two << (i + 1);
             }
         }
+        if (APART && !whole)
+            add_rows_apart<T, DP>(dv, lds.rows[1], row0, p, room, lane, [&](int r) {
+                return sees(key - lds.sees[row0 + r].x, 0, lds.sees[row0 + r].x, lds.sees[row0 + r].y);
+            });
+        else
+            add_rows<T, DP>(dv, lds.rows[1], row0, Weights<T>(p), lane);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f4_t delta = *reinterpret_cast<const f4_t *>(&lds.stats[1][row0 + 8 * g + 4 * (lane / 32)]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ds[4 * g + r] = scaled(p[4 * g + r]) * (dp[4 * g + r] - delta[r]);
+        }
+        // A weight of 0 times an infinity is none.
         if (!whole) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int2 x = lds.sees[half][8 * (i / 4) + 4 * (lane / 32) + i % 4];
-                const bool there = key >= x.x && key < x.y;
-                p[i] = there ? p[i] : 0.0f;
-                ds[i] = there ? ds[i] : 0.0f;
-            }
+            for (int i = 0; i < 16; ++i) ds[i] = there >> i & 1 ? ds[i] : 0.0f;
         }
-        if (APART && !whole) {
-            const auto there = [&](int r) { return key >= lds.sees[half][r].x && key < lds.sees[half][r].y; };
-            add_rows_apart<T, DP>(dv, lds.rows[half][1], 0, p, room, lane, there);
-            add_rows_apart<T, DP>(dk, lds.rows[half][0], 0, ds, room, lane, there);
-        } else {
-            add_rows<T, DP>(dv, lds.rows[half][1], 0, Weights<T>(p), lane);
-            add_rows<T, DP>(dk, lds.rows[half][0], 0, Weights<T>(ds), lane);
-        }
+        if (APART && !whole)
+            add_rows_apart<T, DP>(dk, lds.rows[0], row0, ds, room, lane, [&](int r) {
+                return sees(key - lds.sees[row0 + r].x, 0, lds.sees[row0 + r].x, lds.sees[row0 + r].y);
+            });
+        else
+            add_rows<T, DP>(dk, lds.rows[0], row0, Weights<T>(ds), lane);
     }
 
     template <bool DIRECT, bool APART>
-    __device__ __forceinline__ void over_rows(const AttentionArgs &a, KeyLds<T, DP> &lds, char *room) {
-        constexpr int BR = kRowTile;
-        const int blocks = (a.rows + BR - 1) / BR;
-        // Without ranges the rows that see a key are all from one on.
-        int block = 0;
-        if (!a.ranges && a.causal) block = (int)(max((int64_t)0, (int64_t)j0 + a.tokens - a.keys) * a.group / BR);
+    __device__ __forceinline__ void over_rows(const AttentionArgs &a, RowsInLds<T, DP> (&lds)[2], char *room) {
+        constexpr int BR = kRowTile<T, DP>, kTileBlocks = BR / 32;
+        const int blocks = (a.rows + 31) / 32;
         const char *qbase = reinterpret_cast<const char *>(head_at<const T>(a.q, worker, 0, kvh * a.group));
         const char *obase = reinterpret_cast<const char *>(head_at<const T>(a.dout, worker, 0, kvh * a.group));
         Stage<T, DP, BR, 256, DIRECT> qs, os;
-        // A group that divides 32 has its rows at the same places of every block.
+        // A group that divides a tile has its rows at the same places of every one.
         const bool steady = BR % a.group == 0;
         float2 stat = {0.0f, 0.0f};
         int2 range = {0, 0};
-        const auto next = [&](int b) {
-            if (!a.ranges) return b;
-            for (; b < blocks; b += kWave) {
-                bool any = false;
-                if (b + lane < blocks) any = block_sight(a, worker, b + lane).any(j0, 128);
-                const unsigned long long m = __ballot(any);
-                if (m) return b + __ffsll((long long)m) - 1;
-            }
-            return blocks;
-        };
-        const auto fetch = [&](int b, int half) {
-            const int row0 = b * BR, t0 = row0 / a.group, rows = min(BR, a.rows - row0);
+        const auto fetch = [&](int block, RowsInLds<T, DP> &to) __attribute__((always_inline)) {
+            const int row0 = block * 32, t0 = token_of(a, row0), rows = min(BR, a.rows - row0);
             const auto at = [&](const Heads &x) {
                 return [&, rs = x.rs, hs = x.hs](int r) {
-                    const int row = row0 + r, t = row / a.group;
+                    const int row = row0 + r, t = token_of(a, row);
                     return ((t - t0) * rs + (row - t * a.group) * hs) * (int64_t)sizeof(T);
                 };
             };
-            if (!steady || rows < BR) {
-                qs.places(rows, threadIdx.x, at(a.q));
-                os.places(rows, threadIdx.x, at(a.dout));
-            }
-            qs.load(qbase + t0 * a.q.rs * (int64_t)sizeof(T), lds.rows[half][0], a.width, rows, threadIdx.x, at(a.q));
-            os.load(obase + t0 * a.dout.rs * (int64_t)sizeof(T), lds.rows[half][1], a.width, rows, threadIdx.x, at(a.dout));
+            // What comes into registers is used only in put().
             if (threadIdx.x < BR) {
                 const int row = row0 + threadIdx.x;
                 stat = float2{0.0f, 0.0f}, range = int2{0, 0};
                 if (row < a.rows) {
-                    const int t = row / a.group;
-                    const int64_t s = (worker * a.heads + kvh * a.group + row % a.group) * a.tokens + t;
-                    stat = float2{a.lse[s] * kLog2e - kBackwardShift<T>, a.delta[s]};
-                    range = seen(a, worker, t);
+                    stat = a.stats[(int64_t)pair * a.rows + row];
+                    const int t = token_of(a, row);
+                    range = a.ranges ? a.ranges[worker * a.range_stride + t] : seen(a, worker, t);
                 }
             }
+            if (!steady) {
+                qs.places(threadIdx.x, at(a.q));
+                os.places(threadIdx.x, at(a.dout));
+            }
+            qs.load(qbase + t0 * a.q.rs * (int64_t)sizeof(T), to.rows[0], a.width, rows, threadIdx.x, at(a.q));
+            os.load(obase + t0 * a.dout.rs * (int64_t)sizeof(T), to.rows[1], a.width, rows, threadIdx.x, at(a.dout));
         };
-        const auto put = [&](int half) {
-            qs.put(lds.rows[half][0], threadIdx.x);
-            os.put(lds.rows[half][1], threadIdx.x);
+        const auto put = [&](RowsInLds<T, DP> &to) {
+            qs.put(to.rows[0], threadIdx.x);
+            os.put(to.rows[1], threadIdx.x);
             if (threadIdx.x < BR) {
-                lds.stats[half][0][threadIdx.x] = stat.x;
-                lds.stats[half][1][threadIdx.x] = stat.y;
-                lds.sees[half][threadIdx.x] = range;
+                to.stats[0][threadIdx.x] = stat.x - kBackwardShift<T>;
+                to.stats[1][threadIdx.x] = stat.y;
+                to.sees[threadIdx.x] = int2{max(range.x, 0), max(0, min(range.y, a.keys))};
             }
         };
         if (DIRECT && a.width < DP) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qs.clear(lds.rows[i / 2][i % 2], threadIdx.x);
+            for (int i = 0; i < 4; ++i) qs.clear(lds[i / 2].rows[i % 2], threadIdx.x);
             __syncthreads();
         }
-        block = next(block);
+        // Without ranges the rows that see a key are all from one on.
+        int block = 0;
+        if (!a.ranges && a.causal)
+            block = (int)(max((int64_t)0, (int64_t)j0 + a.tokens - a.keys) * a.group / BR) * kTileBlocks;
+        Walk walk{worker, j0, mine, -64, part, 0, 0, 0};
+        block = walk.next<kTileBlocks>(a, block, blocks, lane);
         if (block >= blocks) return;
+        unsigned any = (unsigned)(walk.any >> (block - walk.base)), whole = (unsigned)(walk.whole >> (block - walk.base));
         if (steady) {
             const auto at = [&](const Heads &x) {
-                return [&, rs = x.rs, hs = x.hs](int r) { return (r / a.group * rs + r % a.group * hs) * (int64_t)sizeof(T); };
+                return [&, rs = x.rs, hs = x.hs](int r) {
+                    const int t = token_of(a, r);
+                    return (t * rs + (r - t * a.group) * hs) * (int64_t)sizeof(T);
+                };
             };
-            qs.places(BR, threadIdx.x, at(a.q));
-            os.places(BR, threadIdx.x, at(a.dout));
+            qs.places(threadIdx.x, at(a.q));
+            os.places(threadIdx.x, at(a.dout));
         }
-        fetch(block, 0);
-        put(0);
+        fetch(block, lds[0]);
+        put(lds[0]);
         for (int half = 0; block < blocks; half ^= 1) {
             __syncthreads();
-            const int then = next(block + 1);
-            if (then < blocks) fetch(then, half ^ 1);
-            const Sight sight = block_sight(a, worker, block);
-            if (sight.any(mine, 32)) step<APART>(a, lds, half, sight.whole(mine, 32), room);
-            if (then < blocks) put(half ^ 1);
-            block = then;
+            block = walk.next<kTileBlocks>(a, block + kTileBlocks, blocks, lane);
+            if (block < blocks) fetch(block, lds[half ^ 1]);
+#pragma unroll
+            for (int b = 0; b < kTileBlocks; ++b)
+                if (any >> b & 1) step<APART>(a, lds[half], 32 * b, whole >> b & 1, room);
+            if (block < blocks) {
+                put(lds[half ^ 1]);
+                any = (unsigned)(walk.any >> (block - walk.base)), whole = (unsigned)(walk.whole >> (block - walk.base));
+            }
         }
     }
 
     __device__ __forceinline__ void store(const AttentionArgs &a) const {
         if (!valid) return;
-        store_column<T>(head_at<T>(a.dk, worker, key, kvh), a.width, dk, a.scale / up, lane);
-        store_column<T>(head_at<T>(a.dv, worker, key, kvh), a.width, dv, ldexpf(1.0f, -(int)kBackwardShift<T>), lane);
+        const float fk = a.scale / up, fv = ldexpf(1.0f, -(int)kBackwardShift<T>);
+        if (a.parts > 1) {
+            float *to = a.part_out + (((int64_t)pair * a.keys + key) * a.parts + part) * 2 * a.width;
+            store_column<float>(to, a.width, dk, fk, lane);
+            store_column<float>(to + a.width, a.width, dv, fv, lane);
+        } else {
+            store_column<T>(head_at<T>(a.dk, worker, key, kvh), a.width, dk, fk, lane);
+            store_column<T>(head_at<T>(a.dv, worker, key, kvh), a.width, dv, fv, lane);
+        }
     }
 };
 
 template <typename T, int DP>
-__device__ __noinline__ void attention_dkv_apart(const AttentionArgs a, unsigned pair, int tile, float up, KeyLds<T, DP> &lds,
-                                                 char *room) {
+__device__ __noinline__ void attention_dkv_apart(const AttentionArgs a, unsigned pair, int tile, int part, float up,
+                                                 RowsInLds<T, DP> (&lds)[2], char *own, char *room) {
     KeyGradient<T, DP> g;
-    g.start(a, pair, tile, up);
+    g.start(a, pair, tile, part, up, own);
     g.template over_rows<false, true>(a, lds, room);
     g.store(a);
 }
 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(AttentionArgs a) {
-    __shared__ __align__(16) KeyLds<T, DP> lds;
+    __shared__ __align__(16) RowsInLds<T, DP> lds[2];
     __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
     __shared__ float2 red[4];
     unsigned pair;
     int tile;
-    place(a, blockIdx.x, pair, tile);
+    place(a, blockIdx.x / a.parts, pair, tile);
+    const int part = (int)(blockIdx.x % a.parts);
     tile = a.tiles - 1 - tile;   // the first keys are seen by the most rows
     const float up = gradient_scale<T>(a, pair / a.kv, red);
     KeyGradient<T, DP> g;
-    g.start(a, pair, tile, up);
+    g.start(a, pair, tile, part, up, own);
     g.template over_rows<DIRECT, false>(a, lds, nullptr);
     if (__syncthreads_or(g.valid && (not_finite(g.dk) || not_finite(g.dv))))
-        attention_dkv_apart<T, DP>(a, pair, tile, up, lds, room[threadIdx.x / kWave]);
+        attention_dkv_apart<T, DP>(a, pair, tile, part, up, lds, own, room[threadIdx.x / kWave]);
     else
         g.store(a);
+}
+
+// Adds up the parts of dk and dv, in their order: four entries a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_dkv_join_kernel(AttentionArgs a, int64_t total) {
+    const int per = (2 * a.width + 3) / 4;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= total * per) return;
+    const int64_t row = at / per, pair = row / a.keys, worker = pair / a.kv;
+    const int key = (int)(row % a.keys), kvh = (int)(pair % a.kv), k0 = (int)(at % per) * 4;
+    const float *from = a.part_out + row * a.parts * 2 * a.width + k0;
+    const int left = 2 * a.width - k0;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = 0; p < a.parts; ++p, from += 2 * a.width)
+        if (left >= 4) {
+            f4_t v;
+            __builtin_memcpy(&v, from, sizeof v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += i < left ? from[i] : 0.0f;
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = k0 + i;
+        if (k < a.width) head_at<T>(a.dk, worker, key, kvh)[k] = (T)sum[i];
+        else if (k < 2 * a.width) head_at<T>(a.dv, worker, key, kvh)[k - a.width] = (T)sum[i];
+    }
 }
 
 // ---- launches ---------------------------------------------------------------------------
@@ -879,10 +1002,10 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
         hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_bounds_kernel<T>), dim3((unsigned)tiles(total, 8)), dim3(256), 0, st, a, total);
     }
     if (a.tokens)
-        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)(n * a.parts)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)(n * a.norms)), dim3(256), 0, st, a);
     with_width(a.width, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        const dim3 keys_grid((unsigned)(a.pairs * tiles(a.keys, 128))), rows_grid((unsigned)(a.pairs * tiles(a.rows, 128)));
+        const dim3 keys_grid((unsigned)(a.pairs * tiles(a.keys, 128) * a.parts)), rows_grid((unsigned)(a.pairs * tiles(a.rows, 128)));
         a.tiles = (int32_t)tiles(a.keys, 128);
         if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
@@ -894,4 +1017,9 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
         else if (a.tokens)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
     });
+    if (a.parts > 1) {
+        const int64_t total = (int64_t)a.pairs * a.keys;
+        hipLaunchKernelGGL(attention_dkv_join_kernel<T>, dim3((unsigned)tiles(total * tiles(2 * a.width, 4), 256)), dim3(256), 0,
+                           st, a, total);
+    }
 }

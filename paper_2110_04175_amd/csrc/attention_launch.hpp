@@ -21,17 +21,18 @@ struct AttentionArgs {
     Heads q, k, v, out;
     Heads dout, dq, dk, dv;
     float *lse;                // [n][heads][tokens]
-    float *delta;              // [n][heads][tokens]: dout . out
-    float2 *largest;           // [n][parts]: squared norms of rows of dout and v
+    float2 *stats;             // [pairs][rows]: lse in powers of two, dout . out
+    float2 *largest;           // [n][norms]: squared norms of rows of dout and v
     int4 *bounds;              // [n or 1][ceil(rows / 32)]: least and most lo, least and most hi
     const int2 *ranges;
-    float *part_out;           // [pairs][rows][parts][width]
+    float *part_out;           // [pairs][rows][parts][width]; backward: [pairs][keys][parts][2 * width], dk and dv
     float2 *part_soft;         // [pairs][rows][parts]
     int64_t range_stride;      // rows between workers' ranges; 0: all have the same
     int64_t bound_stride;
     int32_t tokens, keys, heads, kv, group, width, rows;   // rows = tokens * group
-    int32_t causal, tiles, parts, span;
+    int32_t causal, tiles, parts, span, norms;
     uint32_t pairs;            // n * kv
+    uint32_t group_factor, group_shift;   // row / group = (mulhi(row, factor) + row) >> shift
     float scale, dot_scale;    // dot_scale = scale * log2(e)
 };
 

@@ -84,6 +84,21 @@ __device__ __forceinline__ f16_t dots(const char *tile, int row0, const u4_t (&o
     return c;
 }
 
+// The same with the columns' own rows in LDS, from row `col` of `own` on.
+template <typename T, int DP>
+__device__ __forceinline__ f16_t dots_in_lds(const char *tile, int row0, const char *own, int col, int lane) {
+    typedef Tile<T, DP> L;
+    f16_t c = {0};
+#pragma unroll
+    for (int i = 0; i < L::kOwn; ++i) {
+        const int at = L::at(lane % 32, 2 * i + lane / 32);
+        const u4_t a = *reinterpret_cast<const u4_t *>(tile + row0 * L::kRowBytes + at);
+        const u4_t b = *reinterpret_cast<const u4_t *>(own + col * L::kRowBytes + at);
+        c = multiply(c, a, b, (T)0.0f);
+    }
+    return c;
+}
+
 // Weights of 32 rows as operands.
 template <typename T>
 struct Weights {
@@ -229,10 +244,35 @@ __device__ __forceinline__ float other_half(float v) {
     return float_of(threadIdx.x % 64 < 32 ? r.y : r.x);
 }
 
+// 16 bytes for each lane from base + off into LDS at `to` + 16 * lane, on their
+// way until wait_for_lds(); base and `to` are the same for the whole wave.  In
+// assembly, because the compiler lets every later read of LDS wait for the
+// builtin's copies, whatever tile it reads, so that none would overlap with work
+// on another.  No register is written, and the address is read when it issues.
+// The no-operations are what it takes from a scalar register's write to its use
+// as an address.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is reserved: all the same it is overwritten
+__device__ __forceinline__ void start_copy(const char *base, unsigned off, const char *to) {
+    // The lower half of a pointer into LDS is the place there.
+    const unsigned place = __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uint64_t>(to));
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const uint64_t from = (unsigned)__builtin_amdgcn_readfirstlane((unsigned)at) |
+                          (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) << 32;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(place), "v"(off), "s"(from) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ void wait_for_lds() {
+    asm volatile("" ::: "memory");
+    wait_for_copies();
+    asm volatile("" ::: "memory");
+}
+
 // R rows of a tile on their way from memory into LDS, by NT threads.  DIRECT:
 // rows start on 16 bytes and have whole chunks, which are copied without
 // registers in between; a lane's LDS place is fixed, so it takes the chunk that
-// belongs there.  Rows that are not there then repeat the last one, and chunks
+// belongs there.  Rows that are not there then repeat the first one, and chunks
 // behind the width stay as they are (zeros from clear()).  Otherwise through
 // registers, at any alignment, zeros in both places.
 template <typename T, int DP, int R, int NT, bool DIRECT>
@@ -249,27 +289,29 @@ struct Stage {
     }
 
     // Where a thread's chunks lie, from a tile's base on: at(r) is where row r
-    // starts, in bytes.  Of `rows` rows, at least one.
+    // starts, in bytes.
     template <typename F>
-    __device__ __forceinline__ void places(int rows, int thread, F at) {
+    __device__ __forceinline__ void places(int thread, F at) {
         if (!DIRECT) return;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int u = i * NT + thread, r = u / L::kChunks;
-            off[i] = (unsigned)at(min(r, rows - 1)) + (u % L::kChunks ^ L::swizzle(r)) * 16;
+            off[i] = (unsigned)at(r) + (u % L::kChunks ^ L::swizzle(r)) * 16;
         }
     }
 
-    // Starts the way of a tile whose places are known.
+    // Starts the way of a tile whose places are known, of which `rows` are there.
+    // DIRECT: in place of the others its first row.
     template <typename F>
     __device__ __forceinline__ void load(const char *base, char *tile, int width, int rows, int thread, F at) {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int u = i * NT + thread, r = u / L::kChunks, place = u % L::kChunks;
             if (DIRECT) {
+                const int chunk = place ^ L::swizzle(r);
                 // A wave's first place in LDS.
                 char *to = tile + (i * NT + __builtin_amdgcn_readfirstlane(thread & ~63)) * 16;
-                if ((place ^ L::swizzle(r)) * L::E < width) copy_to_lds(base + off[i], to);
+                if (chunk * L::E < width) start_copy(base, r < rows ? off[i] : chunk * 16u, to);
             } else {
                 v[i] = load_chunk<T>(reinterpret_cast<const T *>(base + at(min(r, rows - 1))), place * L::E, width, r < rows);
             }
@@ -278,7 +320,7 @@ struct Stage {
     // Ends it: with a barrier behind, all threads can read the tile.
     __device__ __forceinline__ void put(char *tile, int thread) const {
         if (DIRECT) {
-            wait_for_copies();
+            wait_for_lds();
             return;
         }
 #pragma unroll
