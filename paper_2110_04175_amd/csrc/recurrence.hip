@@ -5,9 +5,13 @@
 //   dh_t = dy_t + a_(t+1) dh_(t+1)
 //   dgate_t = dh_t (h_(t-1) - x_t) a_t c_t,   dx_t = c_t dh_t
 //
-// channel by channel.  A run of tokens takes a state s to A s + B; runs compose,
-// so a sequence is cut into chunks of 64 tokens and those into a wave's 8.  A
-// workgroup has 256 channels of a chunk in registers.
+// channel by channel.  A run of tokens takes a state s to A s + B, and runs
+// compose.  A workgroup has 64 channels, one for each lane, and walks through its
+// tokens in tiles of 128: each of its 8 waves has 16 of them in registers, the
+// waves' runs go through LDS, and the next tile is on its way meanwhile.  So gate
+// and x are read once.  Where there are too few channels for the device, tokens
+// are split into parts: a first kernel finds the run of each part, and every
+// workgroup begins with those that lead to its own.
 //
 // Where a sequence starts (in the gradients: ends) nothing is carried, whatever
 // it is: such a run is marked by a negative A (a is not), and no product with
@@ -15,6 +19,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cstdint>
 #include <type_traits>
 
@@ -22,11 +27,11 @@
 
 namespace {
 
-constexpr int kChunk = 64;      // tokens of a workgroup
-constexpr int kSteps = 8;       // of a wave
-constexpr int kChannels = 4;    // of a lane
-constexpr int kBlock = kWave * kChannels;
-constexpr int kThreads = kChunk / kSteps * kWave;
+constexpr int kChunk = 64;      // tokens between the states that are kept
+constexpr int kSteps = 16;      // tokens of a wave in a tile
+constexpr int kWaves = 8;
+constexpr int kTile = kSteps * kWaves;
+constexpr int kThreads = kWaves * kWave;
 
 struct RecurrenceArgs {
     Rows gate, x, h;                   // h: out, or dy
@@ -34,50 +39,82 @@ struct RecurrenceArgs {
     Rows initial, last;                // [n][count]: initial, dinitial; last, dlast
     Rows dinitial;
     float *saved;                      // [n][chunks][width]: the state before each chunk
-    float2 *runs;                      // [n][chunks][width]: A and B of each chunk
+    float2 *runs;                      // [n][parts][width]: A and B of each part
     const int32_t *starts;
     int64_t starts_stride;
     int32_t tokens, width, count, chunks, blocks;   // blocks: of channels
+    int32_t tiles, parts, per;                      // of tokens; tiles of a part
 };
 
-// Where a wave's tokens lie: lane i has token i's.
+// Where a wave's tokens lie.  `plain`: all within one sequence that neither
+// starts nor ends at them.
 struct Places {
-    int seq;
+    bool plain;
+    int seq;                         // lane i: the sequence of token i
     unsigned inside, starts, ends;   // a bit for each token
-
-    __device__ __forceinline__ Places(const RecurrenceArgs &a, int64_t worker, int t0, int lane) {
-        const int t = t0 + lane % kSteps;
-        bool in = t < a.tokens, first, final;
-        if (a.starts) {
-            const int32_t *s = a.starts + worker * a.starts_stride;
-            int low = 0, high = a.count + 1;
-            while (low < high) {
-                const int mid = (low + high) / 2;
-                if (s[mid] <= t) low = mid + 1;
-                else high = mid;
-            }
-            in = in && low > 0 && low <= a.count;
-            seq = in ? low - 1 : 0;
-            first = in && s[seq] == t;
-            final = in && (s[seq + 1] - 1 == t || t == a.tokens - 1);
-        } else {
-            seq = 0;
-            first = in && t == 0;
-            final = in && t == a.tokens - 1;
-        }
-        constexpr unsigned kMask = (1u << kSteps) - 1;
-        inside = (unsigned)__ballot(in) & kMask;
-        starts = (unsigned)__ballot(first) & kMask;
-        ends = (unsigned)__ballot(final) & kMask;
-    }
     __device__ __forceinline__ int sequence(int i) const { return __builtin_amdgcn_readlane(seq, i); }
 };
 
-__device__ __forceinline__ bool empty_sequence(const RecurrenceArgs &a, int64_t worker, int s) {
-    if (!a.starts) return a.tokens == 0;
-    const int32_t *st = a.starts + worker * a.starts_stride;
-    return st[s] >= st[s + 1];
-}
+// A worker's starts, one for each lane where they are no more than that.
+struct Starts {
+    const int32_t *at;
+    int count, tokens, lane, own;
+    bool few;
+
+    __device__ __forceinline__ Starts(const RecurrenceArgs &a, int64_t worker, int l) {
+        at = a.starts ? a.starts + worker * a.starts_stride : nullptr;
+        count = a.count, tokens = a.tokens, lane = l;
+        few = count < kWave;
+        own = INT_MAX;
+        if (!at) own = lane == 0 ? 0 : lane == 1 ? tokens : INT_MAX;
+        else if (few && lane <= count) own = at[lane];
+    }
+    // How many start at or before token t.
+    __device__ __forceinline__ int upto(int t) const { return __popcll(__ballot(own <= t)); }
+
+    __device__ __forceinline__ Places places(int t0) const {
+        Places p{false, 0, 0, 0, 0};
+        if (few) {
+            int c = upto(t0 - 1), next = upto(t0);
+            if (next > 0 && next <= count && t0 + kSteps < tokens && !__ballot(own >= t0 && own <= t0 + kSteps)) {
+                p.plain = true;
+                return p;
+            }
+#pragma unroll 1
+            for (int i = 0; i < kSteps; ++i) {
+                const int t = t0 + i, before = c;
+                c = next;
+                next = upto(t + 1);
+                if (t >= tokens || c == 0 || c > count) continue;
+                p.inside |= 1u << i;
+                p.starts |= (unsigned)(c > before) << i;
+                p.ends |= (unsigned)(next > c || t == tokens - 1) << i;
+                p.seq = lane == i ? c - 1 : p.seq;
+            }
+            return p;
+        }
+        const int t = t0 + lane % kSteps;
+        int low = 0, high = count + 1;
+        while (low < high) {
+            const int mid = (low + high) / 2;
+            if (at[mid] <= t) low = mid + 1;
+            else high = mid;
+        }
+        const bool in = t < tokens && low > 0 && low <= count;
+        p.seq = in ? low - 1 : 0;
+        const bool first = in && at[p.seq] == t;
+        const bool final = in && (at[p.seq + 1] - 1 == t || t == tokens - 1);
+        constexpr unsigned kMask = (1u << kSteps) - 1;
+        p.inside = (unsigned)__ballot(in) & kMask;
+        p.starts = (unsigned)__ballot(first) & kMask;
+        p.ends = (unsigned)__ballot(final) & kMask;
+        p.plain = p.inside == kMask && !p.starts && !p.ends;
+        return p;
+    }
+    __device__ __forceinline__ bool empty(int s) const {
+        return at ? at[s] >= at[s + 1] : tokens == 0;
+    }
+};
 
 struct Run {
     float A, B;
@@ -88,318 +125,302 @@ __device__ __forceinline__ Run then(const Run &p, const Run &r) {
     return Run{r.A < 0.0f ? r.A : p.A < 0.0f ? -1.0f : p.A * r.A, r.from(p.B)};
 }
 
-template <typename T>
-__device__ __forceinline__ void load4(const T *p, int left, float (&v)[4]) {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    if (left >= 4) {
-        t4 t;
-        __builtin_memcpy(&t, p, sizeof t);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < left ? (float)p[i] : 0.0f;
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(T *p, int left, const float (&v)[4]) {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    if (left >= 4) {
-        t4 t;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
-        __builtin_memcpy(p, &t, sizeof t);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) p[i] = (T)v[i];
-    }
-}
-
-// The waves' runs of a chunk, in LDS: what leads from the chunk's edge to this
-// wave, and over the whole chunk.
-struct Chunk {
-    Run runs[kChunk / kSteps][kBlock];
-
-    template <bool REVERSE>
-    __device__ __forceinline__ void join(int wave, int lane, const Run (&own)[4], Run (&before)[4], Run (&all)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            runs[wave][lane * 4 + i] = own[i];
-            before[i] = all[i] = Run{1.0f, 0.0f};
-        }
-        __syncthreads();
-        for (int k = 0; k < kChunk / kSteps; ++k) {
-            const int w = REVERSE ? kChunk / kSteps - 1 - k : k;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (w == wave) before[i] = all[i];
-                all[i] = then(all[i], runs[w][lane * 4 + i]);
-            }
-        }
-    }
-};
-
+// A workgroup's channels and tokens; `channel` is in range for every lane, and
+// `live` says whether it is the lane's own.
 struct Where {
     int64_t worker;
-    int chunk, channel, left, wave, lane, t0;
+    int part, wave, lane, channel;
+    bool live;
     __device__ __forceinline__ explicit Where(const RecurrenceArgs &a) {
         const unsigned block = blockIdx.x % a.blocks, at = blockIdx.x / a.blocks;
-        worker = at / a.chunks;
-        chunk = (int)(at % a.chunks);
+        worker = at / a.parts;
+        part = (int)(at % a.parts);
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         lane = threadIdx.x % kWave;
-        channel = (int)block * kBlock + lane * 4;
-        left = a.width - channel;
-        t0 = chunk * kChunk + wave * kSteps;
+        channel = (int)block * kWave + lane;
+        live = channel < a.width;
+        channel = min(channel, a.width - 1);
     }
-    __device__ __forceinline__ int64_t slot(const RecurrenceArgs &a) const {
-        return (worker * a.chunks + chunk) * a.width + channel;
+    template <typename T>
+    __device__ __forceinline__ float get(const Rows &r, int64_t row) const { return (float)row_at<const T>(r, worker, row)[channel]; }
+    __device__ __forceinline__ float state(const Rows &r, int64_t s) const { return r.data ? get<float>(r, s) : 0.0f; }
+    template <typename T>
+    __device__ __forceinline__ void put(const Rows &r, int64_t row, float v) const {
+        if (live) row_at<T>(r, worker, row)[channel] = (T)v;
     }
 };
 
-// The forward pass.  APART: only the chunk's run is wanted, for the kernel that
-// carries states over chunks.
-template <typename T, bool APART>
-__global__ __launch_bounds__(kThreads) void recurrence_kernel(RecurrenceArgs a) {
-    __shared__ Chunk chunk;
-    const Where w(a);
-    const Places at(a, w.worker, w.t0, w.lane);
-    float av[kSteps][4], bv[kSteps][4];
-    Run own[4];
-    if (w.t0 < a.tokens) {
+// A lane's entries of the tokens from t0 on; those behind the last repeat it.
+template <typename T>
+__device__ __forceinline__ void load_steps(const RecurrenceArgs &a, const Where &w, const Rows &r, int t0, T (&v)[kSteps]) {
+    const T *p = row_at<const T>(r, w.worker, 0) + w.channel;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int64_t t = min(w.t0 + s, a.tokens - 1);
-            load4(row_at<const T>(a.gate, w.worker, t) + w.channel, w.left, av[s]);
-            load4(row_at<const T>(a.x, w.worker, t) + w.channel, w.left, bv[s]);
-        }
-    } else {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) av[s][i] = bv[s][i] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) own[i] = Run{1.0f, 0.0f};
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-        const bool in = at.inside >> s & 1, first = at.starts >> s & 1;
-        float init[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (first && a.initial.data)
-            load4(row_at<const float>(a.initial, w.worker, at.sequence(s)) + w.channel, w.left, init);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float c;
-            const float x = bv[s][i];
-            gates<T>(av[s][i], av[s][i], c);
-            bv[s][i] = c * x;
-            if (first) bv[s][i] = fmaf(av[s][i], init[i], bv[s][i]);
-            // Rows of no sequence leave no state.
-            if (!in) bv[s][i] = 0.0f;
-            if (first || !in) av[s][i] = -1.0f;
-            own[i] = then(own[i], Run{av[s][i], bv[s][i]});
-        }
-    }
-    Run before[4], all[4];
-    chunk.join<false>(w.wave, w.lane, own, before, all);
-    if (APART) {
-        if (w.wave == 0)
-            for (int i = 0; i < 4 && i < w.left; ++i) a.runs[w.slot(a) + i] = float2{all[i].A, all[i].B};
-        return;
-    }
-    float h[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.chunks > 1) load4(a.saved + w.slot(a), w.left, h);
-    else if (a.saved && w.wave == 0) store4(a.saved + w.slot(a), w.left, h);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = before[i].from(h[i]);
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-        if (w.t0 + s >= a.tokens) break;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = Run{av[s][i], bv[s][i]}.from(h[i]);
-        store4(row_at<T>(a.h, w.worker, w.t0 + s) + w.channel, w.left, h);
-        if (a.last.data && at.ends >> s & 1)
-            store4(row_at<float>(a.last, w.worker, at.sequence(s)) + w.channel, w.left, h);
-    }
-    // Sequences of no token keep their state.
-    if (a.last.data)
-        for (int s = w.chunk * (kChunk / kSteps) + w.wave; s < a.count; s += a.chunks * (kChunk / kSteps)) {
-            if (!empty_sequence(a, w.worker, s)) continue;
-            float init[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (a.initial.data) load4(row_at<const float>(a.initial, w.worker, s) + w.channel, w.left, init);
-            store4(row_at<float>(a.last, w.worker, s) + w.channel, w.left, init);
-        }
+    for (int i = 0; i < kSteps; ++i) v[i] = p[(int64_t)min(t0 + i, a.tokens - 1) * r.rs];
 }
 
-// The backward pass.  Runs go back in time: what a token's state gets from the
-// one after it.
-template <typename T, bool APART>
-__global__ __launch_bounds__(kThreads) void recurrence_grad_kernel(RecurrenceArgs a) {
-    __shared__ Chunk chunk;
+// The run of a wave's tokens.  av and bv are its a and c x; states of zero where
+// the tokens are in no sequence.
+__device__ __forceinline__ Run run_of(const RecurrenceArgs &a, const Where &w, const Places &at, float (&av)[kSteps],
+                                      float (&bv)[kSteps]) {
+    Run own{1.0f, 0.0f};
+    if (!at.plain) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const bool in = at.inside >> i & 1, first = at.starts >> i & 1;
+            if (first) bv[i] = fmaf(av[i], w.state(a.initial, at.sequence(i)), bv[i]);
+            if (!in) bv[i] = 0.0f;
+            if (first || !in) av[i] = -1.0f;
+            own = then(own, Run{av[i], bv[i]});
+        }
+        return own;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        own.A *= av[i];
+        own.B = fmaf(av[i], own.B, bv[i]);
+    }
+    return own;
+}
+
+// The state before a part, from the runs of those that lead to it.
+template <bool REVERSE>
+__device__ __forceinline__ float state_before(const RecurrenceArgs &a, const Where &w) {
+    float s = 0.0f;
+    const int many = REVERSE ? a.parts - 1 - w.part : w.part;
+#pragma unroll 8
+    for (int k = 0; k < many; ++k) {
+        const float2 v = a.runs[(w.worker * a.parts + (REVERSE ? a.parts - 1 - k : k)) * a.width + w.channel];
+        s = Run{v.x, v.y}.from(s);
+    }
+    return s;
+}
+
+// The run of a part: each wave's of its own eighth, then all of them.
+template <typename T, bool REVERSE>
+__global__ __launch_bounds__(kThreads) void recurrence_part_kernel(RecurrenceArgs a) {
+    __shared__ Run runs[kWaves][kWave];
     const Where w(a);
-    const Places at(a, w.worker, w.t0, w.lane);
-    float av[kSteps][4], cv[kSteps][4], kv[kSteps][4], dv[kSteps][4];
-    Run own[4], before[4], all[4];
-    if (w.t0 < a.tokens) {
+    // Nothing follows the last part.
+    if (w.part == (REVERSE ? 0 : a.parts - 1)) return;
+    const Starts starts(a, w.worker, w.lane);
+    Run all{1.0f, 0.0f};
+    const int turn = REVERSE ? kWaves - 1 - w.wave : w.wave;
+#pragma unroll 1
+    for (int k = 0; k < a.per; ++k) {
+        const int t0 = (w.part * a.per * kWaves + w.wave * a.per + (REVERSE ? a.per - 1 - k : k)) * kSteps;
+        if (t0 >= a.tokens) continue;
+        T graw[kSteps], xraw[kSteps];
+        load_steps(a, w, a.gate, t0, graw);
+        load_steps(a, w, REVERSE ? a.h : a.x, t0, xraw);
+        const Places at = starts.places(t0);
+        float av[kSteps], bv[kSteps];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int64_t t = min(w.t0 + s, a.tokens - 1);
-            load4(row_at<const T>(a.gate, w.worker, t) + w.channel, w.left, av[s]);
-            if (!APART) load4(row_at<const T>(a.x, w.worker, t) + w.channel, w.left, kv[s]);
-            load4(row_at<const T>(a.h, w.worker, t) + w.channel, w.left, dv[s]);
+        for (int i = 0; i < kSteps; ++i) {
+            float c;
+            gates<T>((float)graw[i], av[i], c);
+            bv[i] = REVERSE ? (float)xraw[i] : c * (float)xraw[i];
         }
-    } else {
+        if (!REVERSE) {
+            all = then(all, run_of(a, w, at, av, bv));
+        } else if (at.plain) {
+            float product = 1.0f;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+            for (int i = kSteps - 1; i >= 0; --i) {
+                all.B = av[i] * (all.B + bv[i]);
+                product *= av[i];
+            }
+            all.A = all.A < 0.0f ? all.A : all.A * product;
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) av[s][i] = kv[s][i] = dv[s][i] = 0.0f;
-    }
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) gates<T>(av[s][i], av[s][i], cv[s][i]);
-    if (!APART) {
-        // The states before each token, from the chunk's: kv = (h_(t-1) - x) a c.
-#pragma unroll
-        for (int i = 0; i < 4; ++i) own[i] = Run{1.0f, 0.0f};
-        const auto initial = [&](int s, float (&init)[4]) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) init[i] = 0.0f;
-            if (at.starts >> s & 1 && a.initial.data)
-                load4(row_at<const float>(a.initial, w.worker, at.sequence(s)) + w.channel, w.left, init);
-        };
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const bool in = at.inside >> s & 1, first = at.starts >> s & 1;
-            float init[4];
-            initial(s, init);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float b = cv[s][i] * kv[s][i];
-                own[i] = then(own[i], !in     ? Run{-1.0f, 0.0f}
-                                      : first ? Run{-1.0f, fmaf(av[s][i], init[i], b)}
-                                              : Run{av[s][i], b});
+            for (int i = kSteps - 1; i >= 0; --i) {
+                const bool in = at.inside >> i & 1, first = at.starts >> i & 1, final = at.ends >> i & 1;
+                if (final) all = Run{-1.0f, w.state(a.last, at.sequence(i))};
+                all = !in ? Run{-1.0f, 0.0f} : then(all, Run{av[i], av[i] * bv[i]});
+                if (first) all = Run{-1.0f, 0.0f};
             }
         }
-        chunk.join<false>(w.wave, w.lane, own, before, all);
+    }
+    runs[turn][w.lane] = all;
+    __syncthreads();
+    if (w.wave) return;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) all = k ? then(all, runs[k][w.lane]) : runs[0][w.lane];
+    if (w.live) a.runs[(w.worker * a.parts + w.part) * a.width + w.channel] = float2{all.A, all.B};
+}
+
+// The forward pass.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(RecurrenceArgs a) {
+    __shared__ Run runs[2][kWaves][kWave];
+    const Where w(a);
+    const Starts starts(a, w.worker, w.lane);
+    const int first = w.part * a.per, end = min(first + a.per, a.tiles);
+    T graw[kSteps], xraw[kSteps];
+    if (first < end) {
+        load_steps(a, w, a.gate, first * kTile + w.wave * kSteps, graw);
+        load_steps(a, w, a.x, first * kTile + w.wave * kSteps, xraw);
+    }
+    float carry = state_before<false>(a, w);
+#pragma unroll 1
+    for (int tile = first; tile < end; ++tile) {
+        const int t0 = tile * kTile + w.wave * kSteps;
+        const Places at = starts.places(t0);
+        float av[kSteps], bv[kSteps];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float c;
+            gates<T>((float)graw[i], av[i], c);
+            bv[i] = c * (float)xraw[i];
+        }
+        if (tile + 1 < end) {
+            load_steps(a, w, a.gate, t0 + kTile, graw);
+            load_steps(a, w, a.x, t0 + kTile, xraw);
+        }
+        runs[tile & 1][w.wave][w.lane] = run_of(a, w, at, av, bv);
         __syncthreads();
-        float h[4];
-        load4(a.saved + w.slot(a), w.left, h);
+        float h = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = before[i].from(h[i]);
+        for (int k = 0; k < kWaves; ++k) {
+            if (k == w.wave) h = carry;
+            carry = runs[tile & 1][k][w.lane].from(carry);
+        }
+        if (t0 >= a.tokens) continue;
+        if (a.saved && t0 % kChunk == 0 && w.live) a.saved[(w.worker * a.chunks + t0 / kChunk) * a.width + w.channel] = h;
+        if (at.plain) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const bool in = at.inside >> s & 1, first = at.starts >> s & 1;
-            float init[4];
-            initial(s, init);
+            for (int i = 0; i < kSteps; ++i) {
+                h = fmaf(av[i], h, bv[i]);
+                w.put<T>(a.h, t0 + i, h);
+            }
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float prior = first ? init[i] : h[i], x = kv[s][i];
-                h[i] = in ? fmaf(av[s][i], prior, cv[s][i] * x) : 0.0f;
-                kv[s][i] = (prior - x) * (av[s][i] * cv[s][i]);
+            for (int i = 0; i < kSteps; ++i) {
+                if (t0 + i >= a.tokens) break;
+                h = Run{av[i], bv[i]}.from(h);
+                w.put<T>(a.h, t0 + i, h);
+                if (a.last.data && at.ends >> i & 1) w.put<float>(a.last, at.sequence(i), h);
             }
         }
     }
-    // From the last token to the first: g is what comes from behind.
+    if (a.tiles == 0 && a.saved && w.wave == 0 && w.live) a.saved[w.worker * a.chunks * a.width + w.channel] = 0.0f;
+    // Sequences of no token keep their state.
+    if (a.last.data)
+        for (int s = w.part * kWaves + w.wave; s < a.count; s += a.parts * kWaves)
+            if (starts.empty(s)) w.put<float>(a.last, s, w.state(a.initial, s));
+}
+
+// The backward pass, tile by tile from the last one on.
+struct BothRuns {
+    Run ahead, back;
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads, 2) void recurrence_grad_kernel(RecurrenceArgs a) {
+    __shared__ BothRuns runs[2][kWaves][kWave];
+    const Where w(a);
+    const Starts starts(a, w.worker, w.lane);
+    const int first = w.part * a.per, end = min(first + a.per, a.tiles);
+    T graw[kSteps], xraw[kSteps], draw[kSteps];
+    float sraw = 0.0f;
+    const auto load = [&](int t0) {
+        load_steps(a, w, a.gate, t0, graw);
+        load_steps(a, w, a.x, t0, xraw);
+        load_steps(a, w, a.h, t0, draw);
+        sraw = a.saved[(w.worker * a.chunks + min(t0 / kChunk, a.chunks - 1)) * a.width + w.channel];
+    };
+    if (first < end) load((end - 1) * kTile + w.wave * kSteps);
+    float carry = state_before<true>(a, w);
+#pragma unroll 1
+    for (int tile = end - 1; tile >= first; --tile) {
+        const int t0 = tile * kTile + w.wave * kSteps;
+        const Places at = starts.places(t0);
+        float av[kSteps], cv[kSteps], xv[kSteps], dv[kSteps], h = sraw;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) own[i] = Run{1.0f, 0.0f};
-#pragma unroll
-    for (int s = kSteps - 1; s >= 0; --s) {
-        const bool in = at.inside >> s & 1, first = at.starts >> s & 1, final = at.ends >> s & 1;
-        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (final && a.last.data)
-            load4(row_at<const float>(a.last, w.worker, at.sequence(s)) + w.channel, w.left, d);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            // g -> a (dy + g), from a sequence's last token on from dlast alone; what
-            // passes its first one is its initial state's.
-            if (final) own[i] = Run{-1.0f, d[i]};
-            own[i] = !in ? Run{-1.0f, 0.0f} : then(own[i], Run{av[s][i], av[s][i] * dv[s][i]});
-            if (first) own[i] = Run{-1.0f, 0.0f};
+        for (int i = 0; i < kSteps; ++i) {
+            gates<T>((float)graw[i], av[i], cv[i]);
+            xv[i] = (float)xraw[i], dv[i] = (float)draw[i];
         }
-    }
-    chunk.join<true>(w.wave, w.lane, own, before, all);
-    if (APART) {
-        if (w.wave == 0)
-            for (int i = 0; i < 4 && i < w.left; ++i) a.runs[w.slot(a) + i] = float2{all[i].A, all[i].B};
-        return;
-    }
-    float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    // The carrying kernel left in A what comes into the chunk.
-    if (a.chunks > 1) {
+        if (tile > first) load(t0 - kTile);
+        BothRuns own{{1.0f, 0.0f}, {1.0f, 0.0f}};
+        if (at.plain) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < w.left) g[i] = a.runs[w.slot(a) + i].x;
-    }
+            for (int i = 0; i < kSteps; ++i) {
+                own.ahead.A *= av[i];
+                own.ahead.B = fmaf(av[i], own.ahead.B, cv[i] * xv[i]);
+            }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g[i] = before[i].from(g[i]);
+            for (int i = kSteps - 1; i >= 0; --i) own.back.B = av[i] * (own.back.B + dv[i]);
+            own.back.A = own.ahead.A;
+        } else {
 #pragma unroll
-    for (int s = kSteps - 1; s >= 0; --s) {
-        if (w.t0 + s >= a.tokens) continue;
-        const bool in = at.inside >> s & 1, first = at.starts >> s & 1, final = at.ends >> s & 1;
-        if (final) {
+            for (int i = 0; i < kSteps; ++i) {
+                const bool in = at.inside >> i & 1, start = at.starts >> i & 1;
+                float b = cv[i] * xv[i];
+                if (start) b = fmaf(av[i], w.state(a.initial, at.sequence(i)), b);
+                own.ahead = then(own.ahead, !in ? Run{-1.0f, 0.0f} : Run{start ? -1.0f : av[i], b});
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] = 0.0f;
-            if (a.last.data) load4(row_at<const float>(a.last, w.worker, at.sequence(s)) + w.channel, w.left, g);
+            for (int i = kSteps - 1; i >= 0; --i) {
+                const bool in = at.inside >> i & 1, start = at.starts >> i & 1, final = at.ends >> i & 1;
+                // g -> a (dy + g), from a sequence's last token on from dlast alone; what
+                // passes its first one is its initial state's.
+                if (final) own.back = Run{-1.0f, w.state(a.last, at.sequence(i))};
+                own.back = !in ? Run{-1.0f, 0.0f} : then(own.back, Run{av[i], av[i] * dv[i]});
+                if (start) own.back = Run{-1.0f, 0.0f};
+            }
         }
-        float dgate[4], dx[4];
+        runs[tile & 1][w.wave][w.lane] = own;
+        __syncthreads();
+        for (int k = w.wave & ~(kChunk / kSteps - 1); k < w.wave; ++k) h = runs[tile & 1][k][w.lane].ahead.from(h);
+        float g = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float dh = dv[s][i] + g[i];
-            dgate[i] = in ? dh * kv[s][i] : 0.0f;
-            dx[i] = in ? dh * cv[s][i] : 0.0f;
-            g[i] = in ? dh * av[s][i] : 0.0f;
+        for (int k = kWaves - 1; k >= 0; --k) {
+            if (k == w.wave) g = carry;
+            carry = runs[tile & 1][k][w.lane].back.from(carry);
         }
-        store4(row_at<T>(a.dgate, w.worker, w.t0 + s) + w.channel, w.left, dgate);
-        store4(row_at<T>(a.dx, w.worker, w.t0 + s) + w.channel, w.left, dx);
-        if (first) {
-            if (a.dinitial.data) store4(row_at<float>(a.dinitial, w.worker, at.sequence(s)) + w.channel, w.left, g);
+        if (t0 >= a.tokens) continue;
+        if (at.plain) {
+            // xv: what dh is times in dgate.
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] = 0.0f;
+            for (int i = 0; i < kSteps; ++i) {
+                const float x = xv[i];
+                xv[i] = (h - x) * (av[i] * cv[i]);
+                h = fmaf(av[i], h, cv[i] * x);
+            }
+#pragma unroll
+            for (int i = kSteps - 1; i >= 0; --i) {
+                const float dh = dv[i] + g;
+                w.put<T>(a.dgate, t0 + i, dh * xv[i]);
+                w.put<T>(a.dx, t0 + i, dh * cv[i]);
+                g = dh * av[i];
+            }
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const bool in = at.inside >> i & 1, start = at.starts >> i & 1;
+            const float prior = start ? w.state(a.initial, at.sequence(i)) : h, x = xv[i];
+            h = in ? fmaf(av[i], prior, cv[i] * x) : 0.0f;
+            xv[i] = (prior - x) * (av[i] * cv[i]);
+        }
+#pragma unroll
+        for (int i = kSteps - 1; i >= 0; --i) {
+            if (t0 + i >= a.tokens) continue;
+            const bool in = at.inside >> i & 1, start = at.starts >> i & 1, final = at.ends >> i & 1;
+            if (final) g = w.state(a.last, at.sequence(i));
+            const float dh = dv[i] + g;
+            w.put<T>(a.dgate, t0 + i, in ? dh * xv[i] : 0.0f);
+            w.put<T>(a.dx, t0 + i, in ? dh * cv[i] : 0.0f);
+            g = in ? dh * av[i] : 0.0f;
+            if (start) {
+                if (a.dinitial.data) w.put<float>(a.dinitial, at.sequence(i), g);
+                g = 0.0f;
+            }
         }
     }
     if (a.dinitial.data)
-        for (int s = w.chunk * (kChunk / kSteps) + w.wave; s < a.count; s += a.chunks * (kChunk / kSteps)) {
-            if (!empty_sequence(a, w.worker, s)) continue;
-            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (a.last.data) load4(row_at<const float>(a.last, w.worker, s) + w.channel, w.left, d);
-            store4(row_at<float>(a.dinitial, w.worker, s) + w.channel, w.left, d);
-        }
-}
-
-// Carries states over the chunks of a channel.  A workgroup has 16 channels and
-// 16 stretches of chunks: each stretch's run, then the states.
-template <bool REVERSE>
-__global__ __launch_bounds__(256) void carry_kernel(RecurrenceArgs a) {
-    __shared__ Run runs[16][16];
-    const unsigned blocks = (a.width + 15) / 16;
-    const int64_t worker = blockIdx.x / blocks;
-    const int c = (int)(blockIdx.x % blocks) * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
-    const int per = (a.chunks + 15) / 16, from = min(part * per, a.chunks), to = min(from + per, a.chunks);
-    const auto at = [&](int k) {
-        return (worker * a.chunks + (REVERSE ? a.chunks - 1 - k : k)) * a.width + c;
-    };
-    Run r{1.0f, 0.0f};
-    if (c < a.width)
-#pragma unroll 8
-        for (int k = from; k < to; ++k) {
-            const float2 v = a.runs[at(k)];
-            r = then(r, Run{v.x, v.y});
-        }
-    runs[part][threadIdx.x % 16] = r;
-    __syncthreads();
-    if (c >= a.width) return;
-    float s = 0.0f;
-    for (int k = 0; k < part; ++k) s = runs[k][threadIdx.x % 16].from(s);
-#pragma unroll 8
-    for (int k = from; k < to; ++k) {
-        const float2 v = a.runs[at(k)];
-        if (REVERSE) a.runs[at(k)].x = s;
-        else a.saved[at(k)] = s;
-        s = Run{v.x, v.y}.from(s);
-    }
+        for (int s = w.part * kWaves + w.wave; s < a.count; s += a.parts * kWaves)
+            if (starts.empty(s)) w.put<float>(a.dinitial, s, w.state(a.last, s));
 }
 
 // ---- host side -------------------------------------------------------------------------
@@ -408,14 +429,29 @@ constexpr int64_t kMaxTokens = 1 << 30;
 
 int64_t chunks_of(int64_t tokens) { return tiles(tokens, kChunk); }
 
+// Parts of the tokens, and tiles of each.  Two workgroups for a CU, but one
+// where that needs no parts: they read gate and x twice.
+struct RecurrencePlan {
+    int32_t tiles, parts, per;
+    size_t workspace;
+    RecurrencePlan(int32_t n, int64_t tokens, int64_t width) {
+        const int64_t blocks = n * layer_plan::tiles(width, kWave);
+        tiles = (int32_t)layer_plan::tiles(tokens, kTile);
+        const int64_t want = blocks >= kCus * 3 / 4 ? 1 : std::min<int64_t>(layer_plan::tiles(2 * kCus, blocks), tiles / 2);
+        per = (int32_t)layer_plan::tiles(std::max(tiles, 1), std::max<int64_t>(want, 1));
+        parts = (int32_t)layer_plan::tiles(std::max(tiles, 1), per);
+        workspace = parts > 1 ? (size_t)n * parts * width * 8 : 0;
+    }
+};
+
 struct RecurrenceCall : Call {
     bool shape(int32_t n, int64_t tokens, int64_t width, int32_t count) {
         if (!sizes(n, tokens, width, "tokens")) return false;
         if (tokens > kMaxTokens) fail(refuse("tokens must be in 0..2^30"));
         else if (count < 1 || count > 1 << 30) fail(refuse("count must be in 1..2^30"));
         else if ((__int128)n * count * width > ((__int128)1 << 50)) fail(refuse("n * count * width is more than 2^50"));
-        else if (n * chunks_of(tokens) * tiles(width, kBlock) > kMaxBlocks || n * tiles(width, 16) > kMaxBlocks)
-            fail(refuse("n * tokens * width is too large for a launch"));
+        else if (n * tiles(width, kWave) > kMaxBlocks)
+            fail(refuse("n * width is too large for a launch"));
         return code == RELAYSUM_OK;
     }
 
@@ -438,11 +474,6 @@ struct RecurrenceCall : Call {
     }
 };
 
-template <typename F>
-void with_grid(const RecurrenceArgs &a, int32_t n, F f) {
-    f(dim3((unsigned)(n * (int64_t)a.chunks * a.blocks)), dim3(kThreads), dim3((unsigned)(n * ((a.width + 15) / 16))));
-}
-
 }  // namespace
 
 extern "C" {
@@ -455,8 +486,7 @@ int64_t relaysum_recurrence_workspace(int32_t n, int64_t tokens, int64_t width) 
     RecurrenceCall c;
     if (!c.shape(n, tokens, width, 1)) return -1;
     g_error[0] = '\0';
-    const int64_t chunks = chunks_of(tokens);
-    return chunks > 1 ? n * chunks * width * 12 : 0;
+    return (int64_t)RecurrencePlan(n, tokens, width).workspace;
 }
 
 int relaysum_recurrence(int32_t n, int64_t tokens, int64_t width, int32_t count, const int32_t *starts,
@@ -475,7 +505,7 @@ int relaysum_recurrence(int32_t n, int64_t tokens, int64_t width, int32_t count,
         c.states("initial", initial, n, count, width, false);
         c.states("last", last, n, count, width, true);
         if (saved) c.span("saved", saved, (size_t)n * chunks * width * 4, 4, true);
-        const size_t need = chunks > 1 ? (size_t)n * chunks * width * 12 : 0;
+        const size_t need = RecurrencePlan(n, tokens, width).workspace;
         if (need > workspace_bytes)
             c.fail(refuse("the workspace has %zu bytes, %zu are needed", workspace_bytes, need));
         c.span("workspace", workspace, need, 8, true);
@@ -485,20 +515,19 @@ int relaysum_recurrence(int32_t n, int64_t tokens, int64_t width, int32_t count,
     a.gate = rows_of(gate, n, tokens), a.x = rows_of(x, n, tokens), a.h = rows_of(h, n, tokens);
     a.initial = rows_of(initial, n, count), a.last = rows_of(last, n, count);
     a.runs = static_cast<float2 *>(workspace);
-    a.saved = saved || chunks == 1 ? saved : reinterpret_cast<float *>(a.runs + n * chunks * width);
+    a.saved = saved;
     a.starts = starts, a.starts_stride = n > 1 ? starts_stride : 0;
     a.tokens = (int32_t)tokens, a.width = (int32_t)width, a.count = count;
-    a.chunks = (int32_t)chunks, a.blocks = (int32_t)tiles(width, kBlock);
+    a.chunks = (int32_t)chunks, a.blocks = (int32_t)tiles(width, kWave);
+    const RecurrencePlan p(n, tokens, width);
+    a.tiles = p.tiles, a.parts = p.parts, a.per = p.per;
+    const dim3 grid((unsigned)((int64_t)n * a.blocks * a.parts)), block(kThreads);
     const hipStream_t st = (hipStream_t)hip_stream;
     with_type(gate->type, [&](auto zero) {
         using T = decltype(zero);
-        with_grid(a, n, [&](dim3 grid, dim3 block, dim3 carry) {
-            if (chunks > 1) {
-                hipLaunchKernelGGL(HIP_KERNEL_NAME(recurrence_kernel<T, true>), grid, block, 0, st, a);
-                hipLaunchKernelGGL(HIP_KERNEL_NAME(carry_kernel<false>), carry, dim3(256), 0, st, a);
-            }
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(recurrence_kernel<T, false>), grid, block, 0, st, a);
-        });
+        if (a.parts > 1)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(recurrence_part_kernel<T, false>), grid, block, 0, st, a);
+        hipLaunchKernelGGL(recurrence_kernel<T>, grid, block, 0, st, a);
     });
     return done("relaysum_recurrence");
 }
@@ -525,7 +554,7 @@ int relaysum_recurrence_backward(int32_t n, int64_t tokens, int64_t width, int32
         c.states("dlast", dlast, n, count, width, false);
         c.states("dinitial", dinitial, n, count, width, true);
         c.span("saved", saved, (size_t)n * chunks * width * 4, 4, false);
-        const size_t need = chunks > 1 ? (size_t)n * chunks * width * 8 : 0;
+        const size_t need = RecurrencePlan(n, tokens, width).workspace;
         if (need > workspace_bytes)
             c.fail(refuse("the workspace has %zu bytes, %zu are needed", workspace_bytes, need));
         c.span("workspace", workspace, need, 8, true);
@@ -539,17 +568,16 @@ int relaysum_recurrence_backward(int32_t n, int64_t tokens, int64_t width, int32
     a.saved = const_cast<float *>(saved);
     a.starts = starts, a.starts_stride = n > 1 ? starts_stride : 0;
     a.tokens = (int32_t)tokens, a.width = (int32_t)width, a.count = count;
-    a.chunks = (int32_t)chunks, a.blocks = (int32_t)tiles(width, kBlock);
+    a.chunks = (int32_t)chunks, a.blocks = (int32_t)tiles(width, kWave);
+    const RecurrencePlan p(n, tokens, width);
+    a.tiles = p.tiles, a.parts = p.parts, a.per = p.per;
+    const dim3 grid((unsigned)((int64_t)n * a.blocks * a.parts)), block(kThreads);
     const hipStream_t st = (hipStream_t)hip_stream;
     with_type(gate->type, [&](auto zero) {
         using T = decltype(zero);
-        with_grid(a, n, [&](dim3 grid, dim3 block, dim3 carry) {
-            if (chunks > 1) {
-                hipLaunchKernelGGL(HIP_KERNEL_NAME(recurrence_grad_kernel<T, true>), grid, block, 0, st, a);
-                hipLaunchKernelGGL(HIP_KERNEL_NAME(carry_kernel<true>), carry, dim3(256), 0, st, a);
-            }
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(recurrence_grad_kernel<T, false>), grid, block, 0, st, a);
-        });
+        if (a.parts > 1)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(recurrence_part_kernel<T, true>), grid, block, 0, st, a);
+        hipLaunchKernelGGL(recurrence_grad_kernel<T>, grid, block, 0, st, a);
     });
     return done("relaysum_recurrence_backward");
 }
