@@ -7,7 +7,7 @@
 //
 // channel by channel.  A run of tokens takes a state s to A s + B, and runs
 // compose.  A workgroup has 64 channels, one for each lane, and walks through its
-// tokens in tiles of 128: each of its 8 waves has 16 of them in registers, the
+// tokens in tiles of 128: each of its 16 waves has 8 of them in registers, the
 // waves' runs go through LDS, and the next tile is on its way meanwhile.  So gate
 // and x are read once.  Where there are too few channels for the device, tokens
 // are split into parts: a first kernel finds the run of each part, and every
@@ -28,8 +28,8 @@
 namespace {
 
 constexpr int kChunk = 64;      // tokens between the states that are kept
-constexpr int kSteps = 16;      // tokens of a wave in a tile
-constexpr int kWaves = 8;
+constexpr int kSteps = 8;      // tokens of a wave in a tile
+constexpr int kWaves = 16;
 constexpr int kTile = kSteps * kWaves;
 constexpr int kThreads = kWaves * kWave;
 
@@ -153,9 +153,17 @@ struct Where {
 // A lane's entries of the tokens from t0 on; those behind the last repeat it.
 template <typename T>
 __device__ __forceinline__ void load_steps(const RecurrenceArgs &a, const Where &w, const Rows &r, int t0, T (&v)[kSteps]) {
-    const T *p = row_at<const T>(r, w.worker, 0) + w.channel;
+    const T *p = row_at<const T>(r, w.worker, min(t0, a.tokens - 1));
+    if (t0 + kSteps <= a.tokens) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) v[i] = p[(int64_t)min(t0 + i, a.tokens - 1) * r.rs];
+        for (int i = 0; i < kSteps; ++i, p += r.rs) v[i] = p[w.channel];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        v[i] = p[w.channel];
+        if (t0 + i + 1 < a.tokens) p += r.rs;
+    }
 }
 
 // The run of a wave's tokens.  av and bv are its a and c x; states of zero where
@@ -195,7 +203,7 @@ __device__ __forceinline__ float state_before(const RecurrenceArgs &a, const Whe
     return s;
 }
 
-// The run of a part: each wave's of its own eighth, then all of them.
+// The run of a part: each wave's of its own stretch, then all of them.
 template <typename T, bool REVERSE>
 __global__ __launch_bounds__(kThreads) void recurrence_part_kernel(RecurrenceArgs a) {
     __shared__ Run runs[kWaves][kWave];
@@ -315,7 +323,7 @@ struct BothRuns {
 };
 
 template <typename T>
-__global__ __launch_bounds__(kThreads, 2) void recurrence_grad_kernel(RecurrenceArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void recurrence_grad_kernel(RecurrenceArgs a) {
     __shared__ BothRuns runs[2][kWaves][kWave];
     const Where w(a);
     const Starts starts(a, w.worker, w.lane);
@@ -429,8 +437,8 @@ constexpr int64_t kMaxTokens = 1 << 30;
 
 int64_t chunks_of(int64_t tokens) { return tiles(tokens, kChunk); }
 
-// Parts of the tokens, and tiles of each.  Two workgroups for a CU, but one
-// where that needs no parts: they read gate and x twice.
+// Parts of the tokens, and tiles of each.  Two workgroups for a CU; three
+// quarters of them will do where that needs no parts, which read gate and x twice.
 struct RecurrencePlan {
     int32_t tiles, parts, per;
     size_t workspace;
