@@ -115,79 +115,128 @@ struct BlockNormGradArgs {
     int32_t width, stride, parts;
 };
 
-// A workgroup owns every parts-th block of rows of one worker; threads keep
-// their columns' sums in registers over all of them.
+// What a thread reads of a row, as it lies in memory.
 template <typename T, int TPR, int J, bool GATE>
-__global__ __launch_bounds__(block_of(TPR)) void blocknorm_grad_kernel(BlockNormGradArgs a) {
+struct GradRow {
+    v8_t<T> dy[J], z[J], dsum[J], gate[GATE ? J : 1];
+    u2_t codes[J];
+    int8_t exps[J];
+    float rstd, post_rstd;
+
+    static __device__ __forceinline__ v8_t<T> chunk(const Rows &r, int64_t worker, int64_t t, int at, int left) {
+        v8_t<T> v = {};
+        if (!r.data || left <= 0) return v;
+        const T *p = row_at<const T>(r, worker, t) + at;
+        if (left >= 8) {
+            __builtin_memcpy(&v, p, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (T)0.0f;
+        }
+        return v;
+    }
+    __device__ __forceinline__ void load(const BlockNormGradArgs &a, int64_t worker, int64_t t, int lane) {
+        const int64_t row = worker * a.rows + t;
+        rstd = a.rstd[row], post_rstd = a.post_rstd[row];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int at = (lane + j * TPR) * 8, left = a.width - at;
+            dy[j] = chunk(a.dy, worker, t, at, left);
+            z[j] = chunk(a.z, worker, t, at, left);
+            dsum[j] = chunk(a.dsum, worker, t, at, left);
+            if (GATE) gate[j] = chunk(a.gate, worker, t, at, left);
+            codes[j] = u2_t{0, 0};
+            exps[j] = 0;
+            if (left > 0) {
+                codes[j] = *reinterpret_cast<const u2_t *>(a.saved.codes + row * a.stride + at);
+                exps[j] = a.saved.exps[row * a.saved.groups + (a.saved.groups > 1 ? at / kGroup : 0)];
+            }
+        }
+    }
+};
+
+// A workgroup owns every parts-th block of rows of one worker; threads keep
+// their columns' sums in registers over all of them and, but in workgroups of
+// 1024 (which have 128 registers), the worker's weights and the next row: at
+// 16 x 2048 x 1024 bfloat16 119 us (4.2 TB/s) for 268 us without them.
+template <typename T, int TPR, int J, bool GATE>
+__global__ __launch_bounds__(block_of(TPR), (TPR > 256 ? 4 : J == 1 ? 3 : 2)) void blocknorm_grad_kernel(BlockNormGradArgs a) {
     constexpr int kRows = block_of(TPR) / TPR;
+    constexpr bool kAhead = TPR <= 256;
     __shared__ float red[16];
     __shared__ float sums[kRows > 1 ? kRows * TPR * J * 8 : 1];
-    const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const int lane = threadIdx.x % TPR;
+    // The same for a whole wave, where that is one row's or part of it.
+    const int slot = TPR < kWave ? threadIdx.x / TPR : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     const int64_t worker = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts;
     const float scale = a.scale[worker * a.scale_stride];
+    const int64_t step = (int64_t)a.parts * kRows;
     float dw[J][8], dp[J][8], dscale = 0.0f;
+    float weight[kAhead ? J : 1][8], post[kAhead ? J : 1][8];
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[j][i] = dp[j][i] = 0.0f;
-    for (int64_t t = (int64_t)part * kRows + slot; t < a.rows; t += (int64_t)a.parts * kRows) {
-        const int64_t row = worker * a.rows + t;
-        const float rstd = a.rstd[row], post_rstd = a.post_rstd[row];
-        float ds[J][8], zh[J][8], g[J][8], dsum[J][8], dot = 0.0f;
-        float sh[J][8];
+        if constexpr (kAhead) {
+            const int at = (lane + j * TPR) * 8;
+            load8(a.weight + worker * a.weight_stride + at, a.width - at, weight[j]);
+            load8(a.post_weight + worker * a.post_stride + at, a.width - at, post[j]);
+        }
+    }
+    GradRow<T, TPR, J, GATE> in;
+    int64_t t = (int64_t)part * kRows + slot;
+    if (kAhead && t < a.rows) in.load(a, worker, t, lane);
+    for (; t < a.rows; t += step) {
+        if (!kAhead) in.load(a, worker, t, lane);
+        const float rstd = in.rstd, post_rstd = in.post_rstd;
+        float ds[J][8], zh[J][8], sh[J][8], dot = 0.0f, dot2 = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int at = (lane + j * TPR) * 8;
+            const float sc = at < a.width ? rstd * scale_of(in.exps[j]) : 0.0f;
             float w[8];
-            load8(row_at<const T>(a.dy, worker, t) + at, a.width - at, ds[j]);
-            load8(row_at<const T>(a.z, worker, t) + at, a.width - at, zh[j]);
-            if (GATE) load8(row_at<const T>(a.gate, worker, t) + at, a.width - at, g[j]);
-            if (a.dsum.data) load8(row_at<const T>(a.dsum, worker, t) + at, a.width - at, dsum[j]);
-            load8(a.weight + worker * a.weight_stride + at, a.width - at, w);
-            u2_t q = {0, 0};
-            float sc = 0.0f;
-            if (at < a.width) {
-                q = *reinterpret_cast<const u2_t *>(a.saved.codes + row * a.stride + at);
-                sc = rstd * scale_of(a.saved.exps[row * a.saved.groups + (a.saved.groups > 1 ? at / kGroup : 0)]);
-            }
+            if constexpr (!kAhead) load8(a.weight + worker * a.weight_stride + at, a.width - at, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                sh[j][i] = code_at(i < 4 ? q.x : q.y, i % 4) * sc;
+                if constexpr (kAhead) w[i] = weight[j][i];
+                ds[j][i] = (float)in.dy[j][i];
+                sh[j][i] = code_at(i < 4 ? in.codes[j].x : in.codes[j].y, i % 4) * sc;
                 dw[j][i] = fmaf(ds[j][i], sh[j][i], dw[j][i]);
                 ds[j][i] *= w[i];
                 dot = fmaf(ds[j][i], sh[j][i], dot);
             }
         }
         dot = row_reduce<TPR, float, pick_sum>(dot, red) / (float)a.width;
-        float dot2 = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int at = (lane + j * TPR) * 8;
-            float w[8];
-            load8(a.post_weight + worker * a.post_stride + at, a.width - at, w);
+            float w[8], dgate[8];
+            if constexpr (!kAhead) load8(a.post_weight + worker * a.post_stride + at, a.width - at, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                if constexpr (kAhead) w[i] = post[j][i];
                 const float own = rstd * fmaf(-sh[j][i], dot, ds[j][i]);
-                ds[j][i] = a.dsum.data ? dsum[j][i] + own : own;
-                zh[j][i] *= post_rstd;
+                ds[j][i] = a.dsum.data ? (float)in.dsum[j][i] + own : own;
+                zh[j][i] = (float)in.z[j][i] * post_rstd;
                 float gate = 1.0f, rest = 0.0f;
-                if (GATE) gates<T>(g[j][i], gate, rest);
+                if (GATE) gates<T>((float)in.gate[GATE ? j : 0][i], gate, rest);
                 const float dg = ds[j][i] * gate;            // of scale * u
                 const float u = zh[j][i] * w[i];
                 if (at + i < a.width) dscale = fmaf(dg, u, dscale);
-                g[j][i] = dg * scale * u * rest;             // dgate
+                dgate[i] = dg * scale * u * rest;
                 dp[j][i] = fmaf(dg * scale, zh[j][i], dp[j][i]);
                 sh[j][i] = dg * scale * w[i];                // of zh
                 if (at + i < a.width) dot2 = fmaf(sh[j][i], zh[j][i], dot2);
             }
+            if (GATE) store8(row_at<T>(a.dgate, worker, t) + at, a.width - at, dgate);
         }
+        if (kAhead && t + step < a.rows) in.load(a, worker, t + step, lane);
         dot2 = row_reduce<TPR, float, pick_sum>(dot2, red) / (float)a.width;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int at = (lane + j * TPR) * 8;
             store8(row_at<T>(a.ds, worker, t) + at, a.width - at, ds[j]);
-            if (GATE) store8(row_at<T>(a.dgate, worker, t) + at, a.width - at, g[j]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sh[j][i] = post_rstd * fmaf(-zh[j][i], dot2, sh[j][i]);
             store8(row_at<T>(a.dz, worker, t) + at, a.width - at, sh[j]);
