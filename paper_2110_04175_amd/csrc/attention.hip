@@ -131,7 +131,7 @@ ForwardPlan plan_forward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
 
 struct BackwardPlan {
     int32_t norms, parts;
-    size_t stats, largest, bounds, sums;   // offsets
+    size_t stats, largest, bounds, order, sums;   // offsets
     size_t workspace;
 };
 
@@ -148,6 +148,7 @@ BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t head
     p.stats = at, at += tiles((size_t)n * rows * 8, 16) * 16;
     p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.norms * 8, 16) * 16 : 0;
     p.bounds = at, at += (size_t)n * tiles(tokens * (heads / kv), 32) * 16;
+    p.order = at, at += tiles((size_t)n * tiles(keys, 128) * 4, 16) * 16;
     p.sums = at, at += p.parts > 1 ? (size_t)pairs * keys * p.parts * 2 * width * 4 : 0;
     p.workspace = at;
     return p;
@@ -297,6 +298,7 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
     a.stats = reinterpret_cast<float2 *>(ws + p.stats);
     a.largest = reinterpret_cast<float2 *>(ws + p.largest);
     a.bounds = reinterpret_cast<int4 *>(ws + p.bounds);
+    a.order = reinterpret_cast<int32_t *>(ws + p.order);
     a.part_out = reinterpret_cast<float *>(ws + p.sums);
     a.norms = p.norms, a.parts = p.parts;
     a.bound_stride = a.range_stride ? tiles(a.rows, 32) : 0;

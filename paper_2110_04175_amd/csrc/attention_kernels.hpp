@@ -470,56 +470,39 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 
 // ---- backward ----------------------------------------------------------------------
 
-// lse in powers of two and delta = dout . out of every row, 16 lanes each; for binary16 also the largest
-// squared norms of the rows of dout that see something and of v's.
+// For binary16: the largest squared norms of the rows of dout that see something
+// and of v's, 16 lanes a row.
 template <typename T>
-__global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(256) void attention_norms_kernel(AttentionArgs a) {
     __shared__ float red[2][16];
     const int64_t worker = blockIdx.x / a.norms;
     const int part = (int)(blockIdx.x % a.norms), lane = threadIdx.x % 16, slot = threadIdx.x / 16;
-    float most_dout = 0.0f, most_v = 0.0f;
-    const int64_t rows = (int64_t)a.tokens * a.heads;
-    for (int64_t r = (int64_t)part * 16 + slot; r < rows; r += (int64_t)a.norms * 16) {
-        const int t = (int)(r / a.heads), head = (int)(r % a.heads);
-        const T *x = head_at<const T>(a.dout, worker, t, head), *y = head_at<const T>(a.out, worker, t, head);
-        float dot = 0.0f, norm = 0.0f;
+    const auto squares = [&](const T *x) {
+        float norm = 0.0f;
         for (int k = lane * 8; k < a.width; k += 128) {
-            float u[8], v[8];
+            float u[8];
             load8(x + k, a.width - k, u);
-            load8(y + k, a.width - k, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dot = fmaf(u[i], v[i], dot), norm = fmaf(u[i], u[i], norm);
+            for (int i = 0; i < 8; ++i) norm = fmaf(u[i], u[i], norm);
         }
-        dot = row_reduce<16, float, pick_sum>(dot, nullptr);
-        if (lane == 0)
-            a.stats[(worker * a.kv + head / a.group) * a.rows + (int64_t)t * a.group + head % a.group] =
-                float2{a.lse[(worker * a.heads + head) * a.tokens + t] * kLog2e, dot};
-        if (std::is_same<T, _Float16>::value) {
-            norm = row_reduce<16, float, pick_sum>(norm, nullptr);
-            const int2 s = seen(a, worker, t);
-            if (s.x < s.y && norm < INFINITY) most_dout = fmaxf(most_dout, norm);
-        }
+        return row_reduce<16, float, pick_sum>(norm, nullptr);
+    };
+    float most_dout = 0.0f, most_v = 0.0f;
+    for (int64_t r = (int64_t)part * 16 + slot; r < (int64_t)a.tokens * a.heads; r += (int64_t)a.norms * 16) {
+        const int t = (int)((unsigned)r / (unsigned)a.heads), head = (int)((unsigned)r % (unsigned)a.heads);
+        const int2 s = seen(a, worker, t);
+        const float norm = squares(head_at<const T>(a.dout, worker, t, head));
+        if (s.x < s.y && norm < INFINITY) most_dout = fmaxf(most_dout, norm);
     }
-    if (std::is_same<T, _Float16>::value) {
-        const int64_t vrows = (int64_t)a.keys * a.kv;
-        for (int64_t r = (int64_t)part * 16 + slot; r < vrows; r += (int64_t)a.norms * 16) {
-            const T *x = head_at<const T>(a.v, worker, r / a.kv, (int)(r % a.kv));
-            float norm = 0.0f;
-            for (int k = lane * 8; k < a.width; k += 128) {
-                float u[8];
-                load8(x + k, a.width - k, u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) norm = fmaf(u[i], u[i], norm);
-            }
-            norm = row_reduce<16, float, pick_sum>(norm, nullptr);
-            if (norm < INFINITY) most_v = fmaxf(most_v, norm);
-        }
-        if (lane == 0) red[0][slot] = most_dout, red[1][slot] = most_v;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int i = 1; i < 16; ++i) most_dout = fmaxf(most_dout, red[0][i]), most_v = fmaxf(most_v, red[1][i]);
-            a.largest[blockIdx.x] = float2{most_dout, most_v};
-        }
+    for (int64_t r = (int64_t)part * 16 + slot; r < (int64_t)a.keys * a.kv; r += (int64_t)a.norms * 16) {
+        const float norm = squares(head_at<const T>(a.v, worker, r / a.kv, (int)(r % a.kv)));
+        if (norm < INFINITY) most_v = fmaxf(most_v, norm);
+    }
+    if (lane == 0) red[0][slot] = most_dout, red[1][slot] = most_v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) most_dout = fmaxf(most_dout, red[0][i]), most_v = fmaxf(most_v, red[1][i]);
+        a.largest[blockIdx.x] = float2{most_dout, most_v};
     }
 }
 
@@ -540,6 +523,38 @@ __global__ __launch_bounds__(256) void attention_bounds_kernel(AttentionArgs a, 
         b.w = max(b.w, __shfl_xor(b.w, m));
     }
     if (threadIdx.x % 32 == 0) a.bounds[at] = b;
+}
+
+// The tiles of 128 keys of every worker (of all, where they have the same ranges)
+// in the order of how many blocks of rows see them, the most first: a device
+// whose last workgroups have the least to do is done sooner (16 x 2048 tokens, 16
+// heads on 4 of 64: 1024 workgroups, two for a CU at once).  By a workgroup of
+// its own: each block opens and closes a run of tiles, sums give the counts, and
+// a tile's place is the number of those that come before it.
+constexpr int kMostOrdered = 2048;
+
+template <typename T>
+__global__ __launch_bounds__(1024) void attention_order_kernel(AttentionArgs a, int workers) {
+    __shared__ int count[kMostOrdered + 1];
+    const int all = workers * a.tiles, blocks = (a.rows + 31) / 32;
+    for (int i = threadIdx.x; i < all; i += 1024) count[i] = 0;
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < (int64_t)workers * blocks; i += 1024) {
+        const int4 b = a.bounds[i];
+        if (b.x >= b.w || b.x >= a.keys) continue;
+        const int worker = (int)(i / blocks), from = b.x / 128, to = (b.w - 1) / 128 + 1;
+        atomicAdd(&count[worker * a.tiles + from], 1);
+        if (to < a.tiles) atomicSub(&count[worker * a.tiles + to], 1);
+    }
+    __syncthreads();
+    for (int w = threadIdx.x; w < workers; w += 1024)
+        for (int i = 1; i < a.tiles; ++i) count[w * a.tiles + i] += count[w * a.tiles + i - 1];
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += 1024) {
+        int before = 0;
+        for (int j = 0; j < all; ++j) before += count[j] > count[i] || (count[j] == count[i] && j < i);
+        a.order[before] = i;
+    }
 }
 
 // Least and most lo, least and most hi of 32 rows; rows behind the last see nothing.
@@ -573,7 +588,8 @@ __device__ __forceinline__ float gradient_scale(const AttentionArgs &a, int64_t 
     return ldexpf(1.0f, 13 - max(-80, min(80, ilogbf(bound))));
 }
 
-// The gradient of q: as forward, with the weights known from lse.
+// The gradient of q: as forward, with the weights known from lse.  delta is
+// dout . out of a row.
 template <typename T, int DP>
 struct QueryGradient {
     typedef Tile<T, DP> L;
@@ -584,8 +600,15 @@ struct QueryGradient {
     __device__ __forceinline__ void start(const AttentionArgs &a, const RowTile &r, float factor) {
         load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), q, a.width, r.valid, r.lane);
         load_own<T, DP>(head_at<const T>(a.dout, r.worker, r.t, r.head), dout, a.width, r.valid, r.lane);
-        const float2 stat = r.valid ? a.stats[(int64_t)r.pair * a.rows + r.row] : float2{0.0f, 0.0f};
-        off = stat.x, delta = stat.y;
+        off = r.valid ? a.lse[(r.worker * a.heads + r.head) * a.tokens + r.t] * kLog2e : 0.0f;
+        delta = 0.0f;
+#pragma unroll
+        for (int i = 0; i < L::kOwn; ++i)
+            delta = chunk_dot<T>(dout[i], load_chunk<T>(head_at<const T>(a.out, r.worker, r.t, r.head),
+                                                        (2 * i + r.lane / 32) * L::E, a.width, r.valid), delta);
+        delta += other_half(delta);
+        // For the gradients of k and v.
+        if (r.valid && r.lane < 32) a.stats[(int64_t)r.pair * a.rows + r.row] = float2{off, delta};
         up = factor;
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) acc[b] = f16_t{0};
@@ -916,11 +939,18 @@ __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(
     __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
     __shared__ float2 red[4];
-    unsigned pair;
-    int tile;
-    place(a, blockIdx.x / a.parts, pair, tile);
+    const unsigned at = blockIdx.x / a.parts;
     const int part = (int)(blockIdx.x % a.parts);
-    tile = a.tiles - 1 - tile;   // the first keys are seen by the most rows
+    // The first keys are seen by the most rows, without ranges.
+    unsigned pair = at % a.pairs;
+    int tile = (int)(at / a.pairs);
+    if (a.order && a.bound_stride) {
+        tile = a.order[at / a.kv];
+        pair = tile / a.tiles * a.kv + at % a.kv;
+        tile %= a.tiles;
+    } else if (a.order) {
+        tile = a.order[tile];
+    }
     const float up = gradient_scale<T>(a, pair / a.kv, red);
     KeyGradient<T, DP> g;
     g.start(a, pair, tile, part, up, own);
@@ -997,25 +1027,33 @@ void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, h
 
 template <typename T>
 void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_t st) {
+    a.tiles = (int32_t)tiles(a.keys, 128);
     if (a.ranges && a.tokens) {
-        const int64_t total = (a.range_stride ? n : 1) * tiles(a.rows, 32);
+        const int workers = a.range_stride ? n : 1;
+        const int64_t total = workers * tiles(a.rows, 32);
         hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_bounds_kernel<T>), dim3((unsigned)tiles(total, 8)), dim3(256), 0, st, a, total);
+        if ((int64_t)workers * a.tiles <= kMostOrdered)
+            hipLaunchKernelGGL(attention_order_kernel<T>, dim3(1), dim3(1024), 0, st, a, workers);
+        else
+            a.order = nullptr;
+    } else {
+        a.order = nullptr;
     }
-    if (a.tokens)
-        hipLaunchKernelGGL(attention_delta_kernel<T>, dim3((unsigned)(n * a.norms)), dim3(256), 0, st, a);
+    if (a.tokens && std::is_same<T, _Float16>::value)
+        hipLaunchKernelGGL(attention_norms_kernel<T>, dim3((unsigned)(n * a.norms)), dim3(256), 0, st, a);
     with_width(a.width, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
         const dim3 keys_grid((unsigned)(a.pairs * tiles(a.keys, 128) * a.parts)), rows_grid((unsigned)(a.pairs * tiles(a.rows, 128)));
-        a.tiles = (int32_t)tiles(a.keys, 128);
-        if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
-        else if (a.keys)
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);
         a.tiles = (int32_t)tiles(a.rows, 128);
         if (a.tokens && direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, true>), rows_grid, dim3(256), 0, st, a);
         else if (a.tokens)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
+        a.tiles = (int32_t)tiles(a.keys, 128);
+        if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
+        else if (a.keys)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);
     });
     if (a.parts > 1) {
         const int64_t total = (int64_t)a.pairs * a.keys;

@@ -58,6 +58,17 @@ __device__ __forceinline__ u4_t load_chunk(const T *row, int at, int width, bool
     return v;
 }
 
+// The sum of products of two chunks.
+template <typename T>
+__device__ __forceinline__ float chunk_dot(u4_t a, u4_t b, float sum) {
+    constexpr int E = 16 / (int)sizeof(T);
+    typedef T chunk_t __attribute__((ext_vector_type(E)));
+    const chunk_t x = __builtin_bit_cast(chunk_t, a), y = __builtin_bit_cast(chunk_t, b);
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum = fmaf((float)x[i], (float)y[i], sum);
+    return sum;
+}
+
 __device__ __forceinline__ f16_t multiply(f16_t c, u4_t a, u4_t b, __bf16) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8_t, a), __builtin_bit_cast(b8_t, b), c, 0, 0, 0);
 }
@@ -76,11 +87,14 @@ template <typename T, int DP>
 __device__ __forceinline__ f16_t dots(const char *tile, int row0, const u4_t (&own)[Tile<T, DP>::kOwn], int lane) {
     typedef Tile<T, DP> L;
     f16_t c = {0};
+    // Reads are on their way before the first product waits for one.
+    u4_t x[L::kOwn];
 #pragma unroll
-    for (int i = 0; i < L::kOwn; ++i) {
-        const u4_t a = *reinterpret_cast<const u4_t *>(tile + row0 * L::kRowBytes + L::at(lane % 32, 2 * i + lane / 32));
-        c = multiply(c, a, own[i], (T)0.0f);
-    }
+    for (int i = 0; i < L::kOwn; ++i)
+        x[i] = *reinterpret_cast<const u4_t *>(tile + row0 * L::kRowBytes + L::at(lane % 32, 2 * i + lane / 32));
+    if (L::kOwn <= 4) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < L::kOwn; ++i) c = multiply(c, x[i], own[i], (T)0.0f);
     return c;
 }
 
