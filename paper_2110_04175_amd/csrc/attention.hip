@@ -117,6 +117,7 @@ ForwardPlan plan_forward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
     ForwardPlan p{};
     p.tiles = (int32_t)tiles(rows, 128);
     p.blocks = pairs * p.tiles;
+    p.workspace = (size_t)p.blocks * 4;
     if (p.blocks >= kCus) return p;
     p.split = true;
     p.tiles = (int32_t)tiles(rows, 32);
@@ -131,7 +132,7 @@ ForwardPlan plan_forward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
 
 struct BackwardPlan {
     int32_t norms, parts;
-    size_t stats, largest, bounds, order, sums;   // offsets
+    size_t stats, largest, bounds, order, marks, key_marks, sums;   // offsets
     size_t workspace;
 };
 
@@ -149,6 +150,8 @@ BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t head
     p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.norms * 8, 16) * 16 : 0;
     p.bounds = at, at += (size_t)n * tiles(tokens * (heads / kv), 32) * 16;
     p.order = at, at += tiles((size_t)n * tiles(keys, 128) * 4, 16) * 16;
+    p.marks = at, at += tiles((size_t)pairs * tiles(tokens * (heads / kv), 128) * 4, 16) * 16;
+    p.key_marks = at, at += tiles((size_t)blocks * p.parts * 4, 16) * 16;
     p.sums = at, at += p.parts > 1 ? (size_t)pairs * keys * p.parts * 2 * width * 4 : 0;
     p.workspace = at;
     return p;
@@ -237,6 +240,7 @@ int relaysum_attention(int32_t n, int64_t tokens, int64_t keys, int32_t heads, i
     AttentionArgs a = attention_args(n, tokens, keys, heads, kv_heads, width, q, k, v, ranges, ranges_stride, causal,
                                      scale, out, lse);
     a.tiles = p.tiles, a.parts = p.parts, a.span = p.span;
+    a.marks = static_cast<int32_t *>(workspace);
     a.part_soft = static_cast<float2 *>(workspace);
     a.part_out = static_cast<float *>(workspace) + (size_t)a.pairs * a.rows * p.parts * 2;
     const hipStream_t st = (hipStream_t)hip_stream;
@@ -298,6 +302,8 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
     a.stats = reinterpret_cast<float2 *>(ws + p.stats);
     a.largest = reinterpret_cast<float2 *>(ws + p.largest);
     a.bounds = reinterpret_cast<int4 *>(ws + p.bounds);
+    a.marks = reinterpret_cast<int32_t *>(ws + p.marks);
+    a.key_marks = reinterpret_cast<int32_t *>(ws + p.key_marks);
     a.order = reinterpret_cast<int32_t *>(ws + p.order);
     a.part_out = reinterpret_cast<float *>(ws + p.sums);
     a.norms = p.norms, a.parts = p.parts;

@@ -203,9 +203,9 @@ struct RowTile {
     bool valid;
     Sight sight;
 
-    __device__ __forceinline__ RowTile(const AttentionArgs &a, int (&most)[4][2]) {
+    __device__ __forceinline__ RowTile(const AttentionArgs &a, unsigned block, int (&most)[4][2]) {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-        place(a, blockIdx.x, pair, tile);
+        place(a, block, pair, tile);
         worker = pair / a.kv;
         kvh = (int)(pair % a.kv);
         row = tile * 128 + wave * 32 + lane % 32;
@@ -281,31 +281,48 @@ __device__ __forceinline__ void store_rows(const AttentionArgs &a, const RowTile
             empty ? -INFINITY : kLn2 * (st.off + __builtin_amdgcn_logf(sum));
 }
 
-// The rows of a workgroup in whose sums something is not finite, once more, with
-// what they do not see kept out of them.
+// Workgroups in whose sums something is not finite leave a mark in place of
+// results, and a second kernel works on what is marked once more, with what a
+// column does not see kept out of it.  In a kernel of its own, because it takes
+// more registers, and called as a function it costs every wave of the first one
+// a stack (16 x 2048 tokens, 16 heads on 4 of 64: 161 us for 109 us).
+template <typename F>
+__device__ __forceinline__ void over_marks(const int32_t *marks, int64_t blocks, F f) {
+    for (int64_t i = blockIdx.x; i < blocks; i += gridDim.x) {
+        if (!marks[i]) continue;
+        __syncthreads();
+        f((unsigned)i);
+    }
+}
+
 template <typename T, int DP>
-__device__ __noinline__ void attention_apart(const AttentionArgs a, const RowTile r,
-                                             char (&lds)[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
-    constexpr int BN = kKeyTile<T, DP>;
-    Softmax<T, DP> st;
-    load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
-    st.clear();
-    over_keys<T, DP, BN, false>(a, r, lds, [&](const char *tile, int j) {
-        for (int b = 0; b < BN; b += 32)
-            if (r.sight.any(j + b, 32))
-                st.template step<1, true>(a, tile + b * Tile<T, DP>::kRowBytes, tile + (BN + b) * Tile<T, DP>::kRowBytes,
-                                          j + b, r.lo, r.hi, r.sight.whole(j + b, 32), room, r.lane);
+__global__ __launch_bounds__(256) void attention_apart_kernel(AttentionArgs a, int64_t blocks) {
+    constexpr int BN = kKeyTile<T, DP>, kRowBytes = Tile<T, DP>::kRowBytes;
+    __shared__ __align__(16) char lds[2][2 * BN * kRowBytes];
+    __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ int most[4][2];
+    over_marks(a.marks, blocks, [&](unsigned block) {
+        const RowTile r(a, block, most);
+        Softmax<T, DP> st;
+        load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
+        st.clear();
+        over_keys<T, DP, BN, false>(a, r, lds, [&](const char *tile, int j) {
+#pragma unroll 1
+            for (int b = 0; b < BN; b += 32)
+                if (r.sight.any(j + b, 32))
+                    st.template step<1, true>(a, tile + b * kRowBytes, tile + (BN + b) * kRowBytes, j + b, r.lo, r.hi,
+                                              r.sight.whole(j + b, 32), room[r.wave], r.lane);
+        });
+        store_rows(a, r, st, st.l + other_half(st.l));
     });
-    store_rows(a, r, st, st.l + other_half(st.l));
 }
 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_kernel(AttentionArgs a) {
     constexpr int BN = kKeyTile<T, DP>;
     __shared__ __align__(16) char lds[2][2 * BN * Tile<T, DP>::kRowBytes];
-    __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ int most[4][2];
-    const RowTile r(a, most);
+    const RowTile r(a, blockIdx.x, most);
     Softmax<T, DP> st;
     load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), st.q, a.width, r.valid, r.lane);
     st.clear();
@@ -315,10 +332,9 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_kernel(
                                              r.sight.whole(j, BN), nullptr, r.lane);
     });
     const float sum = st.l + other_half(st.l);
-    if (__syncthreads_or(r.valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY))))
-        attention_apart<T, DP>(a, r, lds, room[r.wave]);
-    else
-        store_rows(a, r, st, sum);
+    const bool again = __syncthreads_or(r.valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY)));
+    if (threadIdx.x == 0) a.marks[blockIdx.x] = again;
+    if (!again) store_rows(a, r, st, sum);
 }
 
 // Few rows: the keys are split over workgroups (parts) and their waves, each of
@@ -654,30 +670,18 @@ __device__ __forceinline__ void dq_over_keys(const AttentionArgs &a, const RowTi
     });
 }
 
-template <typename T, int DP>
-__device__ __noinline__ void attention_dq_apart(const AttentionArgs a, const RowTile r, float up,
-                                                char (&lds)[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes], char *room) {
-    QueryGradient<T, DP> g;
-    g.start(a, r, up);
-    dq_over_keys<T, DP, false, true>(a, r, g, lds, room);
-    g.store(a, r);
-}
-
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel(AttentionArgs a) {
     __shared__ __align__(16) char lds[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
-    __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ int most[4][2];
     __shared__ float2 red[4];
-    const RowTile r(a, most);
-    const float up = gradient_scale<T>(a, r.worker, red);
+    const RowTile r(a, blockIdx.x, most);
     QueryGradient<T, DP> g;
-    g.start(a, r, up);
+    g.start(a, r, gradient_scale<T>(a, r.worker, red));
     dq_over_keys<T, DP, DIRECT, false>(a, r, g, lds, nullptr);
-    if (__syncthreads_or(r.valid && not_finite(g.acc)))
-        attention_dq_apart<T, DP>(a, r, up, lds, room[r.wave]);
-    else
-        g.store(a, r);
+    const bool again = __syncthreads_or(r.valid && not_finite(g.acc));
+    if (threadIdx.x == 0) a.marks[blockIdx.x] = again;
+    if (!again) g.store(a, r);
 }
 
 // The gradients of k and v: columns are keys, 128 of a workgroup, and rows the
@@ -924,41 +928,69 @@ struct KeyGradient {
     }
 };
 
-template <typename T, int DP>
-__device__ __noinline__ void attention_dkv_apart(const AttentionArgs a, unsigned pair, int tile, int part, float up,
-                                                 RowsInLds<T, DP> (&lds)[2], char *own, char *room) {
-    KeyGradient<T, DP> g;
-    g.start(a, pair, tile, part, up, own);
-    g.template over_rows<false, true>(a, lds, room);
-    g.store(a);
-}
+// The key head, tile of keys and part of a workgroup.
+struct KeyTile {
+    unsigned pair;
+    int tile, part;
+    __device__ __forceinline__ KeyTile(const AttentionArgs &a, unsigned block) {
+        const unsigned at = block / a.parts;
+        part = (int)(block % a.parts);
+        // The first keys are seen by the most rows, without ranges.
+        pair = at % a.pairs;
+        tile = (int)(at / a.pairs);
+        if (a.order && a.bound_stride) {
+            tile = a.order[at / a.kv];
+            pair = tile / a.tiles * a.kv + at % a.kv;
+            tile %= a.tiles;
+        } else if (a.order) {
+            tile = a.order[tile];
+        }
+    }
+};
 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(AttentionArgs a) {
     __shared__ __align__(16) RowsInLds<T, DP> lds[2];
-    __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
     __shared__ float2 red[4];
-    const unsigned at = blockIdx.x / a.parts;
-    const int part = (int)(blockIdx.x % a.parts);
-    // The first keys are seen by the most rows, without ranges.
-    unsigned pair = at % a.pairs;
-    int tile = (int)(at / a.pairs);
-    if (a.order && a.bound_stride) {
-        tile = a.order[at / a.kv];
-        pair = tile / a.tiles * a.kv + at % a.kv;
-        tile %= a.tiles;
-    } else if (a.order) {
-        tile = a.order[tile];
-    }
-    const float up = gradient_scale<T>(a, pair / a.kv, red);
+    const KeyTile at(a, blockIdx.x);
     KeyGradient<T, DP> g;
-    g.start(a, pair, tile, part, up, own);
+    g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
     g.template over_rows<DIRECT, false>(a, lds, nullptr);
-    if (__syncthreads_or(g.valid && (not_finite(g.dk) || not_finite(g.dv))))
-        attention_dkv_apart<T, DP>(a, pair, tile, part, up, lds, own, room[threadIdx.x / kWave]);
-    else
+    const bool again = __syncthreads_or(g.valid && (not_finite(g.dk) || not_finite(g.dv)));
+    if (threadIdx.x == 0) a.key_marks[blockIdx.x] = again;
+    if (!again) g.store(a);
+}
+
+// What the two kernels above have marked.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_dq_apart_kernel(AttentionArgs a, int64_t blocks) {
+    __shared__ __align__(16) char lds[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
+    __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ int most[4][2];
+    __shared__ float2 red[4];
+    over_marks(a.marks, blocks, [&](unsigned block) {
+        const RowTile r(a, block, most);
+        QueryGradient<T, DP> g;
+        g.start(a, r, gradient_scale<T>(a, r.worker, red));
+        dq_over_keys<T, DP, false, true>(a, r, g, lds, room[r.wave]);
+        g.store(a, r);
+    });
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_dkv_apart_kernel(AttentionArgs a, int64_t blocks) {
+    __shared__ __align__(16) RowsInLds<T, DP> lds[2];
+    __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
+    __shared__ __align__(16) char room[4][kApartBytes<T>];
+    __shared__ float2 red[4];
+    over_marks(a.key_marks, blocks, [&](unsigned block) {
+        const KeyTile at(a, block);
+        KeyGradient<T, DP> g;
+        g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
+        g.template over_rows<false, true>(a, lds, room[threadIdx.x / kWave]);
         g.store(a);
+    });
 }
 
 // Adds up the parts of dk and dv, in their order: four entries a thread.
@@ -1013,13 +1045,17 @@ template <typename T>
 void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, hipStream_t st) {
     with_width(a.width, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        if (p.split)
+        if (p.split) {
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_split_kernel<T, DP>), dim3((unsigned)p.blocks),
                                dim3(64 * kSplitWaves<T, DP>), 0, st, a);
-        else if (direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
+            return;
+        }
+        if (direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
         else
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_apart_kernel<T, DP>), dim3((unsigned)std::min<int64_t>(p.blocks, kCus)),
+                           dim3(256), 0, st, a, p.blocks);
     });
     if (p.parts > 1)
         hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)tiles((int64_t)a.pairs * a.rows, 4)), dim3(256), 0, st, a);
@@ -1049,11 +1085,17 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, true>), rows_grid, dim3(256), 0, st, a);
         else if (a.tokens)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
+        if (a.tokens)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_apart_kernel<T, DP>), dim3(std::min(rows_grid.x, (unsigned)kCus)),
+                               dim3(256), 0, st, a, (int64_t)rows_grid.x);
         a.tiles = (int32_t)tiles(a.keys, 128);
         if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
         else if (a.keys)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);
+        if (a.keys)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_apart_kernel<T, DP>), dim3(std::min(keys_grid.x, (unsigned)kCus)),
+                               dim3(256), 0, st, a, (int64_t)keys_grid.x);
     });
     if (a.parts > 1) {
         const int64_t total = (int64_t)a.pairs * a.keys;

@@ -24,6 +24,7 @@ struct AttentionArgs {
     float2 *stats;             // [pairs][rows]: lse in powers of two, dout . out
     float2 *largest;           // [n][norms]: squared norms of rows of dout and v
     int4 *bounds;              // [n or 1][ceil(rows / 32)]: least and most lo, least and most hi
+    int32_t *marks, *key_marks;   // of each workgroup: what it has done is to be done once more
     int32_t *order;            // [n or 1][ceil(keys / 128)]: worker * tiles + tile, or NULL
     const int2 *ranges;
     float *part_out;           // [pairs][rows][parts][width]; backward: [pairs][keys][parts][2 * width], dk and dv
