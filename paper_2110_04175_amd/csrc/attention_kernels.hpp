@@ -38,6 +38,16 @@ constexpr float kForwardShift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
 template <typename T>
 constexpr float kBackwardShift = std::is_same<T, _Float16>::value ? 15.0f : 0.0f;
 
+// A kernel's arguments for what it does last.  They are read from memory there,
+// not kept in scalar registers from its start on, which would run out of them and
+// take a stack.  `a` is the kernel's first argument.
+__device__ __forceinline__ const AttentionArgs &later_arguments() {
+    typedef const __attribute__((address_space(4))) AttentionArgs *Place;
+    Place p = (Place)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const AttentionArgs *)p;
+}
+
 // The token of a row.
 __device__ __forceinline__ int token_of(const AttentionArgs &a, int row) {
     return (int)((__umulhi((unsigned)row, a.group_factor) + (unsigned)row) >> a.group_shift);
@@ -128,14 +138,22 @@ struct Softmax {
     template <int NB, bool APART>
     __device__ __forceinline__ void step(const AttentionArgs &a, const char *kt, const char *vt, int j, int lo, int hi,
                                          bool whole, char *room, int lane) {
+        f16_t s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = dots<T, DP>(kt, 32 * b, q, lane);
+        add<NB, APART>(a, s, vt, j, lo, hi, whole, room, lane);
+    }
+
+    // The same from their products with q.
+    template <int NB, bool APART>
+    __device__ __forceinline__ void add(const AttentionArgs &a, const f16_t (&s)[NB], const char *vt, int j, int lo, int hi,
+                                        bool whole, char *room, int lane) {
         const int h = lane / 32;
         float p[NB][16];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const f16_t s = dots<T, DP>(kt, 32 * b, q, lane);
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[b][i] = s[i];
-        }
+            for (int i = 0; i < 16; ++i) p[b][i] = s[b][i];
         if (!whole) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -333,23 +351,20 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_kernel(
     });
     const float sum = st.l + other_half(st.l);
     const bool again = __syncthreads_or(r.valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY)));
-    if (threadIdx.x == 0) a.marks[blockIdx.x] = again;
-    if (!again) store_rows(a, r, st, sum);
+    const AttentionArgs &later = later_arguments();
+    if (threadIdx.x == 0) later.marks[blockIdx.x] = again;
+    if (!again) store_rows(later, r, st, sum);
 }
 
 // Few rows: the keys are split over workgroups (parts) and their waves, each of
-// which walks through its own keys; waves join through LDS, parts in a second
-// kernel.
+// which walks through its own keys, 32 at a time in turn; waves join through LDS,
+// parts in a second kernel.  Keys go from memory to where the products take them.
 template <typename T, int DP>
-constexpr int kSplitWaves = sizeof(T) == 4 && DP == 256 ? 2 : 4;   // whose tiles fit LDS
-
-template <typename T, int DP>
-__global__ __launch_bounds__((64 * kSplitWaves<T, DP>)) void attention_split_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(64 * split_waves(sizeof(T), DP)) void attention_split_kernel(AttentionArgs a) {
     typedef Tile<T, DP> L;
-    constexpr int W = kSplitWaves<T, DP>;
-    constexpr int kTile = 32 * L::kRowBytes;
-    // A wave's keys and values, and later its sums.
-    constexpr int kOwnBytes = 2 * kTile > 32 * DP * 4 ? 2 * kTile : 32 * DP * 4;
+    constexpr int W = split_waves(sizeof(T), DP);
+    // A wave's values, and later its sums.
+    constexpr int kOwnBytes = std::max(32 * L::kRowBytes, 32 * DP * 4);
     __shared__ __align__(16) char lds[W][kOwnBytes];
     __shared__ __align__(16) char room[W][kApartBytes<T>];
     __shared__ float soft[W][2][32];
@@ -364,46 +379,51 @@ __global__ __launch_bounds__((64 * kSplitWaves<T, DP>)) void attention_split_ker
     const int t = valid ? token_of(a, row) : 0, head = kvh * a.group + (valid ? row - t * a.group : 0);
     const int2 range = valid ? seen(a, worker, t) : int2{0, INT_MAX};
     const int lo = range.x, hi = range.y;
+    Softmax<T, DP> st;
+    load_own<T, DP>(head_at<const T>(a.q, worker, t, head), st.q, a.width, valid, lane);
     const Sight sight = sight_of(lo, hi, valid);
 
-    Softmax<T, DP> st;
-    const T *qrow = head_at<const T>(a.q, worker, t, head);
-#pragma unroll
-    for (int i = 0; i < L::kOwn; ++i) st.q[i] = load_chunk<T>(qrow, (2 * i + lane / 32) * L::E, a.width, valid);
     const T *kbase = head_at<const T>(a.k, worker, 0, kvh), *vbase = head_at<const T>(a.v, worker, 0, kvh);
-    // Keys of this part, 32 at a time in turn.
     const int64_t from = (int64_t)part * a.span, to = min(from + a.span, (int64_t)sight.most_hi);
-    char *kt = lds[wave], *vt = kt + kTile;
-    Stage<T, DP, 32, 64, false> ks, vs;
-    float sum;
-    for (int pass = 0;; ++pass) {
-        st.clear();
-        const auto fetch = [&](int j) {
-            const int rows = min(32, a.keys - j);
-            ks.load(reinterpret_cast<const char *>(kbase + j * a.k.rs), kt, a.width, rows, lane,
-                    [&](int x) { return x * a.k.rs * (int64_t)sizeof(T); });
+    char *vt = lds[wave];
+    const auto next = [&](int64_t j) {
+        while (j < to && !sight.any((int)j, 32)) j += 32 * W;
+        return j;
+    };
+    u4_t keys[L::kOwn];
+    Stage<T, DP, 32, 64, false> vs;
+    const auto over = [&](auto apart) __attribute__((always_inline)) {
+        constexpr bool kApart = decltype(apart)::value;
+        const auto fetch = [&](int64_t j) {
+            const int rows = (int)min((int64_t)32, a.keys - j);
+            load_own<T, DP>(kbase + (j + min(lane % 32, rows - 1)) * a.k.rs, keys, a.width, lane % 32 < rows, lane);
             vs.load(reinterpret_cast<const char *>(vbase + j * a.v.rs), vt, a.width, rows, lane,
                     [&](int x) { return x * a.v.rs * (int64_t)sizeof(T); });
         };
-        int64_t j = from + 32 * wave;
-        while (j < to && !sight.any((int)j, 32)) j += 32 * W;
-        if (j < to) fetch((int)j);
+        st.clear();
+        int64_t j = next(from + 32 * wave);
+        if (!kApart && j < to) fetch(j);
+#pragma unroll 1
         while (j < to) {
-            ks.put(kt, lane);
+            // Without registers for what comes next it needs no stack.
+            if (kApart) fetch(j);
+            f16_t s[1] = {};
+#pragma unroll
+            for (int i = 0; i < L::kOwn; ++i) s[0] = multiply(s[0], keys[i], st.q[i], (T)0.0f);
             vs.put(vt, lane);
             wave_fence();
-            int64_t next = j + 32 * W;
-            while (next < to && !sight.any((int)next, 32)) next += 32 * W;
-            if (next < to) fetch((int)next);
-            if (pass)
-                st.template step<1, true>(a, kt, vt, (int)j, lo, hi, sight.whole((int)j, 32), room[wave], lane);
-            else
-                st.template step<1, false>(a, kt, vt, (int)j, lo, hi, sight.whole((int)j, 32), nullptr, lane);
+            const int64_t then = next(j + 32 * W);
+            if (!kApart && then < to) fetch(then);
+            st.template add<1, kApart>(a, s, vt, (int)j, lo, hi, sight.whole((int)j, 32), room[wave], lane);
             wave_fence();
-            j = next;
+            j = then;
         }
+    };
+    over(std::false_type());
+    float sum = st.l + other_half(st.l);
+    if (__ballot(valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY)))) {
+        over(std::true_type());
         sum = st.l + other_half(st.l);
-        if (pass || !__ballot(valid && (not_finite(st.acc) || !(fabsf(sum) < INFINITY)))) break;
     }
     // Waves join: every wave's sums [entry][column], times what brings them to
     // the largest reference.  A wave without keys has none.
@@ -451,13 +471,14 @@ __global__ __launch_bounds__((64 * kSplitWaves<T, DP>)) void attention_split_ker
             empty ? -INFINITY : kLn2 * ((top == -INFINITY ? 0.0f : top) + __builtin_amdgcn_logf(all));
 }
 
-// Parts of a row join: a wave each.
+// Parts of a row join: a workgroup a row, whose waves share out the parts.
+constexpr int kJoinWaves = 8;
+
 template <typename T>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
-    const int lane = threadIdx.x % kWave;
-    const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    if (at >= (int64_t)a.pairs * a.rows) return;
-    const int64_t pair = at / a.rows, worker = pair / a.kv;
+__global__ __launch_bounds__(64 * kJoinWaves) void attention_join_kernel(AttentionArgs a) {
+    __shared__ float sums[kJoinWaves][256];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t at = blockIdx.x, pair = at / a.rows, worker = pair / a.kv;
     const int r = (int)(at % a.rows), t = token_of(a, r), head = (int)(pair % a.kv) * a.group + r - t * a.group;
     const int2 range = seen(a, worker, t);
     const bool empty = range.x >= range.y;
@@ -470,16 +491,26 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
         all += soft[p].y * (soft[p].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(soft[p].x - top));
 #pragma unroll
     for (int m = 1; m < kWave; m *= 2) all += __shfl_xor(all, m);
-    const float inv = 1.0f / all;
-    T *out = head_at<T>(a.out, worker, t, head);
     for (int k = lane; k < a.width; k += kWave) {
+        const float *from = a.part_out + at * a.parts * a.width + k;
         float v = 0.0f;
-        for (int p = 0; p < a.parts; ++p)
-            if (soft[p].x != -INFINITY)
-                v += a.part_out[(at * a.parts + p) * a.width + k] * __builtin_amdgcn_exp2f(soft[p].x - top);
-        out[k] = (T)(empty ? 0.0f : v * inv);
+#pragma unroll 8
+        for (int p = wave; p < a.parts; p += kJoinWaves) {
+            const float x = from[(int64_t)p * a.width], own = soft[p].x;
+            v += own == -INFINITY ? 0.0f : x * __builtin_amdgcn_exp2f(own - top);
+        }
+        sums[wave][k] = v;
     }
-    if (a.lse && lane == 0)
+    __syncthreads();
+    const int k = threadIdx.x;
+    if (k < a.width) {
+        float v = sums[0][k];
+#pragma unroll
+        for (int w = 1; w < kJoinWaves; ++w) v += sums[w][k];
+        // All of its scores are -infinity: 0 / 0.
+        head_at<T>(a.out, worker, t, head)[k] = (T)(empty ? 0.0f : v * (1.0f / all));
+    }
+    if (a.lse && k == 0)
         a.lse[(worker * a.heads + head) * a.tokens + t] =
             empty ? -INFINITY : kLn2 * ((top == -INFINITY ? 0.0f : top) + __builtin_amdgcn_logf(all));
 }
@@ -680,8 +711,9 @@ __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel
     g.start(a, r, gradient_scale<T>(a, r.worker, red));
     dq_over_keys<T, DP, DIRECT, false>(a, r, g, lds, nullptr);
     const bool again = __syncthreads_or(r.valid && not_finite(g.acc));
-    if (threadIdx.x == 0) a.marks[blockIdx.x] = again;
-    if (!again) g.store(a, r);
+    const AttentionArgs &later = later_arguments();
+    if (threadIdx.x == 0) later.marks[blockIdx.x] = again;
+    if (!again) g.store(later, r);
 }
 
 // The gradients of k and v: columns are keys, 128 of a workgroup, and rows the
@@ -958,8 +990,9 @@ __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(
     g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
     g.template over_rows<DIRECT, false>(a, lds, nullptr);
     const bool again = __syncthreads_or(g.valid && (not_finite(g.dk) || not_finite(g.dv)));
-    if (threadIdx.x == 0) a.key_marks[blockIdx.x] = again;
-    if (!again) g.store(a);
+    const AttentionArgs &later = later_arguments();
+    if (threadIdx.x == 0) later.key_marks[blockIdx.x] = again;
+    if (!again) g.store(later);
 }
 
 // What the two kernels above have marked.
@@ -1047,7 +1080,7 @@ void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, h
         constexpr int DP = decltype(dp)::value;
         if (p.split) {
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_split_kernel<T, DP>), dim3((unsigned)p.blocks),
-                               dim3(64 * kSplitWaves<T, DP>), 0, st, a);
+                               dim3(64 * split_waves(sizeof(T), DP)), 0, st, a);
             return;
         }
         if (direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
@@ -1058,7 +1091,8 @@ void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, h
                            dim3(256), 0, st, a, p.blocks);
     });
     if (p.parts > 1)
-        hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)tiles((int64_t)a.pairs * a.rows, 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((int64_t)a.pairs * a.rows)),
+                           dim3(64 * kJoinWaves), 0, st, a);
 }
 
 template <typename T>

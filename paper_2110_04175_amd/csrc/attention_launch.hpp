@@ -38,6 +38,15 @@ struct AttentionArgs {
     float scale, dot_scale;    // dot_scale = scale * log2(e)
 };
 
+// The heads' width that kernels are made for.
+constexpr int padded_width(int64_t width) { return width <= 64 ? 64 : width <= 128 ? 128 : 256; }
+
+// Waves of a workgroup that has few rows: as many as LDS holds the sums of.
+constexpr int split_waves(int bytes, int padded) {
+    const int own = 32 * padded * 4 + 16 * 32 * bytes + 256;
+    return own * 8 <= 160 << 10 ? 8 : own * 4 <= 160 << 10 ? 4 : 2;
+}
+
 // Tiles of the forward pass, or the parts that the keys are split into.
 struct ForwardPlan {
     int64_t blocks;

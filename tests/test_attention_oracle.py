@@ -135,7 +135,7 @@ def test_workspaces():
     assert size > 0 and size % 4 == 0
     rc, said = forward(n=1, t=1, keys=100000, h=8, kv=1, w=128, ws=6 * BASE, size=size - 1)
     assert rc == rs.RELAYSUM_ERR_INVALID_ARG and "workspace" in said
-    assert lib.relaysum_attention_workspace(64, 2048, 2048, 16, 16, 64) == 0
+    assert 0 < lib.relaysum_attention_workspace(64, 2048, 2048, 16, 16, 64) <= 1 << 20
     assert lib.relaysum_attention_workspace(1, 1, 1, 3, 2, 64) == -1
     assert lib.relaysum_attention_backward_workspace(1, 1, 1, 3, 2, 64, 0) == -1
     assert lib.relaysum_attention_backward_workspace(1, 1, 1, 2, 2, 64, 3) == -1
