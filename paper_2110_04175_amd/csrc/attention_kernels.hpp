@@ -997,31 +997,31 @@ __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(
 
 // What the two kernels above have marked.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_dq_apart_kernel(AttentionArgs a, int64_t blocks) {
-    __shared__ __align__(16) char lds[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
+__global__ __launch_bounds__(256) void attention_grad_apart_kernel(AttentionArgs a, int64_t row_blocks, int64_t key_blocks) {
+    constexpr int kRowBytes = Tile<T, DP>::kRowBytes;
+    __shared__ __align__(16) union {
+        char keys[2][2 * kKeyTile<T, DP> * kRowBytes];
+        RowsInLds<T, DP> rows[2];
+    } lds;
+    __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * kRowBytes : 16];
     __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ int most[4][2];
     __shared__ float2 red[4];
-    over_marks(a.marks, blocks, [&](unsigned block) {
+    const int tiles = a.tiles;
+    a.tiles = (a.rows + 127) / 128;
+    over_marks(a.marks, row_blocks, [&](unsigned block) {
         const RowTile r(a, block, most);
         QueryGradient<T, DP> g;
         g.start(a, r, gradient_scale<T>(a, r.worker, red));
-        dq_over_keys<T, DP, false, true>(a, r, g, lds, room[r.wave]);
+        dq_over_keys<T, DP, false, true>(a, r, g, lds.keys, room[r.wave]);
         g.store(a, r);
     });
-}
-
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_dkv_apart_kernel(AttentionArgs a, int64_t blocks) {
-    __shared__ __align__(16) RowsInLds<T, DP> lds[2];
-    __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
-    __shared__ __align__(16) char room[4][kApartBytes<T>];
-    __shared__ float2 red[4];
-    over_marks(a.key_marks, blocks, [&](unsigned block) {
+    a.tiles = tiles;
+    over_marks(a.key_marks, key_blocks, [&](unsigned block) {
         const KeyTile at(a, block);
         KeyGradient<T, DP> g;
         g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
-        g.template over_rows<false, true>(a, lds, room[threadIdx.x / kWave]);
+        g.template over_rows<false, true>(a, lds.rows, room[threadIdx.x / kWave]);
         g.store(a);
     });
 }
@@ -1102,7 +1102,8 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
         const int workers = a.range_stride ? n : 1;
         const int64_t total = workers * tiles(a.rows, 32);
         hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_bounds_kernel<T>), dim3((unsigned)tiles(total, 8)), dim3(256), 0, st, a, total);
-        if ((int64_t)workers * a.tiles <= kMostOrdered)
+        // Not where all run at once.
+        if ((int64_t)workers * a.tiles <= kMostOrdered && (int64_t)a.pairs * a.tiles * a.parts > 2 * kCus)
             hipLaunchKernelGGL(attention_order_kernel<T>, dim3(1), dim3(1024), 0, st, a, workers);
         else
             a.order = nullptr;
@@ -1119,17 +1120,16 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, true>), rows_grid, dim3(256), 0, st, a);
         else if (a.tokens)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
-        if (a.tokens)
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_apart_kernel<T, DP>), dim3(std::min(rows_grid.x, (unsigned)kCus)),
-                               dim3(256), 0, st, a, (int64_t)rows_grid.x);
         a.tiles = (int32_t)tiles(a.keys, 128);
         if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
         else if (a.keys)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);
-        if (a.keys)
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_apart_kernel<T, DP>), dim3(std::min(keys_grid.x, (unsigned)kCus)),
-                               dim3(256), 0, st, a, (int64_t)keys_grid.x);
+        // Without rows or keys everything is 0.
+        if (a.tokens && a.keys)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_grad_apart_kernel<T, DP>),
+                               dim3(std::min(std::max(rows_grid.x, keys_grid.x), (unsigned)kCus)), dim3(256), 0, st, a,
+                               (int64_t)rows_grid.x, (int64_t)keys_grid.x);
     });
     if (a.parts > 1) {
         const int64_t total = (int64_t)a.pairs * a.keys;
