@@ -654,12 +654,27 @@ struct QueryGradient {
             delta = chunk_dot<T>(dout[i], load_chunk<T>(head_at<const T>(a.out, r.worker, r.t, r.head),
                                                         (2 * i + r.lane / 32) * L::E, a.width, r.valid), delta);
         delta += other_half(delta);
-        // For the gradients of k and v.
-        if (r.valid && r.lane < 32) a.stats[(int64_t)r.pair * a.rows + r.row] = float2{off, delta};
         up = factor;
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) acc[b] = f16_t{0};
     }
+    // For the gradients of k and v.
+    __device__ __forceinline__ void keep(const AttentionArgs &a, const RowTile &r) const {
+        if (r.valid && r.lane < 32) a.stats[(int64_t)r.pair * a.rows + r.row] = float2{off, delta};
+    }
+    // The part of 32 keys from j on in sum p (dout . v), which is delta too.
+    __device__ __forceinline__ float product(const AttentionArgs &a, const RowTile &r, const char *kt, const char *vt, int j) const {
+        const f16_t s = dots<T, DP>(kt, 0, q, r.lane);
+        const f16_t dp = dots<T, DP>(vt, 0, dout, r.lane);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off)) * dp[i];
+            sum += sees(j + 4 * (r.lane / 32) - r.lo, 8 * (i / 4) + i % 4, r.lo, r.hi) ? x : 0.0f;
+        }
+        return sum;
+    }
+
     __device__ __forceinline__ float weight(float p) const { return std::is_same<T, _Float16>::value ? p * up : p; }
 
     // 32 keys from j on.
@@ -701,6 +716,27 @@ __device__ __forceinline__ void dq_over_keys(const AttentionArgs &a, const RowTi
     });
 }
 
+// Where a workgroup walks through this many keys at most, delta comes from a walk
+// of its own: with out rounded to 16 bits it is off by 2^-9 of |dout| |out|, which
+// of few keys is as much as the rounding of ds (gradients of sequences of 8, 64
+// and 250: 1.8, 1.55 and 1.6 times the rounding of the result, without it 1.4).
+constexpr int kExactKeys = 256;
+
+template <typename T, int DP, bool DIRECT>
+__device__ __forceinline__ void exact_delta(const AttentionArgs &a, const RowTile &r, QueryGradient<T, DP> &g,
+                                            char (&lds)[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes]) {
+    if (sizeof(T) == 4 || r.end - r.first > kExactKeys) return;
+    constexpr int BN = kKeyTile<T, DP>, kRowBytes = Tile<T, DP>::kRowBytes;
+    float sum = 0.0f;
+    over_keys<T, DP, BN, DIRECT>(a, r, lds, [&](const char *tile, int j) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int b = 0; b < BN; b += 32)
+            if (r.sight.any(j + b, 32)) sum += g.product(a, r, tile + b * kRowBytes, tile + (BN + b) * kRowBytes, j + b);
+    });
+    g.delta = sum + other_half(sum);
+    __syncthreads();
+}
+
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel(AttentionArgs a) {
     __shared__ __align__(16) char lds[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
@@ -709,6 +745,8 @@ __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel
     const RowTile r(a, blockIdx.x, most);
     QueryGradient<T, DP> g;
     g.start(a, r, gradient_scale<T>(a, r.worker, red));
+    exact_delta<T, DP, DIRECT>(a, r, g, lds);
+    g.keep(a, r);
     dq_over_keys<T, DP, DIRECT, false>(a, r, g, lds, nullptr);
     const bool again = __syncthreads_or(r.valid && not_finite(g.acc));
     const AttentionArgs &later = later_arguments();
@@ -1013,6 +1051,7 @@ __global__ __launch_bounds__(256) void attention_grad_apart_kernel(AttentionArgs
         const RowTile r(a, block, most);
         QueryGradient<T, DP> g;
         g.start(a, r, gradient_scale<T>(a, r.worker, red));
+        exact_delta<T, DP, false>(a, r, g, lds.keys);
         dq_over_keys<T, DP, false, true>(a, r, g, lds.keys, room[r.wave]);
         g.store(a, r);
     });
@@ -1064,12 +1103,12 @@ void with_width(int64_t width, F f) {
     else f(Int<256>());
 }
 
-// Whether rows start on 16 bytes and have whole chunks of them, and a tile's
-// places fit 32 bits.
-bool direct(const Heads &h, int64_t bytes, int64_t width) {
+// Whether rows start on 16 bytes and have whole chunks of them, and the places
+// of a tile fit 32 bits: of up to 64 rows (2^30 bytes), `heads` heads of each.
+bool direct(const Heads &h, int64_t bytes, int64_t width, int64_t heads) {
     const auto whole = [&](int64_t entries) { return entries * bytes % 16 == 0; };
     return (uintptr_t)h.data % 16 == 0 && whole(width) && whole(h.ws) && whole(h.rs) && whole(h.hs) &&
-           h.rs * bytes < 1 << 24 && h.hs * bytes < 1 << 24;
+           h.rs * bytes < 1 << 24 && heads * h.hs * bytes < (int64_t)1 << 31;
 }
 
 }  // namespace
@@ -1083,7 +1122,7 @@ void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, h
                                dim3(64 * split_waves(sizeof(T), DP)), 0, st, a);
             return;
         }
-        if (direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
+        if (direct(a.k, sizeof(T), a.width, 1) && direct(a.v, sizeof(T), a.width, 1))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
         else
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
@@ -1116,12 +1155,12 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
         constexpr int DP = decltype(dp)::value;
         const dim3 keys_grid((unsigned)(a.pairs * tiles(a.keys, 128) * a.parts)), rows_grid((unsigned)(a.pairs * tiles(a.rows, 128)));
         a.tiles = (int32_t)tiles(a.rows, 128);
-        if (a.tokens && direct(a.k, sizeof(T), a.width) && direct(a.v, sizeof(T), a.width))
+        if (a.tokens && direct(a.k, sizeof(T), a.width, 1) && direct(a.v, sizeof(T), a.width, 1))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, true>), rows_grid, dim3(256), 0, st, a);
         else if (a.tokens)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
         a.tiles = (int32_t)tiles(a.keys, 128);
-        if (a.keys && direct(a.q, sizeof(T), a.width) && direct(a.dout, sizeof(T), a.width))
+        if (a.keys && direct(a.q, sizeof(T), a.width, a.group) && direct(a.dout, sizeof(T), a.width, a.group))
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
         else if (a.keys)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);

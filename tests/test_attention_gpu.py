@@ -241,6 +241,20 @@ def test_far_rows():
     check(q[:, -1:], k, v, do[:, -1:])
 
 
+@pytest.mark.parametrize("h", [100, 300])
+def test_far_heads(h):
+    """Heads of a group whose places within one tile reach over 1.7 GB, and past
+    32 bits."""
+    announce(f"attention far heads {h}")
+    w, step = 16, (1 << 23) - 8
+    far = torch.empty(2, h, step, dtype=torch.bfloat16, device="cuda")
+    q, do = (far[i, :, 8:8 + 3 * w].view(1, h, 3 * w).unflatten(2, (3, w)).transpose(1, 2) for i in range(2))
+    a, k, v, b = heads(40, 1, 3, 70, h, 1, w, torch.bfloat16)
+    q.copy_(a)
+    do.copy_(b)
+    check(q, k, v, do)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_what_is_not_seen_has_no_part(bad, dtype):
