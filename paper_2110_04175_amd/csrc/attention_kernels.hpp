@@ -691,7 +691,8 @@ struct QueryGradient {
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                ds[i] = sees(j + 4 * (r.lane / 32) - r.lo, 8 * (i / 4) + i % 4, r.lo, r.hi) ? ds[i] : 0.0f;
+                // A row's only key has weight 1 whatever its score is: ds is 0.
+                ds[i] = sees(j + 4 * (r.lane / 32) - r.lo, 8 * (i / 4) + i % 4, r.lo, r.hi - r.lo == 1 ? r.lo : r.hi) ? ds[i] : 0.0f;
             }
         }
         if (APART && !whole)
@@ -872,7 +873,8 @@ struct KeyGradient {
                 const i4_t x = *reinterpret_cast<const i4_t *>(&lds.sees[row0 + 8 * (i / 4) + 4 * (lane / 32) + i % 4]);
                 const bool one = sees(key - x[0], 0, x[0], x[1]), two = sees(key - x[2], 0, x[2], x[3]);
                 p[i] = one ? p[i] : 0.0f, p[i + 1] = two ? p[i + 1] : 0.0f;
-                there |= one << i | two << (i + 1);
+                // Not the gradient of a row's only key: its weight is 1 whatever its score is.
+                there |= (one && x[1] - x[0] != 1) << i | (two && x[3] - x[2] != 1) << (i + 1);
             }
         }
         if (APART && !whole)

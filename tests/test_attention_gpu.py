@@ -324,6 +324,20 @@ def test_long_sums():
     check(q, k, v, do)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_an_only_key(dtype):
+    """The weight of a row's only key is 1 whatever its score is: q and k have no
+    gradient, exactly.  out is v only up to roundings: p = 2^(s - off) is 1 up to
+    that of off, and p v is rounded and divided by p (check() counts them)."""
+    announce(f"attention of one key {dtype}")
+    for n, t, w in ((1, 1, 16), (3, 1, 100), (2, 40, 64)):
+        q, k, v, do = heads(41, n, t, t, 4, 2, w, dtype)
+        own = torch.stack([torch.arange(t), torch.arange(1, t + 1)], 1).int().cuda().unsqueeze(0)
+        for ranges in ((None, own) if t == 1 else (own,)):
+            out, lse, dq, dk, dv = check(q, k, v, do, ranges)
+            assert (dq == 0).all() and (dk == 0).all()
+
+
 def test_no_rows_and_no_keys():
     announce("attention of nothing")
     for t, keys in ((0, 5), (5, 0), (0, 0)):
