@@ -765,6 +765,12 @@ constexpr int kRowTile = Tile<T, DP>::kRowBytes > 128 ? 32 : 64;
 template <typename T, int DP>
 constexpr bool kValuesInLds = sizeof(T) == 2 && DP == 128;
 
+// Which gradients a kernel of keys gives: of more than 128 entries dk and dv one
+// after the other, since sums of both leave no registers for the keys' rows.
+enum { kBoth = 0, kOnlyValues = 1, kOnlyKeys = 2 };
+template <typename T, int DP>
+constexpr bool kOneByOne = DP > 128;
+
 template <typename T, int DP>
 struct RowsInLds {
     char rows[2][kRowTile<T, DP> * Tile<T, DP>::kRowBytes];   // q, dout
@@ -809,13 +815,13 @@ struct Walk {
     }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, int WHICH>
 struct KeyGradient {
     typedef Tile<T, DP> L;
-    static constexpr bool kInLds = kValuesInLds<T, DP>;
-    u4_t k[L::kOwn], v[kInLds ? 1 : L::kOwn];
+    static constexpr bool kInLds = kValuesInLds<T, DP>, kDk = WHICH != kOnlyValues, kDv = WHICH != kOnlyKeys;
+    u4_t k[L::kOwn], v[kInLds || !kDk ? 1 : L::kOwn];
     const char *values;   // 32 rows of v
-    f16_t dk[L::kBlocks], dv[L::kBlocks];
+    f16_t dk[kDk ? L::kBlocks : 1], dv[kDv ? L::kBlocks : 1];
     int64_t worker;
     int kvh, j0, mine, key, lane, part;
     unsigned pair;
@@ -833,7 +839,8 @@ struct KeyGradient {
         up = factor;
         load_own<T, DP>(head_at<const T>(a.k, worker, valid ? key : 0, kvh), k, a.width, valid, lane);
         const T *vrow = head_at<const T>(a.v, worker, valid ? key : 0, kvh);
-        if constexpr (kInLds) {
+        if constexpr (!kDk) {
+        } else if constexpr (kInLds) {
             char *to = own + threadIdx.x / kWave * 32 * L::kRowBytes;
             values = to;
             for (int i = 0; i < L::kOwn; ++i)
@@ -843,7 +850,9 @@ struct KeyGradient {
             load_own<T, DP>(vrow, v, a.width, valid, lane);
         }
 #pragma unroll
-        for (int b = 0; b < L::kBlocks; ++b) dk[b] = dv[b] = f16_t{0};
+        for (f16_t &x : dk) x = f16_t{0};
+#pragma unroll
+        for (f16_t &x : dv) x = f16_t{0};
     }
 
     // A weight, held times 2^kBackwardShift, times the factor of ds.
@@ -863,7 +872,8 @@ struct KeyGradient {
             for (int r = 0; r < 4; ++r) p[4 * g + r] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + r], a.dot_scale, -off[r]));
         }
         f16_t dp;
-        if constexpr (kInLds) dp = dots_in_lds<T, DP>(lds.rows[1], row0, values, 0, lane);
+        if constexpr (!kDk) dp = f16_t{0};
+        else if constexpr (kInLds) dp = dots_in_lds<T, DP>(lds.rows[1], row0, values, 0, lane);
         else dp = dots<T, DP>(lds.rows[1], row0, v, lane);
         unsigned there = 0xffff;
         if (!whole) {
@@ -877,29 +887,29 @@ struct KeyGradient {
                 there |= (one && x[1] - x[0] != 1) << i | (two && x[3] - x[2] != 1) << (i + 1);
             }
         }
-        if (APART && !whole)
-            add_rows_apart<T, DP>(dv, lds.rows[1], row0, p, room, lane, [&](int r) {
-                return sees(key - lds.sees[row0 + r].x, 0, lds.sees[row0 + r].x, lds.sees[row0 + r].y);
-            });
-        else
-            add_rows<T, DP>(dv, lds.rows[1], row0, Weights<T>(p), lane);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f4_t delta = *reinterpret_cast<const f4_t *>(&lds.stats[1][row0 + 8 * g + 4 * (lane / 32)]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) ds[4 * g + r] = scaled(p[4 * g + r]) * (dp[4 * g + r] - delta[r]);
+        const auto there_apart = [&](int r) {
+            const int2 x = lds.sees[row0 + r];
+            return sees(key - x.x, 0, x.x, x.y);
+        };
+        if constexpr (kDv) {
+            if (APART && !whole) add_rows_apart<T, DP>(dv, lds.rows[1], row0, p, room, lane, there_apart);
+            else add_rows<T, DP>(dv, lds.rows[1], row0, Weights<T>(p), lane);
         }
-        // A weight of 0 times an infinity is none.
-        if (!whole) {
+        if constexpr (kDk) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ds[i] = there >> i & 1 ? ds[i] : 0.0f;
+            for (int g = 0; g < 4; ++g) {
+                const f4_t delta = *reinterpret_cast<const f4_t *>(&lds.stats[1][row0 + 8 * g + 4 * (lane / 32)]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) ds[4 * g + r] = scaled(p[4 * g + r]) * (dp[4 * g + r] - delta[r]);
+            }
+            // A weight of 0 times an infinity is none.
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ds[i] = there >> i & 1 ? ds[i] : 0.0f;
+            }
+            if (APART && !whole) add_rows_apart<T, DP>(dk, lds.rows[0], row0, ds, room, lane, there_apart);
+            else add_rows<T, DP>(dk, lds.rows[0], row0, Weights<T>(ds), lane);
         }
-        if (APART && !whole)
-            add_rows_apart<T, DP>(dk, lds.rows[0], row0, ds, room, lane, [&](int r) {
-                return sees(key - lds.sees[row0 + r].x, 0, lds.sees[row0 + r].x, lds.sees[row0 + r].y);
-            });
-        else
-            add_rows<T, DP>(dk, lds.rows[0], row0, Weights<T>(ds), lane);
     }
 
     template <bool DIRECT, bool APART>
@@ -991,11 +1001,11 @@ struct KeyGradient {
         const float fk = a.scale / up, fv = ldexpf(1.0f, -(int)kBackwardShift<T>);
         if (a.parts > 1) {
             float *to = a.part_out + (((int64_t)pair * a.keys + key) * a.parts + part) * 2 * a.width;
-            store_column<float>(to, a.width, dk, fk, lane);
-            store_column<float>(to + a.width, a.width, dv, fv, lane);
+            if constexpr (kDk) store_column<float>(to, a.width, dk, fk, lane);
+            if constexpr (kDv) store_column<float>(to + a.width, a.width, dv, fv, lane);
         } else {
-            store_column<T>(head_at<T>(a.dk, worker, key, kvh), a.width, dk, fk, lane);
-            store_column<T>(head_at<T>(a.dv, worker, key, kvh), a.width, dv, fv, lane);
+            if constexpr (kDk) store_column<T>(head_at<T>(a.dk, worker, key, kvh), a.width, dk, fk, lane);
+            if constexpr (kDv) store_column<T>(head_at<T>(a.dv, worker, key, kvh), a.width, dv, fv, lane);
         }
     }
 };
@@ -1020,18 +1030,19 @@ struct KeyTile {
     }
 };
 
-template <typename T, int DP, bool DIRECT>
+template <typename T, int DP, bool DIRECT, int WHICH>
 __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(AttentionArgs a) {
     __shared__ __align__(16) RowsInLds<T, DP> lds[2];
     __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
     __shared__ float2 red[4];
     const KeyTile at(a, blockIdx.x);
-    KeyGradient<T, DP> g;
+    KeyGradient<T, DP, WHICH> g;
     g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
     g.template over_rows<DIRECT, false>(a, lds, nullptr);
-    const bool again = __syncthreads_or(g.valid && (not_finite(g.dk) || not_finite(g.dv)));
+    const bool again = __syncthreads_or(g.valid && ((g.kDk && not_finite(g.dk)) || (g.kDv && not_finite(g.dv))));
     const AttentionArgs &later = later_arguments();
-    if (threadIdx.x == 0) later.key_marks[blockIdx.x] = again;
+    // What the values' kernel has marked stays so.
+    if (threadIdx.x == 0 && (again || WHICH != kOnlyKeys)) later.key_marks[blockIdx.x] = again;
     if (!again) g.store(later);
 }
 
@@ -1060,10 +1071,20 @@ __global__ __launch_bounds__(256) void attention_grad_apart_kernel(AttentionArgs
     a.tiles = tiles;
     over_marks(a.key_marks, key_blocks, [&](unsigned block) {
         const KeyTile at(a, block);
-        KeyGradient<T, DP> g;
-        g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
-        g.template over_rows<false, true>(a, lds.rows, room[threadIdx.x / kWave]);
-        g.store(a);
+        const float up = gradient_scale<T>(a, at.pair / a.kv, red);
+        const auto one = [&](auto which) {
+            KeyGradient<T, DP, decltype(which)::value> g;
+            g.start(a, at.pair, at.tile, at.part, up, own);
+            g.template over_rows<false, true>(a, lds.rows, room[threadIdx.x / kWave]);
+            g.store(a);
+        };
+        if constexpr (kOneByOne<T, DP>) {
+            one(Int<kOnlyValues>());
+            __syncthreads();
+            one(Int<kOnlyKeys>());
+        } else {
+            one(Int<kBoth>());
+        }
     });
 }
 
@@ -1162,10 +1183,19 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
         else if (a.tokens)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dq_kernel<T, DP, false>), rows_grid, dim3(256), 0, st, a);
         a.tiles = (int32_t)tiles(a.keys, 128);
-        if (a.keys && direct(a.q, sizeof(T), a.width, a.group) && direct(a.dout, sizeof(T), a.width, a.group))
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true>), keys_grid, dim3(256), 0, st, a);
-        else if (a.keys)
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false>), keys_grid, dim3(256), 0, st, a);
+        const bool whole = direct(a.q, sizeof(T), a.width, a.group) && direct(a.dout, sizeof(T), a.width, a.group);
+        const auto keys = [&](auto which) {
+            constexpr int kWhich = decltype(which)::value;
+            if (whole)
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, true, kWhich>), keys_grid, dim3(256), 0, st, a);
+            else
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_dkv_kernel<T, DP, false, kWhich>), keys_grid, dim3(256), 0, st, a);
+        };
+        if constexpr (kOneByOne<T, DP>) {
+            if (a.keys) keys(Int<kOnlyValues>()), keys(Int<kOnlyKeys>());
+        } else if (a.keys) {
+            keys(Int<kBoth>());
+        }
         // Without rows or keys everything is 0.
         if (a.tokens && a.keys)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_grad_apart_kernel<T, DP>),
