@@ -150,7 +150,8 @@ BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t head
     // Rows of a key head are split over workgroups where there are few of them, at
     // least four tiles each.
     p.parts = 1;
-    while (p.parts < 32 && blocks * p.parts < 3 * kCus && 8 * p.parts * 64 <= tokens * (heads / kv)) p.parts *= 2;
+    const int64_t enough = width > 128 ? 3 * kCus / 2 : 3 * kCus;   // one or two run on a CU
+    while (p.parts < 32 && blocks * p.parts < enough && 8 * p.parts * 64 <= tokens * (heads / kv)) p.parts *= 2;
     size_t at = 0;
     p.stats = at, at += tiles((size_t)n * rows * 8, 16) * 16;
     p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.norms * 8, 16) * 16 : 0;

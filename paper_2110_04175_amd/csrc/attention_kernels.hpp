@@ -304,6 +304,11 @@ __device__ __forceinline__ void store_rows(const AttentionArgs &a, const RowTile
 // column does not see kept out of it.  In a kernel of its own, because it takes
 // more registers, and called as a function it costs every wave of the first one
 // a stack (16 x 2048 tokens, 16 heads on 4 of 64: 161 us for 109 us).
+//
+// Few workgroups look at the marks: there is seldom one, and with heads above 128
+// entries these kernels do take a stack (11 to 24 us of 256 workgroups).
+constexpr int kApartBlocks = kCus / 4;
+
 template <typename F>
 __device__ __forceinline__ void over_marks(const int32_t *marks, int64_t blocks, F f) {
     for (int64_t i = blockIdx.x; i < blocks; i += gridDim.x) {
@@ -1149,7 +1154,7 @@ void attention::launch_attention(const AttentionArgs &a, const ForwardPlan &p, h
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, true>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
         else
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_kernel<T, DP, false>), dim3((unsigned)p.blocks), dim3(256), 0, st, a);
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_apart_kernel<T, DP>), dim3((unsigned)std::min<int64_t>(p.blocks, kCus)),
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_apart_kernel<T, DP>), dim3((unsigned)std::min<int64_t>(p.blocks, kApartBlocks)),
                            dim3(256), 0, st, a, p.blocks);
     });
     if (p.parts > 1)
@@ -1199,7 +1204,7 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
         // Without rows or keys everything is 0.
         if (a.tokens && a.keys)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(attention_grad_apart_kernel<T, DP>),
-                               dim3(std::min(std::max(rows_grid.x, keys_grid.x), (unsigned)kCus)), dim3(256), 0, st, a,
+                               dim3(std::min(std::max(rows_grid.x, keys_grid.x), (unsigned)kApartBlocks)), dim3(256), 0, st, a,
                                (int64_t)rows_grid.x, (int64_t)keys_grid.x);
     });
     if (a.parts > 1) {
