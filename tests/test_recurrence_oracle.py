@@ -73,7 +73,8 @@ def forward(n=2, t=200, w=32, count=3, starts=9 * BASE, stride=4, ws=8 * BASE, s
     ("one type", dict(x=rows(2 * BASE, 2, 200, 32, 0))), ("unknown type", dict(gate=rows(BASE, 2, 200, 32, 7))),
     ("type float", dict(initial=rows(5 * BASE, 2, 3, 32))), ("type float", dict(last=rows(5 * BASE, 2, 3, 32))),
     ("share memory", dict(h=rows(BASE, 2, 200, 32))), ("share memory", dict(last=rows(3 * BASE, 2, 3, 32, 0))),
-    ("share memory", dict(saved=3 * BASE)), ("workspace", dict(size=100)), ("NULL", dict(ws=None)),
+    ("share memory", dict(saved=3 * BASE)), ("workspace", dict(t=1000, size=100)),
+    ("NULL", dict(t=1000, ws=None)),
     ("too large", dict(n=1 << 24, t=1, w=512, count=1)),
 ])
 def test_refusals(text, kw):
@@ -83,7 +84,7 @@ def test_refusals(text, kw):
 
 def test_refused_backward():
     lib = layer._lib()
-    n, t, w, count = 2, 200, 32, 1
+    n, t, w, count = 2, 1000, 32, 1
     a = [rows((i + 1) * BASE, n, t, w) for i in range(5)]   # dh, gate, x, dgate, dx
 
     def call(x, saved=7 * BASE, size=1 << 30):
@@ -105,6 +106,8 @@ def test_sizes():
     lib = layer._lib()
     assert [lib.relaysum_recurrence_chunks(t) for t in (0, 1, 64, 65, -1)] == [1, 1, 1, 2, -1]
     assert layer.CHUNK == 64
+    # Parts where there are few channels for many tokens.
     assert lib.relaysum_recurrence_workspace(3, 64, 100) == 0
-    assert lib.relaysum_recurrence_workspace(3, 65, 100) > 0
+    assert lib.relaysum_recurrence_workspace(3, 1000, 100) > 0
+    assert lib.relaysum_recurrence_workspace(16, 2048, 1024) == 0
     assert lib.relaysum_recurrence_workspace(0, 65, 100) == -1
