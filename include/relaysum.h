@@ -573,10 +573,11 @@ int relaysum_attention_ranges(int32_t n, int64_t tokens, int64_t keys, int32_t c
 /*   q, k, v, out   heads of one type, 1 <= width <= 256
  *   ranges         8-byte aligned, or NULL; ranges_stride rows between workers'
  *                  (0: all have the same)
- *   scale          positive
+ *   scale          positive, at most 2^126
  *   lse            out, float[n][heads][tokens], or NULL: for the backward pass
  *   workspace      relaysum_attention_workspace bytes, 16-byte aligned (NULL if 0):
- *                  few rows share their keys out, and join
+ *                  sums of few rows' keys that are shared out and join, or a mark
+ *                  for each tile of many rows
  * tokens * heads and keys up to 2^30. */
 int64_t relaysum_attention_workspace(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
                                      int32_t kv_heads, int64_t width);

@@ -238,7 +238,7 @@ int relaysum_attention(int32_t n, int64_t tokens, int64_t keys, int32_t heads, i
         c.heads("out", out, type, n, tokens, heads, width, true);
         if (tokens) c.ranges(ranges, ranges_stride, n, tokens, false);
         if (lse) c.span("lse", lse, (size_t)n * heads * tokens * 4, 4, true);
-        if (!(scale > 0.0f && scale < INFINITY)) c.fail(refuse("scale must be positive"));
+        if (!(scale > 0.0f && scale <= 0x1p126f)) c.fail(refuse("scale must be positive, and at most 2^126"));
         if (c.code == RELAYSUM_OK && tokens) {
             p = plan_forward(n, tokens, keys, heads, kv_heads, width, type);
             c.product_launch(p, workspace, workspace_bytes);
@@ -289,7 +289,7 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
         c.heads("dq", dq, type, n, tokens, heads, width, true);
         c.heads("dk", dk, type, n, keys, kv_heads, width, true);
         c.heads("dv", dv, type, n, keys, kv_heads, width, true);
-        if (!(scale > 0.0f && scale < INFINITY)) c.fail(refuse("scale must be positive"));
+        if (!(scale > 0.0f && scale <= 0x1p126f)) c.fail(refuse("scale must be positive, and at most 2^126"));
         if (c.code == RELAYSUM_OK) {
             p = plan_backward(n, tokens, keys, heads, kv_heads, width, type);
             const int64_t pairs = (int64_t)n * kv_heads;

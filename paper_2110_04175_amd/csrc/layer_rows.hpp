@@ -118,11 +118,10 @@ __device__ __forceinline__ void gates(float f, float &a, float &c) {
     f = f < -87.0f ? -87.0f : f > 200.0f ? 200.0f : f;
     const float t = -f * kLog2e;
     float e = __builtin_amdgcn_exp2f(t);
-    if (std::is_same<T, float>::value) {
-        // What the product with log2(e) lost.
-        const float lost = fmaf(-f, kLog2e, -t) + -f * 1.925963033500e-8f;
-        e = fmaf(e, lost * 0.69314718f, e);
-    }
+    // What the product with log2(e) lost.
+    float lost = fmaf(-f, kLog2e, -t);
+    if (std::is_same<T, float>::value) lost += -f * 1.925963033500e-8f;
+    e = fmaf(e, lost * 0.69314718f, e);
     a = __builtin_amdgcn_rcpf(1.0f + e);
     if (std::is_same<T, float>::value) a = fmaf(a, fmaf(-a, 1.0f + e, 1.0f), a);
     c = e * a;

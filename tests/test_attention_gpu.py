@@ -315,6 +315,14 @@ def test_large_scores_and_small_gradients(dtype):
     check(q, k, v, do, scale=3.0)
 
 
+@pytest.mark.parametrize("scale", [1e-42, 1e-38, 1e-20])
+def test_small_scales(scale):
+    """Scales at which every key has the same weight, in tiles and in parts."""
+    announce(f"attention scale {scale}")
+    check(*heads(42, 1, 1, 700, 4, 2, 64, torch.bfloat16), scale=scale, grad=False)
+    check(*heads(43, 2, 300, 300, 64, 64, 16, torch.float32), scale=scale, grad=False)
+
+
 def test_long_sums():
     """One row over 20,000 keys, in parts, and 1,500 rows of one head."""
     announce("attention long")
