@@ -281,6 +281,33 @@ def test_what_is_not_seen_has_no_part(bad, dtype):
     assert not torch.isfinite(out[0, late:, :, 3]).any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [48, 100, 200])
+def test_what_is_not_seen_in_many_tiles(width, dtype):
+    """As above with as many workgroups as take whole tiles of rows; workers 3, 17
+    and 39 hold what is not finite, behind two sequences or at the end of one."""
+    announce(f"attention not finite in tiles width={width} {dtype}")
+    n, t, cut, late = 40, 70, 33, 61
+    q, k, v, do = heads(44, n, t, t, 4, 2, width, dtype)
+    ends = [late if i == 3 else t for i in range(n)]
+    starts = torch.tensor([[0, cut, e] for e in ends], dtype=torch.int32, device="cuda")
+    ranges = layer.attention_ranges(starts, t)
+    good = bounds(q, k, v, do, ranges.cpu().numpy(), True, width ** -0.5, True)
+    for i, bad in ((3, float("nan")), (17, float("inf")), (39, float("nan"))):
+        for x in (q, k, v, do):
+            x[i, late:, :, 3] = bad
+    out, lse = layer.attention(q, k, v, ranges)
+    grads = layer.attention_backward(do, q, k, v, out, lse, ranges)
+    del good[1]
+    whole = [i for i in range(n) if i not in (17, 39)]
+    for got, (want, off), what in zip((out, *grads), good, ("out", "dq", "dk", "dv")):
+        near(got[whole], want[whole], off[whole], what)
+        near(got[:, :cut], want[:, :cut], off[:, :cut], what)
+        if what in ("out", "dq"):
+            near(got[:, cut:late], want[:, cut:late], off[:, cut:late], what)
+    assert not torch.isfinite(out[[17, 39], late:, :, 3]).any()
+
+
 def test_scores_that_are_not_finite():
     """A visible score of +infinity or NaN makes a row NaN; of -infinity takes
     a key out, of all keys leaves 0 / 0."""
