@@ -318,13 +318,9 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(RecurrenceArgs 
 }
 
 // The backward pass, tile by tile from the last one on.
-struct BothRuns {
-    Run ahead, back;
-};
-
 template <typename T>
 __global__ __launch_bounds__(kThreads, 4) void recurrence_grad_kernel(RecurrenceArgs a) {
-    __shared__ BothRuns runs[2][kWaves][kWave];
+    __shared__ Run runs_ahead[2][kWaves][kWave], runs_back[2][kWaves][kWave];
     const Where w(a);
     const Starts starts(a, w.worker, w.lane);
     const int first = w.part * a.per, end = min(first + a.per, a.tiles);
@@ -349,42 +345,43 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_grad_kernel(Recurrence
             xv[i] = (float)xraw[i], dv[i] = (float)draw[i];
         }
         if (tile > first) load(t0 - kTile);
-        BothRuns own{{1.0f, 0.0f}, {1.0f, 0.0f}};
+        Run ahead{1.0f, 0.0f}, back{1.0f, 0.0f};
         if (at.plain) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                own.ahead.A *= av[i];
-                own.ahead.B = fmaf(av[i], own.ahead.B, cv[i] * xv[i]);
+                ahead.A *= av[i];
+                ahead.B = fmaf(av[i], ahead.B, cv[i] * xv[i]);
             }
 #pragma unroll
-            for (int i = kSteps - 1; i >= 0; --i) own.back.B = av[i] * (own.back.B + dv[i]);
-            own.back.A = own.ahead.A;
+            for (int i = kSteps - 1; i >= 0; --i) back.B = av[i] * (back.B + dv[i]);
+            back.A = ahead.A;
         } else {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const bool in = at.inside >> i & 1, start = at.starts >> i & 1;
                 float b = cv[i] * xv[i];
                 if (start) b = fmaf(av[i], w.state(a.initial, at.sequence(i)), b);
-                own.ahead = then(own.ahead, !in ? Run{-1.0f, 0.0f} : Run{start ? -1.0f : av[i], b});
+                ahead = then(ahead, !in ? Run{-1.0f, 0.0f} : Run{start ? -1.0f : av[i], b});
             }
 #pragma unroll
             for (int i = kSteps - 1; i >= 0; --i) {
                 const bool in = at.inside >> i & 1, start = at.starts >> i & 1, final = at.ends >> i & 1;
                 // g -> a (dy + g), from a sequence's last token on from dlast alone; what
                 // passes its first one is its initial state's.
-                if (final) own.back = Run{-1.0f, w.state(a.last, at.sequence(i))};
-                own.back = !in ? Run{-1.0f, 0.0f} : then(own.back, Run{av[i], av[i] * dv[i]});
-                if (start) own.back = Run{-1.0f, 0.0f};
+                if (final) back = Run{-1.0f, w.state(a.last, at.sequence(i))};
+                back = !in ? Run{-1.0f, 0.0f} : then(back, Run{av[i], av[i] * dv[i]});
+                if (start) back = Run{-1.0f, 0.0f};
             }
         }
-        runs[tile & 1][w.wave][w.lane] = own;
+        runs_ahead[tile & 1][w.wave][w.lane] = ahead;
+        runs_back[tile & 1][w.wave][w.lane] = back;
         __syncthreads();
-        for (int k = w.wave & ~(kChunk / kSteps - 1); k < w.wave; ++k) h = runs[tile & 1][k][w.lane].ahead.from(h);
+        for (int k = w.wave & ~(kChunk / kSteps - 1); k < w.wave; ++k) h = runs_ahead[tile & 1][k][w.lane].from(h);
         float g = 0.0f;
 #pragma unroll
         for (int k = kWaves - 1; k >= 0; --k) {
             if (k == w.wave) g = carry;
-            carry = runs[tile & 1][k][w.lane].back.from(carry);
+            carry = runs_back[tile & 1][k][w.lane].from(carry);
         }
         if (t0 >= a.tokens) continue;
         if (at.plain) {
