@@ -152,6 +152,30 @@ def test_random_sequences(seed):
     check(*inputs(seed, n, t, w, count, dtype)[:3], starts, *inputs(seed, n, t, w, count, dtype)[3:])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("count", [7, 63, 64, 200])
+def test_sequences_in_parts_of_tokens(count, dtype):
+    """Few channels and many tokens, which are split: sequences that begin and end
+    within parts, at their edges (512 tokens) and over several of them, fewer and
+    more than a wave's lanes, some empty, rows in none that hold NaN."""
+    announce(f"recurrence in parts count={count} {dtype}")
+    n, t, w = 2, 3000, 70
+    rng = np.random.default_rng(count)
+    starts = [sorted(rng.integers(0, t - 20, count + 1).tolist()) for _ in range(n)]
+    starts[0][1:4] = sorted([512, 512, 1024])
+    starts[0] = sorted(starts[0])
+    starts[1][0] = 0
+    gate, x, initial, dh, dlast = inputs(16, n, t, w, count, dtype)
+    for i, s in enumerate(starts):
+        for v in (gate, x, dh):
+            v[i, :s[0]] = float("nan")
+            v[i, s[-1]:] = float("nan")
+    got = check(gate, x, initial, starts, dh, dlast)
+    for i, s in enumerate(starts):
+        for v in (got[0], got[2], got[3]):
+            assert (v[i, :s[0]] == 0).all() and (v[i, s[-1]:] == 0).all()
+
+
 def test_shared_starts():
     announce("recurrence shared starts")
     gate, x, initial, dh, dlast = inputs(3, 3, 100, 50, 2, torch.bfloat16)
