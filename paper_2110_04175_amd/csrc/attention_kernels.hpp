@@ -658,24 +658,49 @@ __device__ __forceinline__ float gradient_scale(const AttentionArgs &a, int64_t 
     return ldexpf(1.0f, 13 - max(-80, min(80, ilogbf(bound))));
 }
 
+// A column's own row in the gradients: in registers, or of more than 128 floats,
+// two of which with a sum would pass the registers of a wave, in memory.
+template <typename T, int DP>
+struct OwnRow {
+    static constexpr bool kFar = sizeof(T) == 4 && DP > 128;
+    u4_t x[kFar ? 1 : Tile<T, DP>::kOwn];
+    const T *row;
+    bool valid;
+
+    __device__ __forceinline__ void load(const T *from, int width, bool there, int lane) {
+        row = from, valid = there;
+        if constexpr (!kFar) load_own<T, DP>(from, x, width, there, lane);
+    }
+    __device__ __forceinline__ u4_t chunk(int i, int width, int lane) const {
+        if constexpr (kFar) return load_chunk<T>(row, (2 * i + lane / 32) * Tile<T, DP>::E, width, valid);
+        else return x[i];
+    }
+    // Of 32 rows of a tile from row0 on.
+    __device__ __forceinline__ f16_t products(const char *tile, int row0, int width, int lane) const {
+        if constexpr (kFar) return dots_in_memory<T, DP>(tile, row0, row, width, valid, lane);
+        else return dots<T, DP>(tile, row0, x, lane);
+    }
+};
+
 // The gradient of q: as forward, with the weights known from lse.  delta is
 // dout . out of a row.  16 x 2048 tokens, 16 heads on 4 of 64, bfloat16 132 us; 16,384
 // tokens, 8 heads on 2 of 128 800 us, 1030 TFLOP/s.
 template <typename T, int DP>
 struct QueryGradient {
     typedef Tile<T, DP> L;
-    u4_t q[L::kOwn], dout[L::kOwn];
+    OwnRow<T, DP> q, dout;
     f16_t acc[L::kBlocks];
     float off, delta, up;
 
     __device__ __forceinline__ void start(const AttentionArgs &a, const RowTile &r, float factor) {
-        load_own<T, DP>(head_at<const T>(a.q, r.worker, r.t, r.head), q, a.width, r.valid, r.lane);
-        load_own<T, DP>(head_at<const T>(a.dout, r.worker, r.t, r.head), dout, a.width, r.valid, r.lane);
+        q.load(head_at<const T>(a.q, r.worker, r.t, r.head), a.width, r.valid, r.lane);
+        dout.load(head_at<const T>(a.dout, r.worker, r.t, r.head), a.width, r.valid, r.lane);
         off = r.valid ? a.lse[(r.worker * a.heads + r.head) * a.tokens + r.t] * kLog2e : 0.0f;
         delta = 0.0f;
-#pragma unroll
+        constexpr int kAtOnce = OwnRow<T, DP>::kFar ? 4 : L::kOwn;
+#pragma unroll kAtOnce
         for (int i = 0; i < L::kOwn; ++i)
-            delta = chunk_dot<T>(dout[i], load_chunk<T>(head_at<const T>(a.out, r.worker, r.t, r.head),
+            delta = chunk_dot<T>(dout.chunk(i, a.width, r.lane), load_chunk<T>(head_at<const T>(a.out, r.worker, r.t, r.head),
                                                         (2 * i + r.lane / 32) * L::E, a.width, r.valid), delta);
         delta += other_half(delta);
         up = factor;
@@ -688,8 +713,8 @@ struct QueryGradient {
     }
     // The part of 32 keys from j on in sum p (dout . v), which is delta too.
     __device__ __forceinline__ float product(const AttentionArgs &a, const RowTile &r, const char *kt, const char *vt, int j) const {
-        const f16_t s = dots<T, DP>(kt, 0, q, r.lane);
-        const f16_t dp = dots<T, DP>(vt, 0, dout, r.lane);
+        const f16_t s = q.products(kt, 0, a.width, r.lane);
+        const f16_t dp = dout.products(vt, 0, a.width, r.lane);
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -706,8 +731,8 @@ struct QueryGradient {
     __device__ __forceinline__ void step(const AttentionArgs &a, const RowTile &r, const char *kt, const char *vt, int j,
                                          char *room) {
         const bool whole = r.sight.whole(j, 32);
-        const f16_t s = dots<T, DP>(kt, 0, q, r.lane);
-        const f16_t dp = dots<T, DP>(vt, 0, dout, r.lane);
+        const f16_t s = q.products(kt, 0, a.width, r.lane);
+        const f16_t dp = dout.products(vt, 0, a.width, r.lane);
         float ds[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -847,7 +872,7 @@ template <typename T, int DP, int WHICH>
 struct KeyGradient {
     typedef Tile<T, DP> L;
     static constexpr bool kInLds = kValuesInLds<T, DP>, kDk = WHICH != kOnlyValues, kDv = WHICH != kOnlyKeys;
-    u4_t k[L::kOwn], v[kInLds || !kDk ? 1 : L::kOwn];
+    OwnRow<T, DP> k, v;
     const char *values;   // 32 rows of v
     f16_t dk[kDk ? L::kBlocks : 1], dv[kDv ? L::kBlocks : 1];
     int64_t worker;
@@ -865,7 +890,7 @@ struct KeyGradient {
         key = mine + lane % 32;
         valid = key < a.keys;
         up = factor;
-        load_own<T, DP>(head_at<const T>(a.k, worker, valid ? key : 0, kvh), k, a.width, valid, lane);
+        k.load(head_at<const T>(a.k, worker, valid ? key : 0, kvh), a.width, valid, lane);
         const T *vrow = head_at<const T>(a.v, worker, valid ? key : 0, kvh);
         if constexpr (!kDk) {
         } else if constexpr (kInLds) {
@@ -875,7 +900,7 @@ struct KeyGradient {
                 *reinterpret_cast<u4_t *>(to + L::at(lane % 32, 2 * i + lane / 32)) =
                     load_chunk<T>(vrow, (2 * i + lane / 32) * L::E, a.width, valid);
         } else {
-            load_own<T, DP>(vrow, v, a.width, valid, lane);
+            v.load(vrow, a.width, valid, lane);
         }
 #pragma unroll
         for (f16_t &x : dk) x = f16_t{0};
@@ -891,7 +916,7 @@ struct KeyGradient {
     // 32 rows of a tile from row0 on.
     template <bool APART>
     __device__ __forceinline__ void step(const AttentionArgs &a, const RowsInLds<T, DP> &lds, int row0, bool whole, char *room) {
-        const f16_t s = dots<T, DP>(lds.rows[0], row0, k, lane);
+        const f16_t s = k.products(lds.rows[0], row0, a.width, lane);
         float p[16], ds[16];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -902,7 +927,7 @@ struct KeyGradient {
         f16_t dp;
         if constexpr (!kDk) dp = f16_t{0};
         else if constexpr (kInLds) dp = dots_in_lds<T, DP>(lds.rows[1], row0, values, 0, lane);
-        else dp = dots<T, DP>(lds.rows[1], row0, v, lane);
+        else dp = v.products(lds.rows[1], row0, a.width, lane);
         unsigned there = 0xffff;
         if (!whole) {
             there = 0;

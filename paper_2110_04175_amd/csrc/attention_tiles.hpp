@@ -113,6 +113,20 @@ __device__ __forceinline__ f16_t dots_in_lds(const char *tile, int row0, const c
     return c;
 }
 
+// The same with the columns' own rows in memory, where registers do not hold
+// them: caches do.
+template <typename T, int DP>
+__device__ __forceinline__ f16_t dots_in_memory(const char *tile, int row0, const T *own, int width, bool valid, int lane) {
+    typedef Tile<T, DP> L;
+    f16_t c = {0};
+#pragma unroll 8
+    for (int i = 0; i < L::kOwn; ++i) {
+        const u4_t a = *reinterpret_cast<const u4_t *>(tile + row0 * L::kRowBytes + L::at(lane % 32, 2 * i + lane / 32));
+        c = multiply(c, a, load_chunk<T>(own, (2 * i + lane / 32) * L::E, width, valid), (T)0.0f);
+    }
+    return c;
+}
+
 // Weights of 32 rows as operands.
 template <typename T>
 struct Weights {
