@@ -148,10 +148,10 @@ BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t head
     p.norms = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles(rows, 64), std::max<int64_t>(1, 8 * kCus / n)));
     p.norms = std::min(p.norms, 256);
     // Rows of a key head are split over workgroups where there are few of them, at
-    // least four tiles each.
+    // least four tiles each; without keys there is nothing to split.
     p.parts = 1;
     const int64_t enough = width > 128 ? 3 * kCus / 2 : 3 * kCus;   // one or two run on a CU
-    while (p.parts < 32 && blocks * p.parts < enough && 8 * p.parts * 64 <= tokens * (heads / kv)) p.parts *= 2;
+    while (blocks && p.parts < 32 && blocks * p.parts < enough && 8 * p.parts * 64 <= tokens * (heads / kv)) p.parts *= 2;
     size_t at = 0;
     p.stats = at, at += tiles((size_t)n * rows * 8, 16) * 16;
     p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.norms * 8, 16) * 16 : 0;
