@@ -137,16 +137,14 @@ ForwardPlan plan_forward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
 }
 
 struct BackwardPlan {
-    int32_t norms, parts;
-    size_t stats, largest, bounds, order, marks, key_marks, sums;   // offsets
+    int32_t parts;
+    size_t stats, bounds, order, marks, key_marks, sums;   // offsets
     size_t workspace;
 };
 
-BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t heads, int32_t kv, int64_t width, int32_t type) {
+BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t heads, int32_t kv, int64_t width) {
     BackwardPlan p{};
     const int64_t rows = tokens * heads, pairs = (int64_t)n * kv, blocks = pairs * tiles(keys, 128);
-    p.norms = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles(rows, 64), std::max<int64_t>(1, 8 * kCus / n)));
-    p.norms = std::min(p.norms, 256);
     // Rows of a key head are split over workgroups where there are few of them, at
     // least four tiles each; without keys there is nothing to split.
     p.parts = 1;
@@ -154,7 +152,6 @@ BackwardPlan plan_backward(int32_t n, int64_t tokens, int64_t keys, int32_t head
     while (blocks && p.parts < 32 && blocks * p.parts < enough && 8 * p.parts * 64 <= tokens * (heads / kv)) p.parts *= 2;
     size_t at = 0;
     p.stats = at, at += tiles((size_t)n * rows * 8, 16) * 16;
-    p.largest = at, at += type == RELAYSUM_HALF ? tiles((size_t)n * p.norms * 8, 16) * 16 : 0;
     p.bounds = at, at += (size_t)n * tiles(tokens * (heads / kv), 32) * 16;
     p.order = at, at += tiles((size_t)n * tiles(keys, 128) * 4, 16) * 16;
     p.marks = at, at += tiles((size_t)pairs * tiles(tokens * (heads / kv), 128) * 4, 16) * 16;
@@ -266,7 +263,7 @@ int64_t relaysum_attention_backward_workspace(int32_t n, int64_t tokens, int64_t
         return -1;
     }
     g_error[0] = '\0';
-    return (int64_t)plan_backward(n, tokens, keys, heads, kv_heads, width, type).workspace;
+    return (int64_t)plan_backward(n, tokens, keys, heads, kv_heads, width).workspace;
 }
 
 int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t heads, int32_t kv_heads,
@@ -291,7 +288,7 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
         c.heads("dv", dv, type, n, keys, kv_heads, width, true);
         if (!(scale > 0.0f && scale <= 0x1p126f)) c.fail(refuse("scale must be positive, and at most 2^126"));
         if (c.code == RELAYSUM_OK) {
-            p = plan_backward(n, tokens, keys, heads, kv_heads, width, type);
+            p = plan_backward(n, tokens, keys, heads, kv_heads, width);
             const int64_t pairs = (int64_t)n * kv_heads;
             if (pairs * tiles(tokens * (heads / kv_heads), 128) > kMaxBlocks || pairs * tiles(keys, 128) * p.parts > kMaxBlocks)
                 c.fail(refuse("n * kv_heads is too large"));
@@ -309,13 +306,12 @@ int relaysum_attention_backward(int32_t n, int64_t tokens, int64_t keys, int32_t
     a.dv = heads_of(dv, n, keys, kv_heads);
     char *ws = static_cast<char *>(workspace);
     a.stats = reinterpret_cast<float2 *>(ws + p.stats);
-    a.largest = reinterpret_cast<float2 *>(ws + p.largest);
     a.bounds = reinterpret_cast<int4 *>(ws + p.bounds);
     a.marks = reinterpret_cast<int32_t *>(ws + p.marks);
     a.key_marks = reinterpret_cast<int32_t *>(ws + p.key_marks);
     a.order = reinterpret_cast<int32_t *>(ws + p.order);
     a.part_out = reinterpret_cast<float *>(ws + p.sums);
-    a.norms = p.norms, a.parts = p.parts;
+    a.parts = p.parts;
     a.bound_stride = a.range_stride ? tiles(a.rows, 32) : 0;
     const hipStream_t st = (hipStream_t)hip_stream;
     with_type(q->type, [&](auto zero) { launch_attention_backward<decltype(zero)>(a, n, st); });

@@ -540,42 +540,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attention_join_kernel(Attenti
 
 // ---- backward ----------------------------------------------------------------------
 
-// For binary16: the largest squared norms of the rows of dout that see something
-// and of v's, 16 lanes a row.
-template <typename T>
-__global__ __launch_bounds__(256) void attention_norms_kernel(AttentionArgs a) {
-    __shared__ float red[2][16];
-    const int64_t worker = blockIdx.x / a.norms;
-    const int part = (int)(blockIdx.x % a.norms), lane = threadIdx.x % 16, slot = threadIdx.x / 16;
-    const auto squares = [&](const T *x) {
-        float norm = 0.0f;
-        for (int k = lane * 8; k < a.width; k += 128) {
-            float u[8];
-            load8(x + k, a.width - k, u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) norm = fmaf(u[i], u[i], norm);
-        }
-        return row_reduce<16, float, pick_sum>(norm, nullptr);
-    };
-    float most_dout = 0.0f, most_v = 0.0f;
-    for (int64_t r = (int64_t)part * 16 + slot; r < (int64_t)a.tokens * a.heads; r += (int64_t)a.norms * 16) {
-        const int t = (int)((unsigned)r / (unsigned)a.heads), head = (int)((unsigned)r % (unsigned)a.heads);
-        const int2 s = seen(a, worker, t);
-        const float norm = squares(head_at<const T>(a.dout, worker, t, head));
-        if (s.x < s.y && norm < INFINITY) most_dout = fmaxf(most_dout, norm);
-    }
-    for (int64_t r = (int64_t)part * 16 + slot; r < (int64_t)a.keys * a.kv; r += (int64_t)a.norms * 16) {
-        const float norm = squares(head_at<const T>(a.v, worker, r / a.kv, (int)(r % a.kv)));
-        if (norm < INFINITY) most_v = fmaxf(most_v, norm);
-    }
-    if (lane == 0) red[0][slot] = most_dout, red[1][slot] = most_v;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) most_dout = fmaxf(most_dout, red[0][i]), most_v = fmaxf(most_v, red[1][i]);
-        a.largest[blockIdx.x] = float2{most_dout, most_v};
-    }
-}
-
 // What blocks of 32 rows see.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_bounds_kernel(AttentionArgs a, int64_t total) {
@@ -638,25 +602,43 @@ __device__ __forceinline__ Sight block_sight(const AttentionArgs &a, int64_t wor
                  seen(a, worker, token_of(a, last)).y};
 }
 
-// The power of two that ds is held times in binary16, so that its largest is
-// below 2^15: |ds| <= 2 |dout| |v|.  Every thread of the workgroup takes part.
+// What a column's ds is held times in binary16, which loses bits below 2^-14: a
+// power of two that brings the largest that the column has had to 2^13 at least,
+// and never past the type's largest number.  Where a larger one comes by, the sums
+// so far follow, which are floats.  It is the column's own, because one of several
+// columns, or from bounds of |dout| and |v|, leaves no bits to a column where
+// another, or what it does not see, is large.
 template <typename T>
-__device__ __forceinline__ float gradient_scale(const AttentionArgs &a, int64_t worker, float2 *red) {
-    if (!std::is_same<T, _Float16>::value) return 1.0f;
-    float2 m = {0.0f, 0.0f};
-    for (int p = threadIdx.x; p < a.norms; p += 256) {
-        const float2 v = a.largest[worker * a.norms + p];
-        m.x = fmaxf(m.x, v.x), m.y = fmaxf(m.y, v.y);
-    }
+struct Held {
+    static constexpr bool kOn = std::is_same<T, _Float16>::value;
+    float up;
+
+    __device__ __forceinline__ void clear() { up = kOn ? 0x1p100f : 1.0f; }
+
+    template <int B>
+    __device__ __forceinline__ void hold(float (&ds)[16], f16_t (&sums)[B]) {
+        if constexpr (kOn) {
+            float top = 0.0f;
 #pragma unroll
-    for (int s = 1; s < kWave; s *= 2) m.x = fmaxf(m.x, __shfl_xor(m.x, s)), m.y = fmaxf(m.y, __shfl_xor(m.y, s));
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = m;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) m.x = fmaxf(m.x, red[w].x), m.y = fmaxf(m.y, red[w].y);
-    const float bound = 2.0f * sqrtf(m.x) * sqrtf(m.y);
-    if (!(bound > 0.0f)) return 1.0f;
-    return ldexpf(1.0f, 13 - max(-80, min(80, ilogbf(bound))));
-}
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(ds[i]));
+            top = fmaxf(top, other_half(top));
+            const bool more = top * up > 65504.0f && top < INFINITY;
+            if (__ballot(more)) {
+                const float to = more ? ldexpf(1.0f, 13 - ilogbf(top)) : up, f = to / up;
+#pragma unroll
+                for (int b = 0; b < B; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sums[b][i] *= f;
+                up = to;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ds[i] *= up;
+        }
+    }
+    // What the sums are to be multiplied by, with a factor of their own.  Finite:
+    // sums of zero stay zero.
+    __device__ __forceinline__ float down(float f) const { return fminf(f / up, 3e38f); }
+};
 
 // A column's own row in the gradients: in registers, or of more than 128 floats,
 // two of which with a sum would pass the registers of a wave, in memory.
@@ -690,9 +672,10 @@ struct QueryGradient {
     typedef Tile<T, DP> L;
     OwnRow<T, DP> q, dout;
     f16_t acc[L::kBlocks];
-    float off, delta, up;
+    float off, delta;
+    Held<T> held;
 
-    __device__ __forceinline__ void start(const AttentionArgs &a, const RowTile &r, float factor) {
+    __device__ __forceinline__ void start(const AttentionArgs &a, const RowTile &r) {
         q.load(head_at<const T>(a.q, r.worker, r.t, r.head), a.width, r.valid, r.lane);
         dout.load(head_at<const T>(a.dout, r.worker, r.t, r.head), a.width, r.valid, r.lane);
         off = r.valid ? a.lse[(r.worker * a.heads + r.head) * a.tokens + r.t] * kLog2e : 0.0f;
@@ -703,7 +686,7 @@ struct QueryGradient {
             delta = chunk_dot<T>(dout.chunk(i, a.width, r.lane), load_chunk<T>(head_at<const T>(a.out, r.worker, r.t, r.head),
                                                         (2 * i + r.lane / 32) * L::E, a.width, r.valid), delta);
         delta += other_half(delta);
-        up = factor;
+        held.clear();
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) acc[b] = f16_t{0};
     }
@@ -724,8 +707,6 @@ struct QueryGradient {
         return sum;
     }
 
-    __device__ __forceinline__ float weight(float p) const { return std::is_same<T, _Float16>::value ? p * up : p; }
-
     // 32 keys from j on.
     template <bool APART>
     __device__ __forceinline__ void step(const AttentionArgs &a, const RowTile &r, const char *kt, const char *vt, int j,
@@ -736,7 +717,7 @@ struct QueryGradient {
         float ds[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            ds[i] = weight(__builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off))) * (dp[i] - delta);
+            ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.dot_scale, -off)) * (dp[i] - delta);
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -744,13 +725,14 @@ struct QueryGradient {
                 ds[i] = sees(j + 4 * (r.lane / 32) - r.lo, 8 * (i / 4) + i % 4, r.lo, r.hi - r.lo == 1 ? r.lo : r.hi) ? ds[i] : 0.0f;
             }
         }
+        held.hold(ds, acc);
         if (APART && !whole)
             add_rows_apart<T, DP>(acc, kt, 0, ds, room, r.lane, [&](int x) { return j + x >= r.lo && j + x < r.hi; });
         else
             add_rows<T, DP>(acc, kt, 0, Weights<T>(ds), r.lane);
     }
     __device__ __forceinline__ void store(const AttentionArgs &a, const RowTile &r) const {
-        if (r.valid) store_column<T>(head_at<T>(a.dq, r.worker, r.t, r.head), a.width, acc, a.scale / up, r.lane);
+        if (r.valid) store_column<T>(head_at<T>(a.dq, r.worker, r.t, r.head), a.width, acc, held.down(a.scale), r.lane);
     }
 };
 
@@ -791,10 +773,9 @@ template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel(AttentionArgs a) {
     __shared__ __align__(16) char lds[2][2 * kKeyTile<T, DP> * Tile<T, DP>::kRowBytes];
     __shared__ int most[4][2];
-    __shared__ float2 red[4];
     const RowTile r(a, blockIdx.x, most);
     QueryGradient<T, DP> g;
-    g.start(a, r, gradient_scale<T>(a, r.worker, red));
+    g.start(a, r);
     exact_delta<T, DP, DIRECT>(a, r, g, lds);
     g.keep(a, r);
     dq_over_keys<T, DP, DIRECT, false>(a, r, g, lds, nullptr);
@@ -879,9 +860,9 @@ struct KeyGradient {
     int kvh, j0, mine, key, lane, part;
     unsigned pair;
     bool valid;
-    float up;
+    Held<T> held;   // with p in it, of ds times 2^kBackwardShift
 
-    __device__ __forceinline__ void start(const AttentionArgs &a, unsigned at, int tile, int turn, float factor, char *own) {
+    __device__ __forceinline__ void start(const AttentionArgs &a, unsigned at, int tile, int turn, char *own) {
         lane = threadIdx.x % kWave;
         pair = at, part = turn;
         worker = pair / a.kv;
@@ -889,7 +870,7 @@ struct KeyGradient {
         j0 = tile * 128, mine = j0 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * 32;
         key = mine + lane % 32;
         valid = key < a.keys;
-        up = factor;
+        held.clear();
         k.load(head_at<const T>(a.k, worker, valid ? key : 0, kvh), a.width, valid, lane);
         const T *vrow = head_at<const T>(a.v, worker, valid ? key : 0, kvh);
         if constexpr (!kDk) {
@@ -906,11 +887,6 @@ struct KeyGradient {
         for (f16_t &x : dk) x = f16_t{0};
 #pragma unroll
         for (f16_t &x : dv) x = f16_t{0};
-    }
-
-    // A weight, held times 2^kBackwardShift, times the factor of ds.
-    __device__ __forceinline__ float scaled(float p) const {
-        return kBackwardShift<T> != 0.0f ? p * ldexpf(up, -(int)kBackwardShift<T>) : p;
     }
 
     // 32 rows of a tile from row0 on.
@@ -953,13 +929,14 @@ struct KeyGradient {
             for (int g = 0; g < 4; ++g) {
                 const f4_t delta = *reinterpret_cast<const f4_t *>(&lds.stats[1][row0 + 8 * g + 4 * (lane / 32)]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) ds[4 * g + r] = scaled(p[4 * g + r]) * (dp[4 * g + r] - delta[r]);
+                for (int r = 0; r < 4; ++r) ds[4 * g + r] = p[4 * g + r] * (dp[4 * g + r] - delta[r]);
             }
             // A weight of 0 times an infinity is none.
             if (!whole) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) ds[i] = there >> i & 1 ? ds[i] : 0.0f;
             }
+            held.hold(ds, dk);
             if (APART && !whole) add_rows_apart<T, DP>(dk, lds.rows[0], row0, ds, room, lane, there_apart);
             else add_rows<T, DP>(dk, lds.rows[0], row0, Weights<T>(ds), lane);
         }
@@ -1051,7 +1028,7 @@ struct KeyGradient {
 
     __device__ __forceinline__ void store(const AttentionArgs &a) const {
         if (!valid) return;
-        const float fk = a.scale / up, fv = ldexpf(1.0f, -(int)kBackwardShift<T>);
+        const float fv = ldexpf(1.0f, -(int)kBackwardShift<T>), fk = held.down(a.scale * fv);
         if (a.parts > 1) {
             float *to = a.part_out + (((int64_t)pair * a.keys + key) * a.parts + part) * 2 * a.width;
             if constexpr (kDk) store_column<float>(to, a.width, dk, fk, lane);
@@ -1087,10 +1064,9 @@ template <typename T, int DP, bool DIRECT, int WHICH>
 __global__ __launch_bounds__(256, (kKeyWaves<T, DP>)) void attention_dkv_kernel(AttentionArgs a) {
     __shared__ __align__(16) RowsInLds<T, DP> lds[2];
     __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * Tile<T, DP>::kRowBytes : 16];
-    __shared__ float2 red[4];
     const KeyTile at(a, blockIdx.x);
     KeyGradient<T, DP, WHICH> g;
-    g.start(a, at.pair, at.tile, at.part, gradient_scale<T>(a, at.pair / a.kv, red), own);
+    g.start(a, at.pair, at.tile, at.part, own);
     g.template over_rows<DIRECT, false>(a, lds, nullptr);
     const bool again = __syncthreads_or(g.valid && ((g.kDk && not_finite(g.dk)) || (g.kDv && not_finite(g.dv))));
     const AttentionArgs &later = later_arguments();
@@ -1110,13 +1086,12 @@ __global__ __launch_bounds__(256) void attention_grad_apart_kernel(AttentionArgs
     __shared__ __align__(16) char own[kValuesInLds<T, DP> ? 128 * kRowBytes : 16];
     __shared__ __align__(16) char room[4][kApartBytes<T>];
     __shared__ int most[4][2];
-    __shared__ float2 red[4];
     const int tiles = a.tiles;
     a.tiles = (a.rows + 127) / 128;
     over_marks(a.marks, row_blocks, [&](unsigned block) {
         const RowTile r(a, block, most);
         QueryGradient<T, DP> g;
-        g.start(a, r, gradient_scale<T>(a, r.worker, red));
+        g.start(a, r);
         exact_delta<T, DP, false>(a, r, g, lds.keys);
         dq_over_keys<T, DP, false, true>(a, r, g, lds.keys, room[r.wave]);
         g.store(a, r);
@@ -1124,10 +1099,9 @@ __global__ __launch_bounds__(256) void attention_grad_apart_kernel(AttentionArgs
     a.tiles = tiles;
     over_marks(a.key_marks, key_blocks, [&](unsigned block) {
         const KeyTile at(a, block);
-        const float up = gradient_scale<T>(a, at.pair / a.kv, red);
         const auto one = [&](auto which) {
             KeyGradient<T, DP, decltype(which)::value> g;
-            g.start(a, at.pair, at.tile, at.part, up, own);
+            g.start(a, at.pair, at.tile, at.part, own);
             g.template over_rows<false, true>(a, lds.rows, room[threadIdx.x / kWave]);
             g.store(a);
         };
@@ -1225,8 +1199,6 @@ void attention::launch_attention_backward(AttentionArgs a, int32_t n, hipStream_
     } else {
         a.order = nullptr;
     }
-    if (a.tokens && std::is_same<T, _Float16>::value)
-        hipLaunchKernelGGL(attention_norms_kernel<T>, dim3((unsigned)(n * a.norms)), dim3(256), 0, st, a);
     with_width(a.width, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
         const dim3 keys_grid((unsigned)(a.pairs * tiles(a.keys, 128) * a.parts)), rows_grid((unsigned)(a.pairs * tiles(a.rows, 128)));

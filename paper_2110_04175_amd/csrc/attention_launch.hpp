@@ -22,7 +22,6 @@ struct AttentionArgs {
     Heads dout, dq, dk, dv;
     float *lse;                // [n][heads][tokens]
     float2 *stats;             // [pairs][rows]: lse in powers of two, dout . out
-    float2 *largest;           // [n][norms]: squared norms of rows of dout and v
     int4 *bounds;              // [n or 1][ceil(rows / 32)]: least and most lo, least and most hi
     int32_t *marks, *key_marks;   // of each workgroup: what it has done is to be done once more
     int32_t *order;            // [n or 1][ceil(keys / 128)]: worker * tiles + tile, or NULL
@@ -32,7 +31,7 @@ struct AttentionArgs {
     int64_t range_stride;      // rows between workers' ranges; 0: all have the same
     int64_t bound_stride;
     int32_t tokens, keys, heads, kv, group, width, rows;   // rows = tokens * group
-    int32_t causal, tiles, parts, span, norms;
+    int32_t causal, tiles, parts, span;
     uint32_t pairs;            // n * kv
     uint32_t group_factor, group_shift;   // row / group = (mulhi(row, factor) + row) >> shift
     float scale, dot_scale;    // dot_scale = scale * log2(e)
