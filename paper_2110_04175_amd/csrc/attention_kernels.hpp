@@ -177,8 +177,10 @@ struct Softmax {
             for (int i = 0; i < 16; ++i) top = fmaxf(top, p[b][i]);
         top = fmaxf(top, other_half(top));
         // Finite, so that the first score passes -infinity whatever the scale is.
-        if (__ballot(top > m + fminf(8.0f / a.dot_scale, 3e38f))) {
-            const float to = fmaxf(m, top);
+        const bool past = top > m + fminf(8.0f / a.dot_scale, 3e38f);
+        if (__ballot(past)) {
+            // Others' references stay: what they do not see moves no rounding of theirs.
+            const float to = past ? top : m;
             const float moved = to == -INFINITY ? 0.0f : to * a.dot_scale - kForwardShift<T>;
             const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(off - moved);
             l *= f;

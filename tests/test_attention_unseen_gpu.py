@@ -87,6 +87,37 @@ def test_large_values_and_gradients_that_are_not_seen(size, dtype):
     same(everything(q, k, v, do, ranges), want, slice(0, cuts[1]), "the first sequence")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", SIZES)
+def test_large_scores_that_are_not_seen(size, dtype):
+    """Queries and keys fifty times as large in padding and in the other sequence:
+    scores there pass the first one's by thousands, which keeps its bits."""
+    announce(f"attention beside large scores {size} {dtype}")
+    q, k, v, do, ranges = packed(6, *size, dtype)
+    cut = size[2][1]
+    want = everything(q, k, v, do, ranges)
+    q[:, cut:] *= 50
+    k[:, cut:] *= 50
+    got = everything(q, k, v, do, ranges)
+    same(got, want, slice(0, cut), "the first sequence")
+    assert all(torch.isfinite(x[:, cut:size[2][2]]).all() for x in got[:1] + got[2:])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", SIZES)
+def test_later_tokens_with_large_scores(size, dtype):
+    """As above, within one sequence: tokens from the middle of a tile on, which the
+    earlier ones do not see."""
+    announce(f"attention before large scores {size} {dtype}")
+    q, k, v, do, _ = packed(7, *size, dtype)
+    late = size[1] * 2 // 3 // 32 * 32 + 20
+    assert late < size[1]
+    want = everything(q, k, v, do, None)
+    q[:, late:] *= 50
+    k[:, late:] *= 50
+    same(everything(q, k, v, do, None)[:3], want[:3], slice(0, late), "the earlier tokens")
+
+
 @pytest.mark.parametrize("width", [64, 128, 200])
 def test_heads_of_other_keys_that_are_large(width):
     """In binary16 a key head's values and its queries' gradients take no bits from
