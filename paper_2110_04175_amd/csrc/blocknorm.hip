@@ -83,7 +83,7 @@ __global__ __launch_bounds__(block_of(TPR)) void blocknorm_kernel(BlockNormArgs 
                 // As exact as a float's, whatever the type: rstd and y follow from s in
                 // 32 bits.
                 float g = 1.0f, rest;
-                if (GATE) gates<float>(f[i], g, rest);
+                if (GATE) gates(f[i], g, rest);
                 s[j][i] = (float)(T)fmaf(scale * g, s[j][i] * inv * w[i], r[i]);
             }
             // Behind the width everything stays 0 (gates and all).
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(block_of(TPR), (TPR > 256 ? 4 : J == 1 ? 3 : 2)) vo
                 ds[j][i] = a.dsum.data ? (float)in.dsum[j][i] + own : own;
                 zh[j][i] = (float)in.z[j][i] * post_rstd;
                 float gate = 1.0f, rest = 0.0f;
-                if (GATE) gates<float>((float)in.gate[GATE ? j : 0][i], gate, rest);
+                if (GATE) gates((float)in.gate[GATE ? j : 0][i], gate, rest);
                 const float dg = ds[j][i] * gate;            // of scale * u
                 const float u = zh[j][i] * w[i];
                 if (at + i < a.width) dscale = fmaf(dg, u, dscale);

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void recurrence_part_kernel(RecurrenceArg
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             float c;
-            gates<T>((float)graw[i], av[i], c);
+            gates((float)graw[i], av[i], c);
             bv[i] = REVERSE ? (float)xraw[i] : c * (float)xraw[i];
         }
         if (!REVERSE) {
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(RecurrenceArgs 
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             float c;
-            gates<T>((float)graw[i], av[i], c);
+            gates((float)graw[i], av[i], c);
             bv[i] = c * (float)xraw[i];
         }
         if (tile + 1 < end) {
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_grad_kernel(Recurrence
         float av[kSteps], cv[kSteps], xv[kSteps], dv[kSteps], h = sraw;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            gates<T>((float)graw[i], av[i], cv[i]);
+            gates((float)graw[i], av[i], cv[i]);
             xv[i] = (float)xraw[i], dv[i] = (float)draw[i];
         }
         if (tile > first) load(t0 - kTile);
