@@ -539,10 +539,13 @@ int relaysum_linear_backward_weight(int32_t n, int64_t tokens, int64_t width, in
  * sees all keys, or with causal != 0 the keys up to t + keys - tokens: the last
  * row sees all of them.  A row that sees nothing gives zeros, an lse of -infinity,
  * and no gradient.  Keys and rows that do not see each other have no part in each
- * other's results, also where they hold infinities or NaN.
+ * other's results: not in a bit of them where all are numbers; beside infinities
+ * or NaN sums may be added up in another order.
  *
  * Scores, sums and gradients are held in 32 bits; the weights p and the gradients
- * of the scores enter the second products rounded to the arrays' type.
+ * of the scores enter the second products rounded to the arrays' type.  A row's
+ * values are added up times up to 2^8 before they are divided by its weights' sum:
+ * entries of v that are numbers give numbers up to 2^119 / keys.
  * Errors, streams, capture and the rules for arrays are those of the layer calls
  * above, relaysum_layer_error() has the text; equal inputs give equal bits. */
 

@@ -481,6 +481,11 @@ def _attention_sizes(q, k):
     return n, tokens, keys, heads, kv_heads, width
 
 
+def _scale(scale, width: int) -> float:
+    # A width of 0 is the call's to refuse.
+    return max(width, 1) ** -0.5 if scale is None else scale
+
+
 @functools.lru_cache(maxsize=1024)
 def _attention_workspace(*sizes) -> int:
     return _lib().relaysum_attention_workspace(*sizes)
@@ -509,8 +514,7 @@ def attention(q, k, v, ranges=None, causal: bool = True, scale=None, keep: bool 
     lse = torch.empty((n, heads, tokens), dtype=torch.float32, device=device) if keep else None
     lib = _lib()
     ws, size, _keep = _workspace(_attention_workspace(*sizes), device)
-    _check(lib.relaysum_attention(*sizes, rq, rk, rv, at, stride, causal,
-                                  width ** -0.5 if scale is None else scale, ro,
+    _check(lib.relaysum_attention(*sizes, rq, rk, rv, at, stride, causal, _scale(scale, width), ro,
                                   lse.data_ptr() if keep else None, ws, size, stream),
            "relaysum_attention")
     return out, lse
@@ -539,8 +543,7 @@ def attention_backward(dout, q, k, v, out, lse, ranges=None, causal: bool = True
     lib = _lib()
     ws, size, _keep = _workspace(_attention_backward_workspace(*sizes, rq.type), device)
     _check(lib.relaysum_attention_backward(*sizes, rd, rq, rk, rv, ro, lse.data_ptr(), at, stride, causal,
-                                           width ** -0.5 if scale is None else scale, *to, ws, size,
-                                           stream), "relaysum_attention_backward")
+                                           _scale(scale, width), *to, ws, size, stream), "relaysum_attention_backward")
     return tuple(into)
 
 

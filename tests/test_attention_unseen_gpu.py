@@ -5,6 +5,7 @@ import sys
 import pytest
 import torch
 
+import paper_2110_04175_amd as rs
 from paper_2110_04175_amd import layer
 
 pytestmark = pytest.mark.gpu
@@ -179,3 +180,29 @@ def test_small_weights_beside_large_values(width):
         size_k += c * most.T @ qs[:, h].abs() * (1 + 4 * d / (3 * u) + 800 * 2.0 ** -24 / (3 * u))
     off = 3 * u * size_k + u * dk.abs() + 2.0 ** -24
     assert ((got[3][0, rows, 0].double().cpu() - dk).abs() <= off).all()
+
+
+def test_heads_of_no_width_are_refused():
+    """By the call, as every other width out of range."""
+    announce("attention of no width")
+    x = torch.zeros(1, 2, 1, 0, device="cuda")
+    with pytest.raises(rs.RelaySumError, match="width"):
+        layer.attention(x, x, x)
+    with pytest.raises(rs.RelaySumError, match="width"):
+        layer.attention_backward(x, x, x, x, x, torch.zeros(1, 1, 2, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,n", [(1, 1), (300, 64)])
+def test_the_largest_values(tokens, n, dtype):
+    """Values near 2^119 / keys, of few rows and of many, whose scores rise slowly
+    from key to key, so that references stay behind: results are the values."""
+    announce(f"attention of the largest values {tokens} {n} {dtype}")
+    keys, width = 300, 16
+    big = 2.0 ** 119 / keys * 0.99
+    q = torch.ones(n, tokens, 1, width, dtype=dtype, device="cuda")
+    k = (torch.arange(keys, device="cuda") * 2.0 ** -8).view(1, keys, 1, 1).expand(n, keys, 1, width).to(dtype).contiguous()
+    v = torch.full((n, keys, 1, width), big, dtype=dtype, device="cuda")
+    out, _ = layer.attention(q, k, v, causal=False, scale=1.0)
+    half = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}[dtype]
+    assert ((out.double() / v[0, 0, 0, 0].double() - 1).abs() <= 3 * half + 700 * 2.0 ** -24).all()
