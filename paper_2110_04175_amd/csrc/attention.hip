@@ -118,16 +118,27 @@ ForwardPlan plan_forward(int32_t n, int64_t tokens, int64_t keys, int32_t heads,
     p.tiles = (int32_t)tiles(rows, 128);
     p.blocks = pairs * p.tiles;
     p.workspace = (size_t)p.blocks * 4;
-    // Tiles of 128 rows are better where they are full and occupy a quarter of the
-    // CUs: 6 key heads, 2331 rows and 777 keys each of 80 binary16 entries take 25 us
-    // in 114 tiles, 41 us in parts; 64 key heads, 3 rows and 1024 keys 22 us in tiles,
-    // 18 us in parts.
+    // Tiles of 128 rows, whose waves share keys in LDS, where they are full and occupy
+    // a quarter of the CUs.  Causal prompts in bfloat16, us in tiles and in parts, heads
+    // of 64 | 128:
+    //   114 tiles,  777 keys, 3 workers   19,  24 |  27,  52
+    //    64 tiles, 2048 keys, 4 on 4      37,  53 |  54,  90
+    //    64 tiles, 1024 keys, 8 on 8      23,  16 |  33,  34
+    //    32 tiles, 4096 keys, 1 on 1      66,  43 |  97,  77
+    //    32 tiles,  512 keys, 8 on 8      15,  12 |  22,  25
+    //    32 tiles,  256 keys, 16 on 16    12,  10 |  16,  22
+    //    64 tiles of 96 rows, 1024 keys   22,  18 |  33,  40
+    // So the border is not sharp: full tiles of short prompts lose by a third at heads
+    // of 64 (of floats by half), parts below it by up to a third at heads of 128.
     if (p.blocks >= kCus || (rows >= 128 && p.blocks >= kCus / 4)) return p;
     p.split = true;
     const int64_t waves = split_waves((int)type_bytes(type), padded_width(width));
     p.tiles = (int32_t)tiles(rows, 32);
     const int64_t base = pairs * p.tiles;
-    // Up to four steps of each wave need no parts, which cost a second kernel.
+    // Up to four steps of each wave need no parts, which cost a second kernel.  A row's
+    // three heads on each key head of 64 bfloat16 entries, us with parts from 2, 4 and
+    // 8 steps on: 16 key heads and 1024 keys 11.9, 12.8, 12.8, 2048 keys 11.9, 13.3, 18.9;
+    // 256 key heads 26, 17, 17 and 35, 35, 27.
     const int64_t want = keys <= 4 * 32 * waves ? 1 : std::min<int64_t>(tiles(keys, 64 * waves), tiles(2 * kCus, std::max<int64_t>(1, base)));
     p.span = (int32_t)std::max<int64_t>(32, tiles(tiles(keys, want), 32) * 32);
     p.parts = (int32_t)std::max<int64_t>(1, tiles(keys, p.span));

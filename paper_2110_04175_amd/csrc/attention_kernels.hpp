@@ -117,11 +117,14 @@ __device__ __forceinline__ Sight sight_of(int lo, int hi, bool valid) {
 //
 // 128 rows a workgroup, tiles of 64 keys (of 128 floats or more 32) and their
 // values by turns in two halves of LDS, which all four waves read.  Of heads of 64
-// the vector unit bounds it: for 32 x 32 scores 8 matrix instructions and some 140
-// others, of them 16 exponentials; it is busy 72% at 16 x 2048 tokens, 16 heads on
-// 4, bfloat16 (102 us, 525 TFLOP/s).  Of 128 matrix instructions come nearer: one
-// sequence of 16,384, 8 heads on 2: 590 us, 930 TFLOP/s.  All reads of a product
-// in front of it: 4% quicker with 64 entries, 10% slower with 128 (registers).
+// vector instructions bound it: for 32 x 64 scores 16 matrix instructions and some
+// 155 others where nothing is masked, 32 of them exponentials; masks are 96 more, a
+// reference that moves 68, and a quarter of all are in front of the loop and behind
+// it.  At 16 x 2048 tokens in three texts, 16 heads on 4, bfloat16, vector units are
+// busy 72%, matrix units 29% (92 us, the call 98: 545 TFLOP/s).  Of 128 matrix units
+// are busy half of the time: one sequence of 16,384, 8 heads on 2: 580 us, 950 TFLOP/s.
+// All reads of a product in front of it: 4% quicker with 64 entries, 10% slower
+// with 128 (registers).
 //
 // One pass over the keys: `off` is the column's reference (a maximum of its
 // scores so far, in powers of two), l this lane's sum of the weights
@@ -667,7 +670,7 @@ struct OwnRow {
 };
 
 // The gradient of q: as forward, with the weights known from lse.  delta is
-// dout . out of a row.  16 x 2048 tokens, 16 heads on 4 of 64, bfloat16 132 us; 16,384
+// dout . out of a row.  16 x 2048 tokens, 16 heads on 4 of 64, bfloat16 128 us; 16,384
 // tokens, 8 heads on 2 of 128 800 us, 1030 TFLOP/s.
 template <typename T, int DP>
 struct QueryGradient {
@@ -789,7 +792,7 @@ __global__ __launch_bounds__(256, (kQueryWaves<T, DP>)) void attention_dq_kernel
 
 // The gradients of k and v: columns are keys, 128 of a workgroup, and rows the
 // queries that see them, in tiles of 32 or 64.  Four products of the seven of both
-// kernels: 235 us where dq takes 132, and 1200 (910 TFLOP/s) where it takes 800.
+// kernels: 231 us where dq takes 128, and 1130 (970 TFLOP/s) where it takes 800.
 // Two waves a SIMD, which wait half of the time for LDS and each other; three do
 // not fit the registers.  Loads are used a tile later, in put(): used where they
 // are issued they would wait for all copies on their way (9.2 ms for 3.0).

@@ -13,7 +13,7 @@
 //   dweight = sum dy * sh,  dpost_weight = sum ds * scale * g * zh,  dscale = sum ds * g * u
 //
 // Bound by memory: a row stays in registers from its first load to its last store.
-// 16 x 2048 x 1024 bfloat16 with what the backward pass needs 79 us (5.1 TB/s).
+// 16 x 2048 x 1024 bfloat16 with what the backward pass needs 82 us (4.9 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -163,7 +163,7 @@ struct GradRow {
 // A workgroup owns every parts-th block of rows of one worker; threads keep
 // their columns' sums in registers over all of them and, but in workgroups of
 // 1024 (which have 128 registers), the worker's weights and the next row: at
-// 16 x 2048 x 1024 bfloat16 119 us (4.2 TB/s) for 268 us without them.
+// 16 x 2048 x 1024 bfloat16 118 us (4.3 TB/s) for 268 us without them.
 template <typename T, int TPR, int J, bool GATE>
 __global__ __launch_bounds__(block_of(TPR), (TPR > 256 ? 4 : J == 1 ? 3 : 2)) void blocknorm_grad_kernel(BlockNormGradArgs a) {
     constexpr int kRows = block_of(TPR) / TPR;
