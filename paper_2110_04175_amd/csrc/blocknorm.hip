@@ -52,6 +52,15 @@ __device__ __forceinline__ float row_rstd(float (&v)[J][8], float width, float e
     return scaled_rstd<TPR, J>(v, width, eps, rstd, redf, redu);
 }
 
+// A sum of floats rounded to T: to a float first, as in the other types.  The fused
+// instruction of binary16 would round but once, and 6 sums of 100,000 that lie next to
+// the middle of two neighbours the other way than the same rows as floats.
+template <typename T>
+__device__ __forceinline__ float rounded(float v) {
+    if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(v));
+    return (float)(T)v;
+}
+
 template <typename T, int TPR, int J, bool GATE, bool KEEP>
 __global__ __launch_bounds__(block_of(TPR)) void blocknorm_kernel(BlockNormArgs a) {
     __shared__ float redf[16];
@@ -84,7 +93,7 @@ __global__ __launch_bounds__(block_of(TPR)) void blocknorm_kernel(BlockNormArgs 
                 // 32 bits.
                 float g = 1.0f, rest;
                 if (GATE) gates(f[i], g, rest);
-                s[j][i] = (float)(T)fmaf(scale * g, s[j][i] * inv * w[i], r[i]);
+                s[j][i] = rounded<T>(fmaf(scale * g, s[j][i] * inv * w[i], r[i]));
             }
             // Behind the width everything stays 0 (gates and all).
             if (a.width - at < 8) {
